@@ -1,0 +1,563 @@
+"""Operators of a denoiser trained and sampled on packed sequences.
+
+Images and clips of several resolutions lie one after another in one sequence
+(a document each).  Four operators work on such a batch:
+
+* ``rope``: rotary positions with several axes (time, height, width) on the
+  query and key heads, and the gradient;
+* ``mask``: which keys each query row attends, from the documents' lengths;
+* ``attn``: attention within the documents, optionally causal or with a
+  prefix that every row sees, with tanh-capped scores and a bias linear in the
+  distance, and the gradient;
+* ``clip``: the global norm over all gradient tensors, and clipping.
+
+A case is one pass through one operator; ``train`` cases run forward and
+backward.  With ``own`` false everything is computed by elementary torch
+operations in float32, document by document; ``exact`` is the definition in
+float64.
+"""
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+
+# ---- cases ---------------------------------------------------------------------
+
+
+def _rope(name, dtype, train, tokens, heads, dim, axes, pairs, extent):
+    case = dict(op="rope", dtype=dtype, train=train, tokens=tokens, heads=heads, dim=dim,
+                axes=axes, pairs=pairs, extent=extent)
+    return dict(case, name=name) if name else case
+
+
+def _mask(name, docs, tokens, pad, kind, mix):
+    case = dict(op="mask", docs=docs, tokens=tokens, pad=pad, kind=kind, mix=mix)
+    return dict(case, name=name) if name else case
+
+
+def _attn(name, train, docs, tokens, pad, keys, heads, kv, dim, kind, cap, bias, mix):
+    case = dict(op="attn", train=train, docs=docs, tokens=tokens, pad=pad, keys=keys, heads=heads,
+                kv=kv, dim=dim, kind=kind, cap=cap, bias=bias, mix=mix)
+    return dict(case, name=name) if name else case
+
+
+def _clip(name, dtype, count, total, max_norm, mix):
+    case = dict(op="clip", dtype=dtype, count=count, total=total, max_norm=max_norm, mix=mix)
+    return dict(case, name=name) if name else case
+
+
+def listed():
+    return [
+        # sampling with guidance: two latents of 16 x 16 patches, query and key
+        # heads of a 768-wide block; the smallest call, launch-bound
+        _rope("rope-sample-512x24x64", "bf16", False, 512, 24, 64, 2, "adjacent", 16),
+        # a training batch of eight 1024-token images, 16 + 16 heads of 88
+        _rope("rope-train-8192x32x88", "bf16", True, 8192, 32, 88, 2, "halves", 32),
+        # a video clip of odd extents in float32, three axes
+        _rope("rope-video-15795x16x64", "f32", True, 15795, 16, 64, 3, "adjacent", 45),
+        # the mask of an ordinary training batch of 256-token images
+        _mask("mask-16docs-4096", 16, 4096, 0, "doc", 1),
+        # a large batch of captions and thumbnails, many of them short, some
+        # empty, a prefix in each, padding at the end
+        _mask("mask-1500docs-131072", 1500, 131072, 777, "prefix", 2),
+        # sampling with guidance: two 256-token latents, 12 heads
+        _attn("attn-sample-512x12x64", False, 2, 512, 0, 0, 12, 12, 64, "doc", 0.0, False, 3),
+        # training, a packed batch of ragged resolutions with a padded tail
+        _attn("attn-ragged-4096x12x64", True, 21, 4096, 95, 0, 12, 12, 64, "doc", 0.0, False, 4),
+        # training, 1408 channels as 16 heads of 88, capped scores
+        _attn("attn-capped-8192x16x88", True, 8, 8192, 0, 0, 16, 16, 88, "doc", 30.0, False, 5),
+        # training, image tokens reading text tokens of their own document
+        _attn("attn-cross-4096x16x88", True, 16, 4096, 0, 1232, 16, 16, 88, "doc", 0.0, False, 6),
+        # training, long clips of an autoregressive video model: shared key
+        # heads, a prefix of given frames, a bias that fades with distance
+        _attn("attn-video-12240x16x128", True, 2, 12240, 1, 0, 16, 4, 128, "prefix", 0.0, True, 7),
+        # the gradients of a 64x64x320 stage, about 11 million in float32
+        _clip("clip-48x11M", "f32", 48, 11272960, 1.0, 8),
+        # the gradients of a 16x16x1280 stage and what surrounds it, mixed types
+        _clip("clip-210x160M", "mixed", 210, 160600003, 1.0, 9),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    most = {}
+    for c in listed():
+        w = work(c)
+        for k in w:
+            most[k] = max(most.get(k, 0.0), w[k])
+    while True:
+        case = _draw(rng)
+        w = work(case)
+        if all(w[k] <= most[k] for k in w):
+            return case
+
+
+def _draw(rng):
+    op = rng.choice(("rope", "mask", "attn", "attn", "attn", "clip"))
+    mix = rng.randrange(1 << 30)
+    if op == "rope":
+        dim = rng.choice((32, 40, 64, 72, 80, 88, 96, 128))
+        return _rope(None, rng.choice(("bf16", "bf16", "f32")), rng.random() < 0.6,
+                     _log(rng, 64, 20000), _log(rng, 2, 48), dim, rng.choice((1, 2, 3)),
+                     rng.choice(("adjacent", "halves")), _log(rng, 4, 128))
+    if op == "mask":
+        tokens = _log(rng, 64, 131072)
+        docs = min(tokens // 2, _log(rng, 1, 1500))
+        pad = rng.choice((0, 1, tokens // 17))
+        return _mask(None, docs, tokens, pad, rng.choice(("doc", "causal", "prefix")), mix)
+    if op == "attn":
+        tokens = _log(rng, 128, 12240)
+        docs = min(tokens // 2, _log(rng, 1, 40))
+        pad = rng.choice((0, 0, 1, tokens // 17))
+        kind = rng.choice(("doc", "doc", "causal", "prefix"))
+        keys = 0
+        if kind == "doc" and rng.random() < 0.3:
+            keys = docs * _log(rng, 1, 300) + rng.randint(0, 60)
+        kv = rng.choice((1, 2, 4, 6, 8, 12))
+        heads = kv * rng.choice((1, 1, 2, 4))
+        return _attn(None, rng.random() < 0.7, docs, tokens, pad, keys, min(heads, 24) // kv * kv,
+                     kv, rng.choice((32, 40, 64, 64, 72, 80, 88, 96, 120, 128)), kind,
+                     rng.choice((0.0, 0.0, 20.0, 50.0)), rng.random() < 0.3, mix)
+    count = _log(rng, 1, 210)
+    return _clip(None, rng.choice(("f32", "bf16", "mixed")), count,
+                 max(count, _log(rng, 10000, 160000000)), rng.choice((1.0, 1.0, 1e6)), mix)
+
+
+# ---- sizes that follow from a case ------------------------------------------------
+
+
+def _split(total, n, rng, least):
+    """n lengths of at least `least` that sum to total, unevenly."""
+    w = [rng.lognormvariate(0.0, 0.7) for _ in range(n)]
+    room = total - n * least
+    s = sum(w)
+    out = [least + int(room * x / s) for x in w]
+    out[rng.randrange(n)] += total - sum(out)
+    return out
+
+
+def _offsets(lens):
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    return off
+
+
+def _docs(case):
+    """Offsets of the documents' queries and keys, and their prefixes."""
+    rng = random.Random(case["mix"])
+    n, body = case["docs"], case["tokens"] - case["pad"]
+    if case["op"] == "mask" and n > 100:  # some documents are empty
+        lens = _split(body, n - n // 50, rng, 1)
+        for _ in range(n // 50):
+            lens.insert(rng.randrange(len(lens) + 1), 0)
+    elif case["op"] == "attn" and body % n == 0 and case["pad"] == 0 and n % 2 == 0:
+        # one resolution
+        lens = [body // n] * n
+    else:
+        lens = _split(body, n, rng, 1)
+    keys = _split(case["keys"], n, rng, 1) if case.get("keys") else lens
+    prefix = [rng.randint(0, k // 3 + 1) for k in keys]
+    return _offsets(lens), _offsets(keys), prefix
+
+
+def _spans(case):
+    """(lo, hi, pos, doc) of every query row, as numpy int64."""
+    qo, ko, prefix = (np.array(x, dtype=np.int64) for x in _docs(case))
+    i = np.arange(case["tokens"], dtype=np.int64)
+    doc = np.searchsorted(qo, i, side="right") - 1
+    inside = i < qo[-1]
+    d = np.where(inside, doc, 0)
+    nq, nk = qo[d + 1] - qo[d], ko[d + 1] - ko[d]
+    pos = ko[d] + nk - nq + i - qo[d]
+    lo, hi = ko[d], ko[d + 1]
+    if case["kind"] != "doc":
+        seen = pos + 1
+        if case["kind"] == "prefix":
+            seen = np.maximum(seen, lo + prefix[d])
+        hi = np.minimum(hi, seen)
+    empty = ~inside | (hi <= lo)
+    lo, hi = np.where(empty, 0, lo), np.where(empty, 0, hi)
+    return np.stack([lo, hi, np.where(inside, pos, 0), np.where(inside, doc, -1)], axis=1)
+
+
+def _sizes(case):
+    rng = random.Random(case["mix"])
+    n, total = case["count"], case["total"]
+    small = [min(1280, max(1, total // (4 * n)))] * (n // 3)  # biases and gains
+    big = _split(total - sum(small), n - len(small), rng, 1)
+    sizes = small + big
+    rng.shuffle(sizes)
+    types = [case["dtype"] if case["dtype"] != "mixed" else rng.choice(("f32", "f32", "bf16"))
+             for _ in sizes]
+    return sizes, types
+
+
+def _axis_dims(case):
+    """Channels per axis: even, near equal, the first axes take the rest."""
+    half, a = case["dim"] // 2, case["axes"]
+    return [2 * (half // a + (1 if i < half % a else 0)) for i in range(a)]
+
+
+def work(case):
+    if case["op"] == "rope":
+        n = case["tokens"] * case["heads"] * case["dim"] * (2 if case["train"] else 1)
+        esz = 2 if case["dtype"] == "bf16" else 4
+        return dict(bytes=float(2 * n * esz + 4 * case["tokens"] * case["axes"]), flops=3.0 * n)
+    if case["op"] == "mask":
+        return dict(bytes=float(16 * case["tokens"] + 8 * case["docs"]), flops=0.0)
+    if case["op"] == "clip":
+        sizes, types = _sizes(case)
+        by = sum(s * (2 if t == "bf16" else 4) for s, t in zip(sizes, types))
+        return dict(bytes=float(2 * by), flops=3.0 * case["total"])
+    rows = _spans(case)
+    pairs = float(np.sum(rows[:, 1] - rows[:, 0]))
+    t, h, kv, d = case["tokens"], case["heads"], case["kv"], case["dim"]
+    keys = case["keys"] or t
+    per = (2 * h * t + 2 * kv * keys) * d * 2.0 + 16.0 * t  # q, o, k, v in bf16 and the mask
+    # forward: q k and p v; backward: s again, dp, dq, dk, dv
+    return dict(bytes=per * (2 if case["train"] else 1),
+                flops=(14.0 if case["train"] else 4.0) * pairs * h * d)
+
+
+# ---- inputs -------------------------------------------------------------------------
+
+
+_TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _inputs(case, seed):
+    dev = "cuda"
+    gen = torch.Generator(device=dev).manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device=dev, dtype=torch.float32)
+
+    if case["op"] == "rope":
+        # the query and key heads inside a projection that also holds the values
+        t, h, d = case["tokens"], case["heads"], case["dim"]
+        dt = _TYPES[case["dtype"]]
+        x = normal(t, h + h // 2, d).to(dt)[:, :h]
+        i = torch.arange(t, device=dev)
+        e = case["extent"]
+        shift = int(torch.randint(0, 8, (1,), generator=gen, device=dev))
+        grid = [(i // e ** (case["axes"] - 1 - a)) % (2 * e) + shift for a in range(case["axes"])]
+        pos = torch.stack(grid, dim=1).float()
+        freq = torch.cat([1e4 ** (-torch.arange(0, n, 2, device=dev).double() / n)
+                          for n in _axis_dims(case)]).float()
+        return dict(x=x, g=normal(t, h, d).to(dt) if case["train"] else None, pos=pos, freq=freq)
+    if case["op"] == "mask":
+        qo, _, prefix = _docs(case)
+        # the same lengths in another order
+        perm = torch.randperm(case["docs"], generator=gen, device=dev)
+        lens = torch.tensor(qo, device=dev).diff()[perm]
+        off = torch.zeros(case["docs"] + 1, dtype=torch.int32, device=dev)
+        off[1:] = lens.cumsum(0)
+        return dict(off=off, prefix=torch.tensor(prefix, dtype=torch.int32, device=dev)[perm])
+    if case["op"] == "clip":
+        sizes, types = _sizes(case)
+        grads, outs = [], []
+        flat = {t: (normal(sum(s for s, u in zip(sizes, types) if u == t))) for t in set(types)}
+        at = {t: 0 for t in flat}
+        for s, t in zip(sizes, types):
+            grads.append(flat[t][at[t]:at[t] + s])
+            at[t] += s
+        scale = torch.exp(normal(len(sizes)) * 1.5) * 1e-2
+        torch._foreach_mul_(grads, list(scale.unbind()))
+        flat = {t: v.to(_TYPES[t]) for t, v in flat.items()}
+        dest = {t: torch.empty_like(v) for t, v in flat.items()}
+        at, grads = {t: 0 for t in flat}, []
+        for s, t in zip(sizes, types):
+            grads.append(flat[t][at[t]:at[t] + s])
+            outs.append(dest[t][at[t]:at[t] + s])
+            at[t] += s
+        return dict(flat=flat, dest=dest, grads=grads, outs=outs)
+    t, h, kv, d = case["tokens"], case["heads"], case["kv"], case["dim"]
+    bf = torch.bfloat16
+    if case["keys"]:
+        q = normal(t, h, d).to(bf)
+        k, v = normal(case["keys"], 2 * kv, d).to(bf).split([kv, kv], dim=1)
+    else:
+        q, k, v = normal(t, h + 2 * kv, d).to(bf).split([h, kv, kv], dim=1)
+    qo, ko, prefix = (torch.tensor(x, dtype=torch.int32, device=dev) for x in _docs(case))
+    out = dict(q=q, k=k, v=v, qo=qo, ko=ko, prefix=prefix, slopes=None,
+               g=normal(t, h, d).to(bf) if case["train"] else None)
+    if case["bias"]:
+        out["slopes"] = (2.0 ** (-8.0 * torch.arange(1, h + 1, device=dev) / h)).float()
+    return out
+
+
+def prepare(case, seed):
+    s = dict(_inputs(case, seed), case=case)
+    if case["op"] == "attn":
+        s["docs"] = _docs(case)
+    if case["op"] == "rope":
+        s["dims"] = _axis_dims(case)
+    if not own:
+        return s
+    from paper_2606_19163_amd import ops
+
+    if case["op"] == "rope":
+        s["plan"] = ops.Rope(case["heads"], case["dim"], s["dims"], pairs=case["pairs"],
+                             dtype=s["x"].dtype)
+        s["y"] = torch.empty_like(s["x"], memory_format=torch.contiguous_format)
+        s["dx"] = torch.empty_like(s["y"])
+    elif case["op"] == "mask":
+        s["plan"] = ops.Mask(case["tokens"], docs=case["docs"], causal=case["kind"] != "doc")
+    elif case["op"] == "clip":
+        s["plan"] = ops.GradClip(s["grads"], outs=s["outs"])
+    else:
+        keys = case["keys"] or case["tokens"]
+        s["mask"] = ops.Mask(case["tokens"], keys=keys, docs=case["docs"],
+                             causal=case["kind"] != "doc")
+        s["mask"].build(s["qo"], key_offsets=s["ko"],
+                        prefix=s["prefix"] if case["kind"] == "prefix" else None)
+        s["plan"] = ops.Attn(case["tokens"], case["heads"], case["dim"], keys=keys,
+                             kv_heads=case["kv"], cap=case["cap"])
+        s["o"] = torch.empty((case["tokens"], case["heads"], case["dim"]), dtype=torch.bfloat16,
+                             device="cuda")
+        if case["train"]:
+            s["dq"] = torch.empty_like(s["o"])
+            s["dk"] = torch.empty((keys, case["kv"], case["dim"]), dtype=torch.bfloat16,
+                                  device="cuda")
+            s["dv"] = torch.empty_like(s["dk"])
+    return s
+
+
+# ---- the pass -----------------------------------------------------------------------
+
+
+def run(state):
+    case = state["case"]
+    return globals()[("_own_" if own else "_plain_") + case["op"]](state, case)
+
+
+def _own_rope(s, case):
+    out = {"y": s["plan"].forward(s["x"], s["pos"], s["freq"], out=s["y"])}
+    if case["train"]:
+        out["dx"] = s["plan"].backward(s["g"], s["pos"], s["freq"], out=s["dx"])
+    return out
+
+
+def _own_mask(s, case):
+    return {"rows": s["plan"].build(s["off"],
+                                    prefix=s["prefix"] if case["kind"] == "prefix" else None)}
+
+
+def _own_clip(s, case):
+    norm = s["plan"].run(case["max_norm"])
+    return {"norm": norm, "grads": s["dest"]}
+
+
+def _own_attn(s, case):
+    o, lse = s["plan"].forward(s["q"], s["k"], s["v"], s["mask"], slopes=s["slopes"], out=s["o"])
+    if not case["train"]:
+        return {"o": o}
+    dq, dk, dv = s["plan"].backward(s["g"], s["q"], s["k"], s["v"], o, lse, s["mask"],
+                                    slopes=s["slopes"], out=(s["dq"], s["dk"], s["dv"]))
+    return {"o": o, "dq": dq, "dk": dk, "dv": dv}
+
+
+def _rotate(x, c, s, pairs):
+    """Turn the pairs (a, b) of the last axis to (a c - b s, a s + b c)."""
+    if pairs == "adjacent":
+        a, b = x[..., 0::2], x[..., 1::2]
+        return torch.stack([a * c - b * s, a * s + b * c], dim=-1).reshape(x.shape)
+    n = x.shape[-1] // 2
+    a, b = x[..., :n], x[..., n:]
+    return torch.cat([a * c - b * s, a * s + b * c], dim=-1)
+
+
+def _plain_rope(s, case):
+    axis = torch.cat([torch.full((n // 2,), a, dtype=torch.long) for a, n in enumerate(s["dims"])])
+    angle = (s["pos"][:, axis.to("cuda")] * s["freq"])[:, None]
+    c, sn = torch.cos(angle), torch.sin(angle)
+    out = {"y": _rotate(s["x"].float(), c, sn, case["pairs"]).to(s["x"].dtype)}
+    if case["train"]:
+        out["dx"] = _rotate(s["g"].float(), c, -sn, case["pairs"]).to(s["x"].dtype)
+    return out
+
+
+def _plain_mask(s, case):
+    off, t = s["off"].long(), case["tokens"]
+    # document of a row: how many documents ended at or before it
+    ends = torch.zeros(t + 1, dtype=torch.long, device="cuda")
+    ends.index_add_(0, off[1:], torch.ones_like(off[1:]))
+    doc = ends.cumsum(0)[:t]
+    i = torch.arange(t, device="cuda")
+    inside = i < off[-1]
+    d = torch.where(inside, doc, torch.zeros_like(doc))
+    lo, hi = off[d], off[d + 1]
+    if case["kind"] != "doc":
+        seen = i + 1
+        if case["kind"] == "prefix":
+            seen = torch.maximum(seen, lo + s["prefix"].long()[d])
+        hi = torch.minimum(hi, seen)
+    zero = torch.zeros_like(i)
+    rows = [torch.where(inside, lo, zero), torch.where(inside, hi, zero),
+            torch.where(inside, i, zero), torch.where(inside, doc, zero - 1)]
+    return {"rows": torch.stack(rows, dim=1).int()}
+
+
+def _plain_clip(s, case):
+    total = torch.zeros((), device="cuda")
+    for g in s["grads"]:
+        total = total + (g.float() * g.float()).sum()
+    norm = torch.sqrt(total)
+    coef = torch.clamp(case["max_norm"] / (norm + 1e-6), max=1.0)
+    for g, out in zip(s["grads"], s["outs"]):
+        out.copy_(g.float() * coef)
+    return {"norm": norm.reshape(1), "grads": s["dest"]}
+
+
+def _plain_attn(s, case):
+    t, h, kv, d = case["tokens"], case["heads"], case["kv"], case["dim"]
+    rep, scale, cap = h // kv, 1.0 / math.sqrt(d), case["cap"]
+    qo, ko, prefix = s["docs"]
+    o = torch.zeros((t, h, d), dtype=torch.bfloat16, device="cuda")
+    if case["train"]:
+        dq = torch.zeros_like(o)
+        dk = torch.zeros((s["k"].shape[0], kv, d), dtype=torch.bfloat16, device="cuda")
+        dv = torch.zeros_like(dk)
+    for n in range(case["docs"]):
+        a, b, ka, kb = qo[n], qo[n + 1], ko[n], ko[n + 1]
+        nq, nk = b - a, kb - ka
+        j = torch.arange(nk, device="cuda")
+        i = torch.arange(nq, device="cuda")[:, None] + (nk - nq)
+        see = None
+        if case["kind"] != "doc":
+            see = j <= i
+            if case["kind"] == "prefix":
+                see = see | (j < prefix[n])
+        step = max(1, (1 << 28) // (nq * nk * rep))  # key heads at a time
+        for x in range(0, kv, step):
+            y = min(kv, x + step)
+            qs = s["q"][a:b, x * rep:y * rep].float().transpose(0, 1).contiguous()
+            ks = s["k"][ka:kb, x:y].float().transpose(0, 1).repeat_interleave(rep, 0)
+            vs = s["v"][ka:kb, x:y].float().transpose(0, 1).repeat_interleave(rep, 0)
+            z = torch.bmm(qs, ks.transpose(1, 2).contiguous()) * scale
+            if cap:
+                th = torch.tanh(z / cap)
+                z = cap * th
+            if s["slopes"] is not None:
+                z = z - s["slopes"][x * rep:y * rep, None, None] * (i - j).abs().float()
+            if see is not None:
+                z = torch.where(see, z, torch.full_like(z, -math.inf))
+            p = torch.exp(z - z.amax(dim=-1, keepdim=True))
+            p = p / p.sum(dim=-1, keepdim=True)
+            del z
+            o[a:b, x * rep:y * rep] = torch.bmm(p, vs).transpose(0, 1).to(o.dtype)
+            if not case["train"]:
+                continue
+            g = s["g"][a:b, x * rep:y * rep].float().transpose(0, 1).contiguous()
+            dvh = torch.bmm(p.transpose(1, 2).contiguous(), g)
+            dv[ka:kb, x:y] = dvh.reshape(y - x, rep, nk, d).sum(1).transpose(0, 1).to(dv.dtype)
+            dp = torch.bmm(g, vs.transpose(1, 2).contiguous())
+            ds = p * (dp - (p * dp).sum(dim=-1, keepdim=True))
+            del p, dp
+            if cap:
+                ds = ds * (1.0 - th * th)
+            ds = ds * scale
+            dq[a:b, x * rep:y * rep] = torch.bmm(ds, ks).transpose(0, 1).to(dq.dtype)
+            dkh = torch.bmm(ds.transpose(1, 2).contiguous(), qs)
+            dk[ka:kb, x:y] = dkh.reshape(y - x, rep, nk, d).sum(1).transpose(0, 1).to(dk.dtype)
+    if not case["train"]:
+        return {"o": o}
+    return {"o": o, "dq": dq, "dk": dk, "dv": dv}
+
+
+# ---- the definition in float64 --------------------------------------------------------
+
+
+def exact(case, seed):
+    return globals()["_exact_" + case["op"]](case, _inputs(case, seed))
+
+
+def _exact_rope(case, s):
+    dims = _axis_dims(case)
+    pos, freq = s["pos"].double(), s["freq"].double()
+    parts, at = [], 0
+    for a, n in enumerate(dims):
+        parts.append(pos[:, a:a + 1] * freq[at:at + n // 2])
+        at += n // 2
+    w = torch.exp(1j * torch.cat(parts, dim=1))[:, None]  # a pair is a complex number
+
+    def turn(x, w):
+        x = x.double()
+        n = x.shape[-1] // 2
+        if case["pairs"] == "adjacent":
+            z = torch.view_as_complex(x.reshape(x.shape[:-1] + (n, 2)).contiguous()) * w
+            return torch.view_as_real(z).reshape(x.shape)
+        z = torch.complex(x[..., :n].contiguous(), x[..., n:].contiguous()) * w
+        return torch.cat([z.real, z.imag], dim=-1)
+
+    out = {"y": turn(s["x"], w)}
+    if case["train"]:
+        out["dx"] = turn(s["g"], w.conj())
+    return out
+
+
+def _exact_mask(case, s):
+    off, prefix = s["off"].tolist(), s["prefix"].tolist()
+    rows = np.zeros((case["tokens"], 4), dtype=np.int64)
+    rows[:, 3] = -1
+    for n in range(case["docs"]):
+        a, b = off[n], off[n + 1]
+        i = np.arange(a, b)
+        hi = np.full(b - a, b)
+        if case["kind"] != "doc":
+            p = prefix[n] if case["kind"] == "prefix" else 0
+            hi = np.minimum(b, np.maximum(i + 1, a + p))
+        rows[a:b] = np.stack([np.full(b - a, a), hi, i, np.full(b - a, n)], axis=1)
+    return {"rows": torch.from_numpy(rows).int().cuda()}
+
+
+def _exact_clip(case, s):
+    norm = torch.sqrt(sum((g.double() ** 2).sum() for g in s["grads"]))
+    coef = min(1.0, case["max_norm"] / (float(norm) + 1e-6))
+    return {"norm": norm.reshape(1), "grads": {t: g.double() * coef for t, g in s["flat"].items()}}
+
+
+def _exact_attn(case, s):
+    rep, d = case["heads"] // case["kv"], case["dim"]
+    spans = torch.from_numpy(_spans(case)).cuda()
+    qo, ko, _ = _docs(case)
+    train = case["train"]
+    o = torch.zeros((case["tokens"], case["heads"], d), dtype=torch.float64, device="cuda")
+    dq = torch.zeros_like(o)
+    dk = torch.zeros(s["k"].shape, dtype=torch.float64, device="cuda")
+    dv = torch.zeros_like(dk)
+    for n in range(case["docs"]):
+        rows = torch.arange(qo[n], qo[n + 1], device="cuda")
+        rows = rows[spans[rows, 1] > spans[rows, 0]]
+        if rows.numel() == 0:
+            continue
+        j = torch.arange(ko[n], ko[n + 1], device="cuda")
+        hidden = (j < spans[rows, 0:1]) | (j >= spans[rows, 1:2])
+        far = (spans[rows, 2:3] - j).abs().double()
+        for x in range(case["heads"]):
+            q = s["q"][rows, x].double().requires_grad_(train)
+            k = s["k"][ko[n]:ko[n + 1], x // rep].double().requires_grad_(train)
+            v = s["v"][ko[n]:ko[n + 1], x // rep].double().requires_grad_(train)
+            z = (q @ k.t()) / math.sqrt(d)
+            if case["cap"]:
+                z = case["cap"] * torch.tanh(z / case["cap"])
+            if s["slopes"] is not None:
+                z = z - s["slopes"][x].double() * far
+            y = torch.softmax(z.masked_fill(hidden, -math.inf), dim=-1) @ v
+            o[rows, x] = y.detach()
+            if train:
+                gq, gk, gv = torch.autograd.grad(y, (q, k, v), s["g"][rows, x].double())
+                dq[rows, x] = gq
+                dk[ko[n]:ko[n + 1], x // rep] += gk
+                dv[ko[n]:ko[n + 1], x // rep] += gv
+            del z, y
+    return {"o": o, "dq": dq, "dk": dk, "dv": dv} if train else {"o": o}
