@@ -265,7 +265,7 @@ def _inputs(case, seed):
     if case["op"] == "clip":
         sizes, types = _sizes(case)
         grads, outs = [], []
-        flat = {t: (normal(sum(s for s, u in zip(sizes, types) if u == t))) for t in set(types)}
+        flat = {t: (normal(sum(s for s, u in zip(sizes, types) if u == t))) for t in sorted(set(types))}
         at = {t: 0 for t in flat}
         for s, t in zip(sizes, types):
             grads.append(flat[t][at[t]:at[t] + s])
