@@ -38,19 +38,21 @@ CFLAGS = [
 ]
 
 SOURCES = ["igemm2.hip", "norm.hip", "misc.hip", "probe.hip", "attn.hip",
-           "tnorm.hip", "stage.cpp", "tstage.cpp", "sched.cpp", "partition.cpp"]
+           "tnorm.hip", "mask.hip", "rope.hip", "mattn.hip", "clip.hip", "stage.cpp",
+           "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp"]
 
 # Attention's softmax takes maxima of MFMA results: with the IEEE mode bit
 # off (and no NaN semantics to keep) fmaxf needs no quieting copy of each
 # operand, which halves the VALU work of the row maxima.
-SOURCE_FLAGS = {"attn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}
+SOURCE_FLAGS = {"attn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
+                "mattn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}
 
 
 # Host-only sanitizer build of the orchestration code (CPU tests only): each
 # -fsanitize applies to the host pass alone; the kernels are not built with it.
 ASAN_BUILD = os.path.join(ROOT, "_build_asan")
 ASAN_LIB = os.path.join(ASAN_BUILD, "libpulse_stage_asan.so")
-HOST_SOURCES = ["stage.cpp", "tstage.cpp", "sched.cpp", "partition.cpp"]
+HOST_SOURCES = ["stage.cpp", "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp"]
 ASAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
               "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-fno-sanitize-recover=all",
               "-g"]

@@ -1,0 +1,363 @@
+"""ctypes binding of the packed-sequence operators (``include/pulse_ops.h``).
+
+Images and clips of several resolutions lie one after another in one sequence,
+a document each.  :class:`Mask` says which keys every query row attends,
+:class:`Rope` turns query and key heads by their positions, :class:`Attn` is
+attention under such a mask, forward and backward, and :class:`GradClip` the
+global gradient norm with clipping.
+
+Argument marshalling only: every step runs in the library's HIP kernels, and
+loading fails loudly when the library has not been built.  Tensors are
+``[tokens, heads, head_dim]`` with the last axis contiguous; the other two may
+be strided (the heads inside a projection's output, or head-major storage).
+Work is enqueued on ``stream`` (default: torch's current one), and what a call
+allocates belongs to that stream, so an object may be used from several.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+from .stage import BF16, F32, E_INVALID_ARG, PulseError, _check, lib as _lib
+
+__all__ = ["Rope", "Mask", "Attn", "GradClip", "rope_freqs", "grid_positions", "MaskRow"]
+
+_i32 = ctypes.c_int32
+_i64 = ctypes.c_int64
+_vp = ctypes.c_void_p
+_szp = ctypes.POINTER(ctypes.c_size_t)
+_PAIRS = {"adjacent": 0, "halves": 1}
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("ptr", _vp), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("heads", _i32), ("head_dim", _i32), ("axes", _i32), ("axis_dim", _i32 * 4),
+                ("pairs", _i32), ("dtype", ctypes.c_int)]
+
+
+class MaskRow(ctypes.Structure):
+    _fields_ = [("lo", _i32), ("hi", _i32), ("pos", _i32), ("doc", _i32)]
+
+
+class MaskDesc(ctypes.Structure):
+    _fields_ = [("queries", _i32), ("keys", _i32), ("docs", _i32), ("causal", _i32)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("queries", _i32), ("keys", _i32), ("heads", _i32), ("kv_heads", _i32),
+                ("head_dim", _i32), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("dtype", ctypes.c_int)]
+
+
+class ClipTensor(ctypes.Structure):
+    _fields_ = [("grad", _vp), ("out", _vp), ("n", _i64), ("dtype", ctypes.c_int)]
+
+
+_bound = None
+
+
+def lib():
+    global _bound
+    if _bound is None:
+        L = _lib()
+        st, hp, f = ctypes.c_int, ctypes.POINTER(Heads), ctypes.c_float
+        L.pulse_rope.argtypes = [ctypes.POINTER(RopeDesc), _i32, _i32, hp, _vp, _vp, hp, _vp]
+        L.pulse_rope.restype = st
+        md = ctypes.POINTER(MaskDesc)
+        L.pulse_mask_sizes.argtypes = [md, _szp]
+        L.pulse_mask_sizes.restype = st
+        L.pulse_mask_build.argtypes = [md, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        L.pulse_mask_build.restype = st
+        L.pulse_mask_from_rows.argtypes = [md, _vp, _vp, ctypes.c_size_t, _vp]
+        L.pulse_mask_from_rows.restype = st
+        ad = ctypes.POINTER(AttnDesc)
+        L.pulse_attn_sizes.argtypes = [ad, _szp, _szp]
+        L.pulse_attn_sizes.restype = st
+        L.pulse_attn_forward.argtypes = [ad, hp, hp, hp, _vp, _vp, hp, _vp, _vp, ctypes.c_size_t,
+                                         _vp]
+        L.pulse_attn_forward.restype = st
+        L.pulse_attn_backward.argtypes = [ad, hp, hp, hp, hp, hp, _vp, _vp, _vp, hp, hp, hp, _vp,
+                                          ctypes.c_size_t, _vp]
+        L.pulse_attn_backward.restype = st
+        L.pulse_clip_create.argtypes = [ctypes.POINTER(ClipTensor), _i32, ctypes.POINTER(_vp)]
+        L.pulse_clip_create.restype = st
+        L.pulse_clip_destroy.argtypes = [_vp]
+        L.pulse_clip_destroy.restype = None
+        L.pulse_clip_sizes.argtypes = [_vp, _szp]
+        L.pulse_clip_sizes.restype = st
+        L.pulse_clip_bind.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
+        L.pulse_clip_bind.restype = st
+        L.pulse_clip_run.argtypes = [_vp, f, f, _vp, _vp]
+        L.pulse_clip_run.restype = st
+        _bound = L
+    return _bound
+
+
+def _bad(msg):
+    raise PulseError(E_INVALID_ARG, msg)
+
+
+def _dtype(dt):
+    import torch
+    if dt == torch.bfloat16:
+        return BF16
+    if dt == torch.float32:
+        return F32
+    _bad(f"dtype must be torch.bfloat16 or torch.float32, not {dt}")
+
+
+def _current(t):
+    """Kernels run on the current device: a tensor of another is refused."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _bad(f"a tensor is on {t.device}, not on the current GPU")
+
+
+def _heads(t, name, shape, dtype):
+    if t.shape != shape or t.dtype != dtype:
+        _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and t.shape[2] != 1:
+        _bad(f"{name}: the channels of a head must be contiguous")
+    _current(t)
+    # the stride of an axis of one element is never used
+    return Heads(t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0)
+
+
+def _flat(t, name, n, dtype):
+    """Pointer of a contiguous tensor of n elements (None stays NULL)."""
+    if t is None:
+        return None
+    if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
+        _bad(f"{name} must be contiguous {dtype} with {n} elements, not {t.dtype} "
+             f"{tuple(t.shape)}")
+    _current(t)
+    return t.data_ptr()
+
+
+class _On:
+    """torch's current stream, or `stream` made current, so that allocations
+    belong to the stream the work runs on."""
+
+    def __init__(self, stream):
+        import torch
+        self.ctx = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def rope_freqs(axis_dim, base=10000.0, device="cuda"):
+    """freq[p] = base^(-2 i / n) for pair i of an axis of n channels, the axes
+    one after another (fp32)."""
+    import torch
+    parts = [base ** (-torch.arange(0, n, 2, dtype=torch.float64) / max(n, 1)) for n in axis_dim]
+    return torch.cat(parts).float().to(device)
+
+
+def grid_positions(shapes, device="cuda"):
+    """Positions [tokens, axes] of documents whose tokens are grids (time,
+    height, width or any other number of axes) in row-major order."""
+    import torch
+    out = [torch.cartesian_prod(*[torch.arange(n) for n in s]).reshape(-1, len(s)) for s in shapes]
+    return torch.cat(out).float().to(device)
+
+
+class Rope:
+    """Rotary positions of ``heads`` heads; ``axis_dim``: channels per axis."""
+
+    def __init__(self, heads, head_dim, axis_dim, pairs="adjacent", dtype=None):
+        import torch
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        if pairs not in _PAIRS:
+            _bad(f"pairs must be one of {sorted(_PAIRS)}")
+        if not 1 <= len(axis_dim) <= 4:
+            _bad("one to four axes")
+        self.heads, self.dim, self.axes = heads, head_dim, len(axis_dim)
+        self.half = sum(axis_dim) // 2
+        self.desc = RopeDesc(heads, head_dim, len(axis_dim), (_i32 * 4)(*axis_dim), _PAIRS[pairs],
+                             _dtype(self.dtype))
+        # no tokens: only the descriptor is checked
+        none = Heads(None, 0, 0)
+        _check(lib().pulse_rope(ctypes.byref(self.desc), 0, 0, ctypes.byref(none), None, None,
+                                ctypes.byref(none), None))
+
+    def _run(self, x, pos, freq, out, backward, stream):
+        import torch
+        n = x.shape[0]
+        shape = (n, self.heads, self.dim)
+        with _On(stream) as s:
+            if out is None:
+                out = torch.empty(shape, dtype=self.dtype, device=x.device)
+            hx, hy = _heads(x, "x", shape, self.dtype), _heads(out, "out", shape, self.dtype)
+            _check(lib().pulse_rope(
+                self.desc, n, backward, hx, _flat(pos, "pos", n * self.axes, torch.float32),
+                _flat(freq, "freq", self.half, torch.float32), hy, s))
+        return out
+
+    def forward(self, x, pos, freq, out=None, stream=None):
+        """x turned by its positions; ``out`` may be x."""
+        return self._run(x, pos, freq, out, 0, stream)
+
+    def backward(self, dout, pos, freq, out=None, stream=None):
+        """The gradient of ``forward``'s input from that of its output."""
+        return self._run(dout, pos, freq, out, 1, stream)
+
+
+class Mask:
+    """Which of ``keys`` keys each of ``queries`` rows attends."""
+
+    def __init__(self, queries, keys=None, docs=0, causal=False, device="cuda"):
+        import torch
+        self.queries, self.keys = queries, queries if keys is None else keys
+        self.docs = docs
+        self.desc = MaskDesc(queries, self.keys, docs, 1 if causal else 0)
+        n = ctypes.c_size_t()
+        _check(lib().pulse_mask_sizes(ctypes.byref(self.desc), ctypes.byref(n)))
+        self.bytes = n.value
+        self.buffer = torch.empty(max(n.value // 4, 4), dtype=torch.int32, device=device)
+        self.ptr = self.buffer.data_ptr()
+        #: [queries, 4]: lo, hi, pos, doc of every row
+        self.rows = self.buffer[:4 * queries].view(queries, 4)
+
+    def build(self, offsets, key_offsets=None, prefix=None, stream=None):
+        """From int32 ``offsets`` [docs + 1] on the GPU; returns ``rows``."""
+        import torch
+        with _On(stream) as s:
+            _check(lib().pulse_mask_build(
+                self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32),
+                _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32),
+                _flat(prefix, "prefix", self.docs, torch.int32), self.ptr, self.bytes, s))
+        return self.rows
+
+    def from_rows(self, rows, stream=None):
+        """From the caller's int32 [queries, 4] (it may be ``self.rows``)."""
+        import torch
+        with _On(stream) as s:
+            _check(lib().pulse_mask_from_rows(
+                self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32), self.ptr,
+                self.bytes, s))
+        return self.rows
+
+
+class Attn:
+    """Attention of ``queries`` rows and ``heads`` heads under a mask (bf16)."""
+
+    def __init__(self, queries, heads, head_dim, keys=None, kv_heads=None, scale=None, cap=0.0):
+        self.queries, self.keys = queries, queries if keys is None else keys
+        self.heads, self.kv, self.dim = heads, heads if kv_heads is None else kv_heads, head_dim
+        scale = 1.0 / math.sqrt(head_dim) if scale is None else scale
+        self.desc = AttnDesc(queries, self.keys, heads, self.kv, head_dim, scale, cap, BF16)
+        f, b = ctypes.c_size_t(), ctypes.c_size_t()
+        _check(lib().pulse_attn_sizes(ctypes.byref(self.desc), ctypes.byref(f), ctypes.byref(b)))
+        self.fwd_bytes, self.bwd_bytes = f.value, b.value
+        self.qs = (queries, heads, head_dim)
+        self.ks = (self.keys, self.kv, head_dim)
+
+    def _mask(self, mask):
+        if mask.queries != self.queries or mask.keys != self.keys:
+            _bad(f"the mask is of {mask.queries} rows and {mask.keys} keys")
+        return mask.ptr
+
+    def forward(self, q, k, v, mask, slopes=None, out=None, lse=None, stream=None):
+        """(o, lse): o [queries, heads, head_dim], lse [heads, queries] fp32."""
+        import torch
+        bf = torch.bfloat16
+        with _On(stream) as s:
+            if out is None:
+                out = torch.empty(self.qs, dtype=bf, device=q.device)
+            if lse is None:
+                lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
+            ws = None
+            if self.fwd_bytes:
+                ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
+            _check(lib().pulse_attn_forward(
+                self.desc, _heads(q, "q", self.qs, bf), _heads(k, "k", self.ks, bf),
+                _heads(v, "v", self.ks, bf), self._mask(mask),
+                _flat(slopes, "slopes", self.heads, torch.float32), _heads(out, "out", self.qs, bf),
+                _flat(lse, "lse", self.heads * self.queries, torch.float32),
+                ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
+        return out, lse
+
+    def backward(self, dout, q, k, v, o, lse, mask, slopes=None, out=None, stream=None):
+        """(dq, dk, dv), written into the tensors of ``out`` if given."""
+        import torch
+        bf = torch.bfloat16
+        with _On(stream) as s:
+            if out is None:
+                out = [torch.empty(n, dtype=bf, device=q.device)
+                       for n in (self.qs, self.ks, self.ks)]
+            dq, dk, dv = out
+            ws = None
+            if self.bwd_bytes:
+                ws = torch.empty(self.bwd_bytes, dtype=torch.uint8, device=q.device)
+            _check(lib().pulse_attn_backward(
+                self.desc, _heads(dout, "dout", self.qs, bf), _heads(q, "q", self.qs, bf),
+                _heads(k, "k", self.ks, bf), _heads(v, "v", self.ks, bf),
+                _heads(o, "o", self.qs, bf),
+                _flat(lse, "lse", self.heads * self.queries, torch.float32), self._mask(mask),
+                _flat(slopes, "slopes", self.heads, torch.float32), _heads(dq, "dq", self.qs, bf),
+                _heads(dk, "dk", self.ks, bf), _heads(dv, "dv", self.ks, bf),
+                ws.data_ptr() if ws is not None else None, self.bwd_bytes, s))
+        return dq, dk, dv
+
+
+class GradClip:
+    """The global norm of ``grads`` (contiguous, fp32 or bf16) and their
+    clipping, in place or into ``outs``.  The tensors' addresses are taken
+    once, so they must stay where they are from step to step."""
+
+    def __init__(self, grads, outs=None):
+        import torch
+        self.h = _vp()
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if len(grads) != len(outs):
+            _bad(f"{len(grads)} gradients and {len(outs)} outputs")
+        arr = (ClipTensor * max(len(grads), 1))()
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            if g.dtype != o.dtype or g.numel() != o.numel():
+                _bad(f"gradient {i} and its output differ in type or size")
+            if not g.is_contiguous() or not o.is_contiguous():
+                _bad(f"gradient {i} or its output is not contiguous")
+            _current(g)
+            _current(o)
+            arr[i] = ClipTensor(g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g.dtype))
+        self.grads, self.outs = grads, outs
+        self.device = grads[0].device if grads else "cuda"
+        _check(lib().pulse_clip_create(arr, len(grads), ctypes.byref(self.h)))
+        n = ctypes.c_size_t()
+        _check(lib().pulse_clip_sizes(self.h, ctypes.byref(n)))
+        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        _check(lib().pulse_clip_bind(self.h, self.workspace.data_ptr(), n.value,
+                                     torch.cuda.current_stream().cuda_stream))
+
+    def __del__(self):
+        try:
+            if self.h:
+                lib().pulse_clip_destroy(self.h)
+                self.h = _vp()
+        except Exception:
+            pass
+
+    def run(self, max_norm, eps=1e-6, norm=None, stream=None):
+        """Clip to ``max_norm``; returns the norm before it, fp32 [1].  Calls
+        share one workspace: order the streams that they run on."""
+        import torch
+        with _On(stream) as s:
+            if norm is None:
+                norm = torch.empty(1, dtype=torch.float32, device=self.device)
+            _check(lib().pulse_clip_run(self.h, max_norm, eps,
+                                        _flat(norm, "norm", 1, torch.float32), s))
+        return norm

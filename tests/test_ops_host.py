@@ -1,0 +1,261 @@
+"""Host-side checks of the packed-sequence operators' C ABI (no GPU): every
+refusal returns its status before anything is enqueued, and sizes follow the
+documented layouts.  Pointers here are addresses that nothing reads."""
+
+import ctypes
+import os
+
+import pytest
+
+from paper_2606_19163_amd import ops
+from paper_2606_19163_amd import stage as S
+
+P = 1 << 20  # an aligned address
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not os.path.exists(S.LIB_PATH):
+        from paper_2606_19163_amd import build
+        build.build()
+    yield
+
+
+def _refused(status, expect):
+    assert status == expect, (status, S.lib().pulse_last_error())
+    assert S.lib().pulse_last_error()
+
+
+def _rope(tokens=4, x=None, y=None, pos=P, freq=P, **kw):
+    d = dict(heads=2, head_dim=64, axes=2, axis_dim=(ctypes.c_int32 * 4)(32, 32), pairs=0,
+             dtype=S.BF16)
+    if "axis_dim" in kw:
+        kw["axis_dim"] = (ctypes.c_int32 * 4)(*kw["axis_dim"])
+    d.update(kw)
+    x = ops.Heads(P, 128, 64) if x is None else x
+    y = ops.Heads(P, 128, 64) if y is None else y
+    return ops.lib().pulse_rope(ops.RopeDesc(**d), tokens, 0, x, pos, freq, y, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(heads=0), dict(heads=1025), dict(head_dim=60), dict(head_dim=264), dict(head_dim=0),
+    dict(axes=0), dict(axes=5), dict(axis_dim=(33, 31)), dict(axis_dim=(-2, 34)),
+    dict(axis_dim=(64, 8)), dict(axis_dim=(2, 2)), dict(axis_dim=(0, 0)), dict(tokens=-1),
+    dict(tokens=(1 << 24) + 1),
+])
+def test_rope_shapes(kw):
+    _refused(_rope(**kw), S.E_SHAPE)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=2), dict(pairs=2), dict(pos=None), dict(freq=None), dict(pos=P + 2),
+    dict(x=ops.Heads(None, 128, 64)), dict(x=ops.Heads(P + 2, 128, 64)),
+    dict(x=ops.Heads(P, 124, 64)), dict(x=ops.Heads(P, -128, 64)), dict(x=ops.Heads(P, 128, 4)),
+    dict(y=ops.Heads(P, 64, 64)), dict(y=ops.Heads(P, 128, 0)), dict(y=ops.Heads(P, 64, 128)),
+    dict(y=ops.Heads(P, 1 << 41, 64)), dict(y=ops.Heads(P, 56, 1024)),
+    dict(dtype=S.F32, x=ops.Heads(P, 128, 66)),
+])
+def test_rope_arguments(kw):
+    _refused(_rope(**kw), S.E_INVALID_ARG)
+
+
+def test_rope_null_descriptors_and_no_tokens():
+    L = ops.lib()
+    h = ops.Heads(P, 128, 64)
+    _refused(L.pulse_rope(None, 1, 0, h, P, P, h, None), S.E_INVALID_ARG)
+    _refused(_rope_with(None, h), S.E_INVALID_ARG)
+    assert _rope(tokens=0, x=ops.Heads(None, 0, 0), y=ops.Heads(None, 0, 0)) == S.OK
+
+
+def _rope_with(x, y):
+    d = ops.RopeDesc(2, 64, 2, (ctypes.c_int32 * 4)(32, 32), 0, S.BF16)
+    return ops.lib().pulse_rope(d, 4, 0, x, P, P, y, None)
+
+
+def _mask_size(**kw):
+    d = dict(queries=100, keys=100, docs=3, causal=0)
+    d.update(kw)
+    n = ctypes.c_size_t()
+    return ops.lib().pulse_mask_sizes(ops.MaskDesc(**d), ctypes.byref(n)), n.value
+
+
+def test_mask_sizes():
+    assert _mask_size() == (S.OK, 100 * 16 + 2 * 16)
+    assert _mask_size(queries=0) == (S.OK, 0)
+    assert _mask_size(queries=128) == (S.OK, 130 * 16)
+    for kw in (dict(queries=-1), dict(keys=-1), dict(queries=(1 << 24) + 1),
+               dict(keys=(1 << 24) + 1), dict(docs=-1), dict(docs=(1 << 20) + 1)):
+        _refused(_mask_size(**kw)[0], S.E_SHAPE)
+    _refused(_mask_size(causal=2)[0], S.E_INVALID_ARG)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=None), dict(q=P + 1), dict(k=P + 2), dict(prefix=P), dict(mask=None), dict(mask=P + 8),
+    dict(nbytes=1631), dict(keys=99, k=None),
+])
+def test_mask_build_arguments(kw):
+    a = dict(q=P, k=P, prefix=None, mask=P, nbytes=1632, keys=100)
+    a.update(kw)
+    d = ops.MaskDesc(100, a["keys"], 3, 0)
+    _refused(ops.lib().pulse_mask_build(d, a["q"], a["k"], a["prefix"], a["mask"], a["nbytes"],
+                                        None), S.E_INVALID_ARG)
+
+
+def test_mask_from_rows_arguments():
+    d = ops.MaskDesc(100, 100, 0, 0)
+    f = ops.lib().pulse_mask_from_rows
+    for rows, mask, n in ((None, P, 1632), (P + 4, P, 1632), (P, None, 1632), (P, P, 1600)):
+        _refused(f(d, rows, mask, n, None), S.E_INVALID_ARG)
+    assert f(ops.MaskDesc(0, 5, 0, 0), None, None, 0, None) == S.OK
+
+
+def _attn_desc(**kw):
+    d = dict(queries=100, keys=80, heads=4, kv_heads=2, head_dim=64, scale=0.125, cap=0.0,
+             dtype=S.BF16)
+    d.update(kw)
+    return ops.AttnDesc(**d)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=S.F32), S.E_SHAPE), (dict(queries=-1), S.E_SHAPE),
+    (dict(keys=(1 << 24) + 1), S.E_SHAPE), (dict(heads=0), S.E_SHAPE),
+    (dict(heads=2048, kv_heads=1), S.E_SHAPE), (dict(kv_heads=3), S.E_SHAPE),
+    (dict(kv_heads=0), S.E_SHAPE), (dict(head_dim=0), S.E_SHAPE), (dict(head_dim=60), S.E_SHAPE),
+    (dict(head_dim=136), S.E_SHAPE), (dict(scale=float("nan")), S.E_INVALID_ARG),
+    (dict(scale=float("inf")), S.E_INVALID_ARG), (dict(cap=-1.0), S.E_INVALID_ARG),
+    (dict(cap=float("nan")), S.E_INVALID_ARG), (dict(cap=float("inf")), S.E_INVALID_ARG),
+])
+def test_attn_descriptors(kw, status):
+    _refused(ops.lib().pulse_attn_sizes(_attn_desc(**kw), None, None), status)
+    _refused(ops.lib().pulse_attn_sizes(None, None, None), S.E_INVALID_ARG)
+
+
+def _attn_calls(d, **kw):
+    """Both calls with plausible arguments but for those given."""
+    q, k = ops.Heads(P, 256, 64), ops.Heads(P, 128, 64)
+    a = dict(q=q, k=k, v=k, o=q, dout=q, dq=q, dk=k, dv=k, mask=P, slopes=P, lse=P, ws=P,
+             nbytes=1 << 40)
+    a.update(kw)
+    L = ops.lib()
+    return (L.pulse_attn_forward(d, a["q"], a["k"], a["v"], a["mask"], a["slopes"], a["o"],
+                                 a["lse"], a["ws"], a["nbytes"], None),
+            L.pulse_attn_backward(d, a["dout"], a["q"], a["k"], a["v"], a["o"], a["lse"],
+                                  a["mask"], a["slopes"], a["dq"], a["dk"], a["dv"], a["ws"],
+                                  a["nbytes"], None))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(mask=None), dict(lse=None),
+    dict(mask=P + 4), dict(slopes=P + 1), dict(lse=P + 2), dict(q=ops.Heads(None, 256, 64)),
+    dict(k=ops.Heads(P + 8, 128, 64)), dict(v=ops.Heads(P, 130, 64)),
+    dict(q=ops.Heads(P, 256, -64)),
+])
+def test_attn_arguments_of_both_calls(kw):
+    for status in _attn_calls(_attn_desc(), **kw):
+        _refused(status, S.E_INVALID_ARG)
+
+
+@pytest.mark.parametrize("name", ["dout", "dq", "dk", "dv"])
+def test_attn_arguments_of_the_backward(name):
+    bad = [None, ops.Heads(None, 256, 64), ops.Heads(P + 2, 256, 64)]
+    if name != "dout":
+        bad += [ops.Heads(P, 0, 64), ops.Heads(P, 256, 0), ops.Heads(P, 64, 64)]
+    for h in bad:
+        _refused(_attn_calls(_attn_desc(), **{name: h})[1], S.E_INVALID_ARG)
+
+
+def test_attn_outputs_must_not_overlap_and_workspace():
+    _refused(_attn_calls(_attn_desc(), o=ops.Heads(P, 192, 64))[0], S.E_INVALID_ARG)
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    assert ops.lib().pulse_attn_sizes(_attn_desc(), ctypes.byref(f), ctypes.byref(b)) == S.OK
+    for i, need in enumerate((f.value, b.value)):
+        if need:
+            for kw in (dict(nbytes=need - 1), dict(ws=None), dict(ws=P + 16)):
+                _refused(_attn_calls(_attn_desc(), **kw)[i], S.E_INVALID_ARG)
+    assert b.value >= 4 * 100 * 4
+
+
+def _clip(*tensors, count=None):
+    arr = (ops.ClipTensor * max(len(tensors), 1))(*tensors)
+    h = ctypes.c_void_p()
+    s = ops.lib().pulse_clip_create(arr, len(tensors) if count is None else count,
+                                    ctypes.byref(h))
+    return s, h
+
+
+def test_clip_refusals():
+    L = ops.lib()
+    T = ops.ClipTensor
+    for t in (T(P, P, 5, 2), T(None, P, 5, 0), T(P, None, 5, 0), T(P + 2, P, 5, 0),
+              T(P, P + 1, 5, 1)):
+        s, h = _clip(t)
+        _refused(s, S.E_INVALID_ARG)
+        assert not h
+    for t in (T(P, P, -1, 0), T(P, P, (1 << 38) + 1, 0)):
+        _refused(_clip(t)[0], S.E_SHAPE)
+    _refused(_clip(count=-1)[0], S.E_SHAPE)
+    _refused(_clip(count=(1 << 20) + 1)[0], S.E_SHAPE)
+    _refused(L.pulse_clip_create(None, 1, ctypes.byref(ctypes.c_void_p())), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_create(None, 0, None), S.E_INVALID_ARG)
+    s, h = _clip(T(P, P, 100000, 0), T(None, None, 0, 1), T(P + 2, P + 6, 7, 1))
+    assert s == S.OK
+    n = ctypes.c_size_t()
+    assert L.pulse_clip_sizes(h, ctypes.byref(n)) == S.OK and n.value > 0
+    _refused(L.pulse_clip_sizes(h, None), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_sizes(None, ctypes.byref(n)), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_run(h, 1.0, 0.0, P, None), S.E_NOT_BOUND)
+    _refused(L.pulse_clip_bind(h, None, n.value, None), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_bind(h, P, n.value - 1, None), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_bind(h, P + 128, n.value, None), S.E_INVALID_ARG)
+    _refused(L.pulse_clip_run(None, 1.0, 0.0, P, None), S.E_INVALID_ARG)
+    L.pulse_clip_destroy(h)
+    L.pulse_clip_destroy(None)
+
+
+def test_clip_run_arguments():
+    """On an empty set, whose bind copies nothing."""
+    L = ops.lib()
+    s, h = _clip()
+    assert s == S.OK
+    n = ctypes.c_size_t()
+    L.pulse_clip_sizes(h, ctypes.byref(n))
+    assert L.pulse_clip_bind(h, P, n.value, None) == S.OK
+    nan = float("nan")
+    for mx, eps, norm in ((-1.0, 0.0, P), (nan, 0.0, P), (1.0, -1.0, P), (1.0, nan, P),
+                          (1.0, 0.0, None), (1.0, 0.0, P + 2)):
+        _refused(L.pulse_clip_run(h, mx, eps, norm, None), S.E_INVALID_ARG)
+    L.pulse_clip_destroy(h)
+
+
+def test_binding_refuses_before_the_library():
+    import torch
+    with pytest.raises(S.PulseError):
+        ops.Rope(2, 64, [32, 31])
+    with pytest.raises(S.PulseError):
+        ops.Rope(2, 64, [8] * 5)
+    with pytest.raises(S.PulseError):
+        ops.Rope(2, 64, [64], pairs="other")
+    with pytest.raises(S.PulseError):
+        ops.Rope(2, 64, [64], dtype=torch.float16)
+    with pytest.raises(S.PulseError):
+        ops.Attn(10, 3, 64, kv_heads=2)
+    m = ops.Mask(10, docs=1, device="cpu")
+    assert m.rows.shape == (10, 4)
+    with pytest.raises(S.PulseError):  # not on a GPU
+        ops._heads(torch.zeros(4, 2, 64, dtype=torch.bfloat16), "x", (4, 2, 64), torch.bfloat16)
+    with pytest.raises(S.PulseError):
+        ops._heads(torch.zeros(4, 2, 64), "x", (4, 2, 64), torch.bfloat16)
+    with pytest.raises(S.PulseError):
+        ops._flat(torch.zeros(4, 2).t(), "x", 8, torch.float32)
+    with pytest.raises(S.PulseError):
+        ops.GradClip([torch.zeros(4)])
+    with pytest.raises(S.PulseError):
+        ops.GradClip([torch.zeros(4)], outs=[torch.zeros(5)])
+
+
+def test_rope_frequencies_and_positions():
+    f = ops.rope_freqs([4, 8], base=100.0, device="cpu")
+    assert f.tolist() == pytest.approx([1, 0.1, 1, 100 ** -0.25, 0.1, 100 ** -0.75], rel=1e-6)
+    p = ops.grid_positions([(2, 2), (1, 3)], device="cpu")
+    assert p.tolist() == [[0, 0], [0, 1], [1, 0], [1, 1], [0, 0], [0, 1], [0, 2]]
+    assert ops.grid_positions([(3,)], device="cpu").tolist() == [[0], [1], [2]]
