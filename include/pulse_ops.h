@@ -63,7 +63,7 @@ typedef struct {
   int32_t axis_dim[4]; /* channels per axis: even, >= 0; R a multiple of 8,
                           8 <= R <= head_dim                                */
   int32_t pairs;       /* pulse_rope_pairs                                  */
-  pulse_dtype dtype;   /* PULSE_BF16 or PULSE_F32                           */
+  int32_t dtype;       /* PULSE_BF16 or PULSE_F32                           */
 } pulse_rope_desc;
 
 /* Pair p of axis a of token t turns by the angle pos[t][a] * freq[p]:
@@ -166,7 +166,7 @@ typedef struct {
   const void* grad; /* n elements, aligned to their type                    */
   void* out;        /* receives the clipped gradient; may be grad itself    */
   int64_t n;        /* >= 0                                                 */
-  pulse_dtype dtype;/* of grad and out                                      */
+  int32_t dtype;    /* of grad and out                                      */
 } pulse_clip_tensor;
 
 /* A set of up to 2^20 gradient tensors whose addresses stay the same from
