@@ -127,7 +127,7 @@ typedef struct {
   int32_t head_dim;        /* a multiple of 8, 8..128                        */
   float scale;             /* of the scores (finite)                         */
   float cap;               /* 0: none; else scores become cap tanh(s / cap)  */
-  pulse_dtype dtype;       /* PULSE_BF16 only                                */
+  int32_t dtype;           /* PULSE_BF16 only                                */
 } pulse_attn_desc;
 
 /* Workspace bytes of a forward and of a backward call (either may be NULL). */
