@@ -1,18 +1,30 @@
-// Attention under a row mask (gfx950, bf16 MFMA 16x16x32, fp32
+// Attention under a row mask (gfx950, bf16 MFMA 32x32x16, fp32
 // accumulation).  Query row i attends keys lo_i <= j < hi_i:
 //   z = scale q k^T, capped: z = cap tanh(z / cap), then - slope |pos_i - j|
 //   p = softmax over the attended keys, o = p v, lse = log sum exp z
 // backward: p from z and lse; D = rowsum(do o), dp = do v^T,
 //   ds = p (dp - D) (1 - tanh^2) scale, dq = ds k, dk = ds^T q, dv = p^T do.
-// dq has a kernel per query tile, dk and dv one per key tile, each of which
-// computes z again, so that nothing is accumulated across blocks.
+// dq has a kernel over query rows, dk and dv one over keys, each of which
+// computes z and dp again, so that nothing is accumulated across blocks.
 // Scores are kept in the log2 domain (z log2 e).
 //
-// A key that a row does not attend must not reach it even when it holds a NaN
-// or an infinity, which the products' zero weights do not ensure (0 NaN =
-// NaN).  In a tile that some row attends only in part, an operand fragment
-// that holds such a value is multiplied row by row, with the positions that
-// the row does not attend cleared.
+// The four waves of a block are G groups of 32 rows (or keys) by 4 / G shares
+// of the other side, which streams through LDS in tiles of 64, and a wave
+// works on 32 x 32 scores at a time.  For o and dq it computes
+//   s^T = k q^T    A = k rows (LDS), B = q (registers)
+//   o^T += v^T p^T A = v read down the tile, B = p^T
+// and for dk and dv the same with the sides exchanged, so that p and ds stay
+// in registers: lane (n, hl) of the MFMA's output holds rows
+// 8 (i / 4) + 4 hl + i % 4 of column n (i < 16) and its B operand wants rows
+// 8 hl + t of 16 (t < 8), which is the same set if row r of the first product
+// is row swap23(r) of the tile (bits 2 and 3 exchanged): element i then is
+// row 16 (i / 8) + 8 hl + i % 8.
+//
+// A row that does not attend a key must not be reached by it even when it
+// holds a NaN or an infinity, which the product's zero weight does not ensure
+// (0 NaN = NaN).  In a tile that some row attends only in part, such values
+// are cleared in the operand that is summed over, and the rows that do attend
+// them get them at the end.
 #include "common.hpp"
 #include "okernels.hpp"
 
@@ -21,13 +33,18 @@ namespace {
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 
-constexpr int BT = 64;  // rows and keys per tile
+constexpr int KT = 64;  // keys (or rows) per streamed tile
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr float LOWEST = -3.0e38f;  // finite: below every finite score
+// Forward: a row's reference moves up to its maximum only when a score passes
+// it by more than GROW (log2 units), decided for the whole wave, so that most
+// steps skip the rescaling; weights stay below 2^GROW.
+constexpr float GROW = 8.f;
 
 struct Dev {  // device view of MattnArgs
   int Tq, Tk, H, rep, hd8;
@@ -43,33 +60,41 @@ struct Dev {  // device view of MattnArgs
   float* dsum;
 };
 
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+// The builtins, since the library functions behind threadIdx are built for
+// the IEEE mode that this file turns off and would stay calls.
+// The value is opaque: knowing its range, the compiler splits every LDS
+// address into parts that it keeps in registers across the loops, and spills.
+__device__ __forceinline__ int tid() {
+  int t = __builtin_amdgcn_workitem_id_x();
+  asm("" : "+v"(t));
+  return t;
 }
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// 2^x as one v_exp_f32: results below 2^-126 flush to zero
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ f32x16 splat(float x) {
+  f32x16 v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = x;
+  return v;
+}
+__device__ __forceinline__ int swap23(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+// offset of element i of an output column from its first row (8 hl)
+__device__ __forceinline__ constexpr int elem(int i) { return 16 * (i / 8) + i % 8; }
 
 // element offset of 16-byte chunk c of row r of a [rows][D] tile; the chunks
-// of a row are permuted so that 16 rows of one chunk fall on distinct banks
+// of a row are permuted so that the rows that one LDS access reads fall on
+// distinct banks: {0-3, 8-11} (+4, +16) of one chunk (rows32), {0-3} of two
+// (cols32)
 template <int D>
 __device__ __forceinline__ int toff(int r, int c) {
   const int x = D == 64 ? ((((r >> 1) & 1) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 2))
               : D == 96 ? ((r >> 2) & 3)
-                        : (r & 15);
+                        : ((r & 3) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 3);
   return r * D + ((c ^ x) << 3);
-}
-
-// rows [0, BT) of a strided tensor into a tile; rows past `valid` and channels
-// past the head dimension become 0
-template <int D>
-__device__ __forceinline__ void load_tile(uint16_t* t, const uint16_t* src, long stride, int valid,
-                                          int hd8) {
-  for (int e = threadIdx.x; e < BT * D / 8; e += 256) {
-    const int r = e / (D / 8), c = e % (D / 8);
-    uint4 v{0, 0, 0, 0};
-    if (r < valid && c < hd8) v = *reinterpret_cast<const uint4*>(src + r * stride + c * 8);
-    *reinterpret_cast<uint4*>(t + toff<D>(r, c)) = v;
-  }
 }
 
 // operand of 8 consecutive channels straight from memory (0 where absent)
@@ -79,82 +104,145 @@ __device__ __forceinline__ bf16x8 row_frag(const uint16_t* p, int c, bool ok, in
   return __builtin_bit_cast(bf16x8, v);
 }
 
-template <int D>
-__device__ __forceinline__ bf16x8 frag_row(const uint16_t* t, int r, int kk, int g) {
-  return *reinterpret_cast<const bf16x8*>(t + toff<D>(r, 4 * kk + g));
-}
-
 __device__ __forceinline__ v4s rd_tr(const uint16_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p));
 }
 
-// operand whose k index runs down the tile: lane (g, j) receives rows
-// r0 + 8 g .. + 7 of channel d0 + j
+// A operand of rows: lane (n, hl) gets channels 16 kk + 8 hl .. + 7 of row
+// r0 + swap23(n)
 template <int D>
-__device__ __forceinline__ bf16x8 frag_tr(const uint16_t* t, int r0, int d0, int lane) {
-  const int g = lane >> 4, j = lane & 15;
-  const int col = d0 + 4 * (j & 3);
-  const int r = r0 + 8 * g + (j >> 2);
+__device__ __forceinline__ bf16x8 rows32(const uint16_t* t, int r0, int kk, int lane) {
+  return *reinterpret_cast<const bf16x8*>(
+      t + toff<D>(r0 + swap23(lane & 31), 2 * kk + (lane >> 5)));
+}
+
+// A operand read down the tile: lane (n, hl) gets rows r0 + 8 hl .. + 7 of
+// channel d0 + n.  ds_read_b64_tr_b16: within 16 lanes, lane j receives
+// element j % 4 of the rows addressed by lanes 4 t + j / 4 (t = 0..3).
+template <int D>
+__device__ __forceinline__ bf16x8 cols32(const uint16_t* t, int r0, int d0, int lane) {
+  const int j = lane & 15;
+  const int col = d0 + (lane & 16) + 4 * (j & 3);
+  const int r = r0 + 8 * (lane >> 5) + (j >> 2);
   const v4s lo = rd_tr(t + toff<D>(r, col >> 3) + (col & 7));
   const v4s hi = rd_tr(t + toff<D>(r + 4, col >> 3) + (col & 7));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// a wave's strip of 16 rows x 64 columns
-__device__ __forceinline__ int soff(int r, int c) { return r * BT + ((c ^ (r & 7)) << 3); }
-__device__ __forceinline__ void sput(uint16_t* s, int r, int col, float v) {
-  s[soff(r, col >> 3) + (col & 7)] = f2bf(v);
-}
-__device__ __forceinline__ bf16x8 sfrag(const uint16_t* s, int m, int ks, int g) {
-  return *reinterpret_cast<const bf16x8*>(s + soff(m, 4 * ks + g));
+__device__ __forceinline__ bool odd_lo(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool odd_hi(uint32_t x) { return (x & 0x7f800000u) == 0x7f800000u; }
+
+// NaN and infinities among 8 values become 0; whether there were any
+__device__ __forceinline__ bool clean8(uint4& w) {
+  uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = odd_lo(x[i]), hi = odd_hi(x[i]);
+    x[i] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+    odd |= lo | hi;
+  }
+  w = uint4{x[0], x[1], x[2], x[3]};
+  return odd;
 }
 
-// any NaN or infinity among the wave's fragment
-__device__ __forceinline__ bool nonfinite(bf16x8 v) {
-  const uint4 w = __builtin_bit_cast(uint4, v);
+// o += those of 8 values that are NaN or infinite (a weight p > 0 leaves them
+// what they are); with `nan` they make it NaN
+__device__ __forceinline__ void add_odd(float (&o)[8], uint4 w, bool nan) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-  bool bad = false;
+  const float q = __uint_as_float(0x7fc00000u);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad |= ((x[i] & 0x7f80u) == 0x7f80u) | ((x[i] & 0x7f800000u) == 0x7f800000u);
-  return __any(bad);
-}
-
-// c += a b where row r of a has zero weights at the positions k it does not
-// attend and b holds a NaN or infinity: row r's product is formed with those
-// positions of b cleared.  keep(r, k) says whether row r attends position k
-// (0..31); rows and k as in the operands.
-template <typename F>
-__device__ __forceinline__ f32x4 mma_rows(bf16x8 a, bf16x8 b, f32x4 c, int lane, F keep) {
-  const int g = lane >> 4;
-  for (int r = 0; r < 16; ++r) {
-    bf16x8 z = b;
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-      if (!keep(r, 8 * g + t)) z[t] = (__bf16)0.f;
-    const f32x4 y = mma(a, z, zero4());
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * g + i == r) c[i] += y[i];
+  for (int i = 0; i < 4; ++i) {
+    if (odd_lo(x[i])) o[2 * i] += nan ? q : __uint_as_float(x[i] << 16);
+    if (odd_hi(x[i])) o[2 * i + 1] += nan ? q : __uint_as_float(x[i] & 0xffff0000u);
   }
-  return c;
 }
 
-// log2-domain score and d z / d (scale q.k) of a raw product
-template <bool CAP>
-__device__ __forceinline__ float score(const Dev& a, float raw, float& slope) {
-  if (!CAP) {
-    slope = 1.f;
-    return raw * a.c1;
+// x, or NaN where x is not finite
+__device__ __forceinline__ float finite_or_nan(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return __uint_as_float((b & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : b);
+}
+
+// A thread's 16-byte chunks of a [KT][D] tile of a strided tensor, in
+// registers on their way from memory to LDS.  The chunks are whole rows apart
+// (D = 64, 128) or columns apart (96), so that one address serves them all.
+template <int D>
+struct Stage {
+  static constexpr int N = KT * D / 8 / 256;
+  static constexpr int ROUND = D == 96 ? 4 : D / 8;  // chunks of a row in one round
+  static constexpr int RR = 256 / ROUND;             // rows in one round
+  static_assert(N * 256 == KT * D / 8 && (D == 96 ? KT == RR : KT % RR == 0), "whole rounds");
+  uint4 v[N];
+  const uint16_t* p;
+  long stride;
+  int r, c;
+  __device__ __forceinline__ void init(const uint16_t* src, long row, long st) {
+    r = tid() / ROUND;
+    c = tid() % ROUND;
+    stride = st;
+    p = src + (row + r) * st + 8 * c;
+#pragma unroll
+    for (int u = 0; u < N; ++u) v[u] = uint4{0, 0, 0, 0};
   }
-  // tanh(x) = 1 - 2 / (1 + e^(2x)); e^(2x) may overflow to inf: tanh = 1
-  const float e = ex2(raw * a.c1 * (2.f * LOG2E));
-  const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e);
-  slope = 1.f - t * t;
-  return t * a.c2;
-}
+  // the tile at p, of which rows from `valid` on and channels past hd8 keep
+  // what the registers held
+  __device__ __forceinline__ void load(int valid, int hd8) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int cu = D == 96 ? c + 4 * u : c, ru = D == 96 ? r : r + RR * u;
+      const uint16_t* q = D == 96 ? p + 32 * u : p + RR * u * stride;
+      if (cu < hd8 && ru < valid) v[u] = *reinterpret_cast<const uint4*>(q);
+    }
+  }
+  __device__ __forceinline__ void next() { p += KT * stride; }
+  __device__ __forceinline__ void store(uint16_t* t) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      *reinterpret_cast<uint4*>(
+          t + (D == 96 ? toff<D>(r, c + 4 * u) : toff<D>(r + RR * u, c))) = v[u];
+  }
+  // NaN and infinities become 0; whether there were any.  bad[row] = tag for
+  // the rows that held one.
+  __device__ __forceinline__ bool clean(int* bad = nullptr, int tag = 0) {
+    bool any = false;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const bool b = clean8(v[u]);
+      any |= b;
+      if (bad && b) bad[D == 96 ? r : r + RR * u] = tag;
+    }
+    return any;
+  }
+};
 
-__device__ __forceinline__ float dist(int pos, int j) { return fabsf((float)(pos - j)); }
+// Scores.  t = z - ref from a raw product, all in the log2 domain.
+template <bool CAP, bool BIAS>
+struct Score {
+  float k;     // of the raw product: scale log2e; capped: scale / cap 2 log2e
+  float c2;    // cap log2e
+  float sl;    // slope log2e
+  __device__ __forceinline__ Score(const Dev& a, int h) {
+    k = CAP ? a.c1 * (2.f * LOG2E) : a.c1;
+    c2 = a.c2;
+    sl = BIAS ? a.slopes[h] * LOG2E : 0.f;
+  }
+  // far: the signed distance |pos - j|; dz receives d z / d (scale q.k)
+  __device__ __forceinline__ float operator()(float raw, float ref, float far, float& dz) const {
+    float t;
+    if (CAP) {
+      // tanh(x) = 1 - 2 r with r = 1 / (1 + e^(2x)), 1 - tanh^2 = 4 r (1 - r);
+      // e^(2x) may overflow to inf: r = 0
+      const float r = __builtin_amdgcn_rcpf(1.f + ex2(raw * k));
+      dz = 4.f * r * (1.f - r);
+      t = fmaf(-2.f * c2, r, c2 - ref);
+    } else {
+      dz = 1.f;
+      t = fmaf(raw, k, -ref);
+    }
+    return BIAS ? fmaf(-sl, fabsf(far), t) : t;
+  }
+};
 
 struct Row {
   int lo, hi, pos;
@@ -165,311 +253,518 @@ __device__ __forceinline__ Row row_at(const Dev& a, int i) {
   return Row{r.lo, r.hi, r.pos};
 }
 
-// ---------------------------------------------------------------------------
-// forward: block (64-row tile, head), wave w rows 16 w .. + 15
-// ---------------------------------------------------------------------------
-template <int D, bool CAP>
-__global__ __launch_bounds__(256) void k_mattn_fwd(Dev a) {
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Ps[4][16 * BT];
-  const int qt = blockIdx.x, h = blockIdx.y, kh = h / a.rep;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int q0 = qt * BT + 16 * w;
-  const MaskTile mt = a.tiles[qt];
-  const float sl = a.slopes ? a.slopes[h] * LOG2E : 0.f;
-  bf16x8 qa[D / 32];
-#pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk)
-    qa[kk] = row_frag(a.q + (long)(q0 + m) * a.qt + h * a.qh, 4 * kk + g, q0 + m < a.Tq, a.hd8);
-  Row rw[4];
-  float mx[4], l[4];
-  f32x4 acc[D / 16];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    rw[i] = row_at(a, q0 + 4 * g + i);
-    mx[i] = LOWEST;
-    l[i] = 0.f;
+// mask entry of rows [r0, r0 + n), n a multiple of the table's tile
+__device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
+  MaskTile b{1 << 30, 0, 0, 1 << 30};
+  for (int r = r0; r < r0 + n && r < a.Tq; r += MASK_TILE) {
+    const MaskTile t = a.tiles[r / MASK_TILE];
+    if (t.hi > t.lo) b.lo = min(b.lo, t.lo), b.hi = max(b.hi, t.hi);
+    b.all_lo = max(b.all_lo, t.all_lo);
+    b.all_hi = min(b.all_hi, t.all_hi);
   }
+  return b;
+}
+
+// (tile, head) of this block.  Blocks go round-robin over the 8 XCDs; each
+// XCD takes a contiguous range of the head-major order, so that a head's
+// tensors are fetched into one L2.  Tiles run from the last, which under a
+// causal mask has the most keys (first from the first, for the kernel over
+// keys).
+__device__ __forceinline__ void block_of(int tiles, int heads, bool last, int& tile, int& head) {
+  const int nb = tiles * heads, bid = __builtin_amdgcn_workgroup_id_x();
+  const int q = nb >> 3, r = nb & 7, x = bid & 7;
+  const int lb = x * q + (x < r ? x : r) + (bid >> 3);
+  head = lb / tiles;
+  tile = lb - head * tiles;
+  if (last) tile = tiles - 1 - tile;
+}
+
+constexpr int MP = 36;                      // row pitch of a merge buffer (floats)
+constexpr int MERGE = 4 * 32 * MP * 4;      // its bytes
+
+// Write the waves' column accumulators [channels][32 columns], times f, to
+// rows row0 + .. of out: 32 channels at a time meet in LDS, where the shares
+// of a group are added in order.  fix(row, chunk, o) may change 8 channels
+// before they are rounded.
+template <int D, int G, typename F>
+__device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 32], float f,
+                                           uint16_t* out, long stride, int row0, int rows, int hd8,
+                                           F fix) {
+  constexpr int SH = 4 / G;
+  const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
 #pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd) acc[jd] = zero4();
-  for (int k0 = mt.lo; k0 < mt.hi; k0 += BT) {
+  for (int d = 0; d < D / 32; ++d) {
     __syncthreads();
-    load_tile<D>(Ks, a.k + (long)k0 * a.kt + kh * a.kh, a.kt, a.Tk - k0, a.hd8);
-    load_tile<D>(Vs, a.v + (long)k0 * a.vt + kh * a.vh, a.vt, a.Tk - k0, a.hd8);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<f32x4*>(buf + (w * 32 + n) * MP + 8 * x + 4 * hl) =
+          f32x4{acc[d][4 * x] * f, acc[d][4 * x + 1] * f, acc[d][4 * x + 2] * f,
+                acc[d][4 * x + 3] * f};
     __syncthreads();
-    const bool part = mt.all_lo > k0 || mt.all_hi < k0 + BT;
-    f32x4 s[4];
+    for (int e = tid(); e < G * 128; e += 256) {
+      const int rb = e >> 2, c = e & 3, row = row0 + rb;
+      float o[8] = {};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s[j] = zero4();
+      for (int i = 0; i < SH; ++i) {
+        const float* s = buf + (((rb >> 5) * SH + i) * 32 + (rb & 31)) * MP + 8 * c;
 #pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk)
-        s[j] = mma(qa[kk], frag_row<D>(Ks, 16 * j + m, kk, g), s[j]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float v = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = k0 + 16 * j + m;
-        float dz;
-        float z = score<CAP>(a, s[j][i], dz) - sl * dist(rw[i].pos, key);
-        if (key < rw[i].lo || key >= rw[i].hi) z = -INFINITY;
-        s[j][i] = z;
-        v = fmaxf(v, z);
+        for (int t = 0; t < 8; ++t) o[t] += s[t];
       }
-#pragma unroll
-      for (int x = 1; x < 16; x <<= 1) v = fmaxf(v, __shfl_xor(v, x, 64));
-      const float nm = fmaxf(mx[i], v);
-      const float al = ex2(mx[i] - nm);
-      mx[i] = nm;
-      l[i] *= al;
-#pragma unroll
-      for (int jd = 0; jd < D / 16; ++jd) acc[jd][i] *= al;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = ex2(s[j][i] - nm);
-        l[i] += p;
-        sput(Ps[w], 4 * g + i, 16 * j + m, p);
-      }
+      if (row >= rows || 4 * d + c >= hd8) continue;
+      fix(row, 4 * d + c, o);
+      *reinterpret_cast<uint4*>(out + row * stride + 32 * d + 8 * c) =
+          uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
     }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 p = sfrag(Ps[w], m, ks, g);
-#pragma unroll
-      for (int jd = 0; jd < D / 16; ++jd) {
-        const bf16x8 v = frag_tr<D>(Vs, 32 * ks, 16 * jd, lane);
-        if (part && nonfinite(v))
-          acc[jd] = mma_rows(p, v, acc[jd], lane, [&](int r, int k) {
-            const Row x = row_at(a, q0 + r);
-            const int key = k0 + 32 * ks + k;
-            return key >= x.lo && key < x.hi;
-          });
-        else
-          acc[jd] = mma(p, v, acc[jd]);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor(l[i], x, 64);
-    const int r = q0 + 4 * g + i;
-    if (r >= a.Tq) continue;
-    const bool empty = rw[i].hi <= rw[i].lo;
-    const float f = empty ? 0.f : 1.f / l[i];
-    if (m == 0) a.lse[(long)h * a.Tq + r] = empty ? -INFINITY : (mx[i] + log2f(l[i])) * LN2;
-#pragma unroll
-    for (int jd = 0; jd < D / 16; ++jd)
-      if (2 * jd + (m >> 3) < a.hd8)
-        a.o[(long)r * a.ot + h * a.oh + 16 * jd + m] = f2bf(empty ? 0.f : acc[jd][i] * f);
   }
 }
 
+constexpr int max_of(int a, int b) { return a > b ? a : b; }
+// two stages of two tiles, later the merge buffer
+template <int D>
+constexpr int SMEM = max_of(4 * KT * D * 2, MERGE);
+
 // ---------------------------------------------------------------------------
-// backward, per 64-row tile: D = rowsum(do o), dq = ds k
+// forward
 // ---------------------------------------------------------------------------
-template <int D, bool CAP>
-__global__ __launch_bounds__(256) void k_mattn_bwd_q(Dev a) {
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Ss[4][16 * BT];
-  const int qt = blockIdx.x, h = blockIdx.y, kh = h / a.rep;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int q0 = qt * BT + 16 * w;
-  const MaskTile mt = a.tiles[qt];
-  const float sl = a.slopes ? a.slopes[h] * LOG2E : 0.f;
-  const bool in = q0 + m < a.Tq;
-  bf16x8 qa[D / 32], da[D / 32];
-  float dpart = 0.f;
-#pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) {
-    const long r = q0 + m;
-    qa[kk] = row_frag(a.q + r * a.qt + h * a.qh, 4 * kk + g, in, a.hd8);
-    da[kk] = row_frag(a.dout + r * a.dot + h * a.doh, 4 * kk + g, in, a.hd8);
-    const bf16x8 ov = row_frag(a.o_in + r * a.ot + h * a.oh, 4 * kk + g, in, a.hd8);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) dpart += (float)da[kk][t] * (float)ov[t];
+template <int D, int G, int WPE, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
+  constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
+  __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
+  __shared__ float ml[4][2][32];
+  __shared__ int any_odd;
+  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
+  int tile, h;
+  block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
+  const int kh = h / a.rep;
+  const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
+  const int grp = w / SH, shr = w % SH;
+  const int qrow = tile * RB + grp * 32 + n;
+  MaskTile mt{0, 0, 0, 0};  // of the tile that holds the wave's rows
+  if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
+  const MaskTile bt = tiles_at(a, tile * RB, RB);
+  const uint16_t* vbase = a.v + kh * a.vh;
+  Stage<D> sk, sv;
+  sk.init(a.k + kh * a.kh, bt.lo, a.kt);
+  sv.init(vbase, bt.lo, a.vt);
+  if (bt.lo < bt.hi) {
+    sk.load(a.Tk - bt.lo, a.hd8);
+    sv.load(a.Tk - bt.lo, a.hd8);
   }
-  dpart += __shfl_xor(dpart, 16, 64);
-  dpart += __shfl_xor(dpart, 32, 64);
-  if (g == 0 && in) a.dsum[(long)h * a.Tq + q0 + m] = dpart;
-  Row rw[4];
-  float Di[4], li[4];
+  Score<CAP, BIAS> score(a, h);
+  const bool neg = score.k < 0.f;
+  // q carries the sign of the scale, so that the largest raw product is the
+  // largest score; a scale of 0 becomes so small that scores vanish but a
+  // masked -inf stays
+  score.k = fmaxf(fabsf(score.k), 1e-37f);
+  const Row rw = row_at(a, qrow);
+  bf16x8 qf[D / 16];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = q0 + 4 * g + i;
-    rw[i] = row_at(a, r);
-    Di[i] = __shfl(dpart, 4 * g + i, 64);
-    li[i] = r < a.Tq ? a.lse[(long)h * a.Tq + r] * LOG2E : 0.f;
+  for (int kk = 0; kk < D / 16; ++kk) {
+    qf[kk] = row_frag(a.q + qrow * a.qt + h * a.qh, 2 * kk + hl, qrow < a.Tq, a.hd8);
+    if (neg) qf[kk] = -qf[kk];
   }
-  f32x4 acc[D / 16];
+  float ref = 0.f, l = 0.f;  // l == 0: no reference yet
+  f32x16 acc[D / 32];
 #pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd) acc[jd] = zero4();
-  for (int k0 = mt.lo; k0 < mt.hi; k0 += BT) {
+  for (int d = 0; d < D / 32; ++d) acc[d] = splat(0.f);
+  bool odd = false;  // this thread has left values out
+
+  int it = 0;
+  for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
+    uint16_t* Ks = buf + (it & 1) * 2 * TILE;
+    uint16_t* Vs = Ks + TILE;
+    // this stage was last read two tiles ago, before the previous barrier
+    if (bt.all_lo > k0 || bt.all_hi < k0 + KT) odd |= sv.clean();
+    sk.store(Ks);
+    sv.store(Vs);
     __syncthreads();
-    load_tile<D>(Ks, a.k + (long)k0 * a.kt + kh * a.kh, a.kt, a.Tk - k0, a.hd8);
-    load_tile<D>(Vs, a.v + (long)k0 * a.vt + kh * a.vh, a.vt, a.Tk - k0, a.hd8);
-    __syncthreads();
-    const bool part = mt.all_lo > k0 || mt.all_hi < k0 + BT;
-    f32x4 s[4], dp[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s[j] = zero4();
-      dp[j] = zero4();
-#pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) {
-        s[j] = mma(qa[kk], frag_row<D>(Ks, 16 * j + m, kk, g), s[j]);
-        dp[j] = mma(da[kk], frag_row<D>(Vs, 16 * j + m, kk, g), dp[j]);
-      }
+    if (k0 + KT < bt.hi) {
+      sk.next();
+      sv.next();
+      sk.load(a.Tk - k0 - KT, a.hd8);
+      sv.load(a.Tk - k0 - KT, a.hd8);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int u = 0; u < 2 / SH; ++u) {
+      const int r0 = 32 * (SH * u + shr);  // the step's first key in the tile
+      const int kb = k0 + r0;
+      if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
+      f32x16 s = splat(0.f);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = k0 + 16 * j + m;
+      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Ks, r0, kk, lane), qf[kk], s);
+      const float far = (float)(rw.pos - kb - 8 * hl);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
         float dz;
-        const float z = score<CAP>(a, s[j][i], dz) - sl * dist(rw[i].pos, key);
-        float ds = ex2(z - li[i]) * (dp[j][i] - Di[i]) * dz;
-        if (key < rw[i].lo || key >= rw[i].hi) ds = 0.f;
-        sput(Ss[w], 4 * g + i, 16 * j + m, ds);
+        s[i] = score(s[i], ref, far - (float)elem(i), dz);
+      }
+      if (mt.all_lo > kb || mt.all_hi < kb + 32) {
+        const uint32_t off = kb + 8 * hl - rw.lo, len = rw.hi - rw.lo;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (off + elem(i) >= len) s[i] = -INFINITY;
+      }
+      float mx = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+      if (__any(mx > (l == 0.f ? LOWEST : GROW))) {
+        // relative to the old reference; the first may lie below it
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool first = l + __shfl_xor(l, 32, 64) == 0.f;
+        const float up = mx > LOWEST && (first || mx > 0.f) ? mx : 0.f;
+        const float al = first ? 0.f : ex2(-up);
+        ref += up;
+        l *= al;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] -= up;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= al;
+      }
+      bf16x8 p[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = ex2(s[i]);
+        l += e;
+        p[i / 8][i % 8] = (__bf16)e;
       }
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 p = sfrag(Ss[w], m, ks, g);
+      for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int jd = 0; jd < D / 16; ++jd) {
-        const bf16x8 v = frag_tr<D>(Ks, 32 * ks, 16 * jd, lane);
-        if (part && nonfinite(v))
-          acc[jd] = mma_rows(p, v, acc[jd], lane, [&](int r, int k) {
-            const Row x = row_at(a, q0 + r);
-            const int key = k0 + 32 * ks + k;
-            return key >= x.lo && key < x.hi;
-          });
-        else
-          acc[jd] = mma(p, v, acc[jd]);
-      }
+        for (int ks = 0; ks < 2; ++ks)
+          acc[d] = mma(cols32<D>(Vs, r0 + 16 * ks, 32 * d, lane), p[ks], acc[d]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = q0 + 4 * g + i;
-    if (r >= a.Tq) continue;
-#pragma unroll
-    for (int jd = 0; jd < D / 16; ++jd)
-      if (2 * jd + (m >> 3) < a.hd8)
-        a.dq[(long)r * a.dqt + h * a.dqh + 16 * jd + m] = f2bf(acc[jd][i] * a.scale);
+
+  // merge: R = max ref, l = sum l 2^(ref - R), o = sum o 2^(ref - R) / l
+  if (tid() == 0) any_odd = 0;
+  l += __shfl_xor(l, 32, 64);
+  if (l == 0.f) ref = LOWEST;
+  if (hl == 0) {
+    ml[w][0][n] = ref;
+    ml[w][1][n] = l;
   }
+  __syncthreads();  // also: every wave is done with the tiles
+  if (odd) any_odd = 1;
+  float R = ref, t = 0.f;
+#pragma unroll
+  for (int i = 0; i < SH; ++i) R = fmaxf(R, ml[grp * SH + i][0][n]);
+#pragma unroll
+  for (int i = 0; i < SH; ++i) t += ml[grp * SH + i][1][n] * ex2(ml[grp * SH + i][0][n] - R);
+  const bool empty = rw.hi <= rw.lo;
+  if (shr == 0 && hl == 0 && qrow < a.Tq)
+    a.lse[(long)h * a.Tq + qrow] = empty ? -INFINITY : (R + __builtin_amdgcn_logf(t)) * LN2;
+  // an empty row's accumulators are 0
+  write_rows<D, G>(reinterpret_cast<float*>(smem), acc, empty ? 0.f : ex2(ref - R) / t,
+                   a.o + h * a.oh, a.ot, tile * RB, a.Tq, a.hd8,
+                   [&](int row, int c, float (&o)[8]) {
+                     if (!any_odd) return;
+                     const Row x = row_at(a, row);
+                     for (int j = x.lo; j < x.hi; ++j)
+                       add_odd(o, *reinterpret_cast<const uint4*>(vbase + j * a.vt + 8 * c), false);
+                   });
 }
 
 // ---------------------------------------------------------------------------
-// backward, per 64-key tile and key head: wave w owns keys 16 w .. + 15; the
-// query tiles of every head of the group that attend any of its keys stream by
+// backward over query rows: D = rowsum(do o), dq = ds k
 // ---------------------------------------------------------------------------
-template <int D, bool CAP>
-__global__ __launch_bounds__(256) void k_mattn_bwd_kv(Dev a) {
-  __shared__ __attribute__((aligned(16))) uint16_t Qs[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Os[BT * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Ws[4][16 * BT];
-  const int kt0 = blockIdx.x * BT, kh = blockIdx.y;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int k0 = kt0 + 16 * w;
-  const int nqt = mask_tiles(a.Tq);
-  bf16x8 ka[D / 32], va[D / 32];
-#pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) {
-    const bool in = k0 + m < a.Tk;
-    ka[kk] = row_frag(a.k + (long)(k0 + m) * a.kt + kh * a.kh, 4 * kk + g, in, a.hd8);
-    va[kk] = row_frag(a.v + (long)(k0 + m) * a.vt + kh * a.vh, 4 * kk + g, in, a.hd8);
+template <int D, int G, int WPE, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
+  constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
+  __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
+  __shared__ int bad[2][KT];  // tile in which a key held a NaN or infinity
+  __shared__ int odd_at[2], any_odd;
+  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
+  int tile, h;
+  block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
+  const int kh = h / a.rep;
+  const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
+  const int grp = w / SH, shr = w % SH;
+  const int qrow = tile * RB + grp * 32 + n;
+  MaskTile mt{0, 0, 0, 0};
+  if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
+  const MaskTile bt = tiles_at(a, tile * RB, RB);
+  const uint16_t* kbase = a.k + kh * a.kh;
+  Stage<D> sk, sv;
+  sk.init(kbase, bt.lo, a.kt);
+  sv.init(a.v + kh * a.vh, bt.lo, a.vt);
+  if (bt.lo < bt.hi) {
+    sk.load(a.Tk - bt.lo, a.hd8);
+    sv.load(a.Tk - bt.lo, a.hd8);
   }
-  f32x4 dk[D / 16], dv[D / 16];
+  if (tid() < 2 * KT) bad[tid() / KT][tid() % KT] = -1;
+  if (tid() < 2) odd_at[tid()] = -1;
+  if (tid() == 0) any_odd = 0;
+  const Score<CAP, BIAS> score(a, h);
+  const Row rw = row_at(a, qrow);
+  const bool in = qrow < a.Tq;
+  bf16x8 qf[D / 16], df[D / 16];
+  float Dq = 0.f;
 #pragma unroll
-  for (int jd = 0; jd < D / 16; ++jd) dk[jd] = dv[jd] = zero4();
-  for (int h = kh * a.rep; h < (kh + 1) * a.rep; ++h) {
-    const float sl = a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    for (int qt = 0; qt < nqt; ++qt) {
-      const MaskTile mt = a.tiles[qt];
-      if (mt.lo >= kt0 + BT || mt.hi <= kt0) continue;
-      const bool part = mt.all_lo > kt0 || mt.all_hi < kt0 + BT;
-      const int q0 = qt * BT;
-      __syncthreads();
-      load_tile<D>(Qs, a.q + (long)q0 * a.qt + h * a.qh, a.qt, a.Tq - q0, a.hd8);
-      load_tile<D>(Os, a.dout + (long)q0 * a.dot + h * a.doh, a.dot, a.Tq - q0, a.hd8);
-      __syncthreads();
-      f32x4 s[4], dp[4];
+  for (int kk = 0; kk < D / 16; ++kk) {
+    qf[kk] = row_frag(a.q + qrow * a.qt + h * a.qh, 2 * kk + hl, in, a.hd8);
+    df[kk] = row_frag(a.dout + qrow * a.dot + h * a.doh, 2 * kk + hl, in, a.hd8);
+    const bf16x8 ov = row_frag(a.o_in + qrow * a.ot + h * a.oh, 2 * kk + hl, in, a.hd8);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[j] = zero4();
-        dp[j] = zero4();
+    for (int t = 0; t < 8; ++t) Dq += (float)df[kk][t] * (float)ov[t];
+  }
+  Dq += __shfl_xor(Dq, 32, 64);
+  float l2 = 0.f;
+  if (in) {
+    if (shr == 0 && hl == 0) a.dsum[(long)h * a.Tq + qrow] = Dq;
+    // of a row that attends something: no score of it makes a p then
+    l2 = finite_or_nan(a.lse[(long)h * a.Tq + qrow]) * LOG2E;
+  }
+  f32x16 acc[D / 32];
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-          s[j] = mma(ka[kk], frag_row<D>(Qs, 16 * j + m, kk, g), s[j]);
-          dp[j] = mma(va[kk], frag_row<D>(Os, 16 * j + m, kk, g), dp[j]);
-        }
+  for (int d = 0; d < D / 32; ++d) acc[d] = splat(0.f);
+  __syncthreads();  // bad
+
+  int it = 0;
+  for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
+    uint16_t* Ks = buf + (it & 1) * 2 * TILE;
+    uint16_t* Vs = Ks + TILE;
+    const bool partly = bt.all_lo > k0 || bt.all_hi < k0 + KT;
+    if (partly && sk.clean(bad[it & 1], it)) {
+      odd_at[it & 1] = it;
+      any_odd = 1;
+    }
+    sk.store(Ks);
+    sv.store(Vs);
+    __syncthreads();
+    if (k0 + KT < bt.hi) {
+      sk.next();
+      sv.next();
+      sk.load(a.Tk - k0 - KT, a.hd8);
+      sv.load(a.Tk - k0 - KT, a.hd8);
+    }
+#pragma unroll
+    for (int u = 0; u < 2 / SH; ++u) {
+      const int r0 = 32 * (SH * u + shr);
+      const int kb = k0 + r0;
+      if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
+      f32x16 s = splat(0.f), dp = splat(0.f);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Ks, r0, kk, lane), qf[kk], s);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) dp = mma(rows32<D>(Vs, r0, kk, lane), df[kk], dp);
+      const float far = (float)(rw.pos - kb - 8 * hl);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float dz;
+        const float p = ex2(score(s[i], l2, far - (float)elem(i), dz));
+        s[i] = p * (dp[i] - Dq);
+        if (CAP) s[i] *= dz;
       }
+      if (mt.all_lo > kb || mt.all_hi < kb + 32) {
+        const uint32_t off = kb + 8 * hl - rw.lo, len = rw.hi - rw.lo;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int q = q0 + 16 * j + m;
-        const Row x = row_at(a, q);
-        const float lq = q < a.Tq ? a.lse[(long)h * a.Tq + q] * LOG2E : 0.f;
-        const float Dq = q < a.Tq ? a.dsum[(long)h * a.Tq + q] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = k0 + 4 * g + i;
-          float dz;
-          const float z = score<CAP>(a, s[j][i], dz) - sl * dist(x.pos, key);
-          float p = ex2(z - lq);
-          float ds = p * (dp[j][i] - Dq) * dz;
-          if (key < x.lo || key >= x.hi) p = ds = 0.f;
-          dp[j][i] = ds;
-          sput(Ws[w], 4 * g + i, 16 * j + m, p);
-        }
+        for (int i = 0; i < 16; ++i)
+          if (off + elem(i) >= len) s[i] = 0.f;
       }
-      const auto keep = [&](int ks) {
-        return [&, ks](int r, int k) {
-          const Row x = row_at(a, q0 + 32 * ks + k);
-          return k0 + r >= x.lo && k0 + r < x.hi;
-        };
-      };
+      if (partly && odd_at[it & 1] == it) {
+        // a cleared key's score is not what it was; the rows that attend it
+        // get their NaN at the end
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 p = sfrag(Ws[w], m, ks, g);
-#pragma unroll
-        for (int jd = 0; jd < D / 16; ++jd) {
-          const bf16x8 v = frag_tr<D>(Os, 32 * ks, 16 * jd, lane);
-          dv[jd] = part && nonfinite(v) ? mma_rows(p, v, dv[jd], lane, keep(ks))
-                                        : mma(p, v, dv[jd]);
-        }
+        for (int i = 0; i < 16; ++i)
+          if (bad[it & 1][r0 + 8 * hl + elem(i)] == it) s[i] = 0.f;
       }
+      bf16x8 ds[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int i = 0; i < 16; ++i) ds[i / 8][i % 8] = (__bf16)s[i];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sput(Ws[w], 4 * g + i, 16 * j + m, dp[j][i]);
+      for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 p = sfrag(Ws[w], m, ks, g);
-#pragma unroll
-        for (int jd = 0; jd < D / 16; ++jd) {
-          const bf16x8 v = frag_tr<D>(Qs, 32 * ks, 16 * jd, lane);
-          dk[jd] = part && nonfinite(v) ? mma_rows(p, v, dk[jd], lane, keep(ks))
-                                        : mma(p, v, dk[jd]);
-        }
-      }
+        for (int ks = 0; ks < 2; ++ks)
+          acc[d] = mma(cols32<D>(Ks, r0 + 16 * ks, 32 * d, lane), ds[ks], acc[d]);
     }
   }
+  write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
+                   tile * RB, a.Tq, a.hd8, [&](int row, int c, float (&o)[8]) {
+                     if (!any_odd) return;
+                     const Row x = row_at(a, row);
+                     if (x.hi <= x.lo) return;
+                     const float e = finite_or_nan(a.lse[(long)h * a.Tq + row]) * 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = k0 + 4 * g + i;
-    if (r >= a.Tk) continue;
-#pragma unroll
-    for (int jd = 0; jd < D / 16; ++jd)
-      if (2 * jd + (m >> 3) < a.hd8) {
-        const int c = 16 * jd + m;
-        a.dk[(long)r * a.dkt + kh * a.dkh + c] = f2bf(dk[jd][i] * a.scale);
-        a.dv[(long)r * a.dvt + kh * a.dvh + c] = f2bf(dv[jd][i]);
-      }
+                     for (int t = 0; t < 8; ++t) o[t] += e;
+                     for (int j = x.lo; j < x.hi; ++j)
+                       add_odd(o, *reinterpret_cast<const uint4*>(kbase + j * a.kt + 8 * c), true);
+                   });
+}
+
+// The tiles of query rows, in order, some of whose rows attend some of keys
+// [k0, k1).  Every wave of a block sees the same ones: a wave looks at 64
+// table entries at a time.
+struct Hits {
+  int base, k0, k1;
+  uint64_t bits;
+  __device__ __forceinline__ void look(const Dev& a, int lane) {
+    const int t = base + lane;
+    bool hit = false;
+    if (t < mask_tiles(a.Tq)) {
+      const MaskTile m = a.tiles[t];
+      hit = m.lo < k1 && m.hi > k0;
+    }
+    bits = __ballot(hit);
   }
+  __device__ __forceinline__ void start(const Dev& a, int lane) {
+    base = 0;
+    look(a, lane);
+  }
+  // the next tile, or -1
+  __device__ __forceinline__ int next(const Dev& a, int lane) {
+    while (bits == 0) {
+      base += 64;
+      if (base >= mask_tiles(a.Tq)) return -1;
+      look(a, lane);
+    }
+    const int t = base + __builtin_ctzll(bits);
+    bits &= bits - 1;
+    return t;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// backward over keys: dk = ds^T q, dv = p^T do, the query rows of every head
+// of the group that attend any of the block's keys streaming by
+// ---------------------------------------------------------------------------
+template <int D, int G, int WPE, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
+  constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
+  __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
+  __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT];
+  __shared__ __attribute__((aligned(16))) int Lo[2][KT], Len[2][KT], Pos[2][KT];
+  __shared__ int any_odd;
+  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
+  int tile, kh;
+  block_of((a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh);
+  const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
+  const int grp = w / SH, shr = w % SH;
+  const int kb0 = tile * RB + grp * 32, key = kb0 + n;
+  if (tid() == 0) any_odd = 0;
+  bf16x8 kf[D / 16], vf[D / 16];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    kf[kk] = row_frag(a.k + key * a.kt + kh * a.kh, 2 * kk + hl, key < a.Tk, a.hd8);
+    vf[kk] = row_frag(a.v + key * a.vt + kh * a.vh, 2 * kk + hl, key < a.Tk, a.hd8);
+  }
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = splat(0.f);
+  Stage<D> sq, sd;
+  sq.init(a.q, 0, a.qt);
+  sd.init(a.dout, 0, a.dot);
+  Hits hits;
+  hits.k0 = tile * RB;
+  hits.k1 = tile * RB + RB;
+  float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
+  Row rn{0, 0, 0};
+  __syncthreads();  // any_odd
+
+  // (h, qt) is the tile in the registers, which goes to LDS next
+  const auto fetch = [&](int h, int qt) {
+    const long r = (long)qt * KT;
+    sq.p = a.q + (r + sq.r) * a.qt + h * a.qh + 8 * sq.c;
+    sd.p = a.dout + (r + sd.r) * a.dot + h * a.doh + 8 * sd.c;
+    sq.load(a.Tq - qt * KT, a.hd8);
+    sd.load(a.Tq - qt * KT, a.hd8);
+    if (tid() < KT) {
+      const int i = qt * KT + tid();
+      rn = row_at(a, i);
+      if (i < a.Tq) {
+        ln = a.lse[(long)h * a.Tq + i];
+        dn = a.dsum[(long)h * a.Tq + i];
+      }
+    }
+  };
+  int h = kh * a.rep;
+  hits.start(a, lane);
+  int qt = hits.next(a, lane);
+  if (qt >= 0) fetch(h, qt);
+  for (int it = 0; qt >= 0; ++it) {
+    uint16_t* Qs = buf + (it & 1) * 2 * TILE;
+    uint16_t* Os = Qs + TILE;
+    const Score<CAP, BIAS> score(a, h);
+    const MaskTile mt = a.tiles[qt];
+    if (mt.all_lo > hits.k0 || mt.all_hi < hits.k1) {
+      sq.clean();  // a row with such a q has no finite lse
+      if (sd.clean()) any_odd = 1;
+    }
+    sq.store(Qs);
+    sd.store(Os);
+    if (tid() < KT) {
+      Ls[it & 1][tid()] = finite_or_nan(ln) * LOG2E;
+      Ds[it & 1][tid()] = finite_or_nan(dn);
+      Lo[it & 1][tid()] = rn.lo;
+      Len[it & 1][tid()] = rn.hi - rn.lo;
+      Pos[it & 1][tid()] = rn.pos;
+    }
+    __syncthreads();
+    int qn = hits.next(a, lane);
+    if (qn < 0 && h + 1 < (kh + 1) * a.rep) {
+      ++h;
+      hits.start(a, lane);
+      qn = hits.next(a, lane);
+    }
+    if (qn >= 0) fetch(h, qn);
+#pragma unroll
+    for (int u = 0; u < 2 / SH; ++u) {
+      const int r0 = 32 * (SH * u + shr);  // the step's first row in the tile
+      const int rb = r0 + 8 * hl;
+      if (kb0 >= mt.hi || kb0 + 32 <= mt.lo) continue;
+      f32x16 s = splat(0.f), dp = splat(0.f);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Qs, r0, kk, lane), kf[kk], s);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) dp = mma(rows32<D>(Os, r0, kk, lane), vf[kk], dp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = rb + elem(i);
+        float dz;
+        const float far = BIAS ? (float)(Pos[it & 1][r] - key) : 0.f;
+        const float p = ex2(score(s[i], Ls[it & 1][r], far, dz));
+        dp[i] = p * (dp[i] - Ds[it & 1][r]);
+        if (CAP) dp[i] *= dz;
+        s[i] = p;
+      }
+      if (mt.all_lo > kb0 || mt.all_hi < kb0 + 32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = rb + elem(i);
+          if ((uint32_t)(key - Lo[it & 1][r]) >= (uint32_t)Len[it & 1][r]) s[i] = dp[i] = 0.f;
+        }
+      }
+      bf16x8 p[2], ds[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i / 8][i % 8] = (__bf16)s[i];
+        ds[i / 8][i % 8] = (__bf16)dp[i];
+      }
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          dv[d] = mma(cols32<D>(Os, r0 + 16 * ks, 32 * d, lane), p[ks], dv[d]);
+          dk[d] = mma(cols32<D>(Qs, r0 + 16 * ks, 32 * d, lane), ds[ks], dk[d]);
+        }
+    }
+    qt = qn;
+  }
+  float* mb = reinterpret_cast<float*>(smem);
+  write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt, tile * RB, a.Tk, a.hd8,
+                   [](int, int, float (&)[8]) {});
+  write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt, tile * RB, a.Tk, a.hd8,
+                   [&](int j, int c, float (&o)[8]) {
+                     if (!any_odd) return;
+                     for (int i = 0; i < a.Tq; ++i) {
+                       const Row x = row_at(a, i);
+                       if (j < x.lo || j >= x.hi) continue;
+                       for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
+                         add_odd(o, *reinterpret_cast<const uint4*>(a.dout + i * a.dot +
+                                                                    g * a.doh + 8 * c), false);
+                     }
+                   });
 }
 
 Dev view(const MattnArgs& a) {
@@ -498,23 +793,46 @@ Dev view(const MattnArgs& a) {
   return d;
 }
 
-template <int D, bool CAP>
-hipError_t fwd(const Dev& d, hipStream_t st) {
-  hipLaunchKernelGGL((k_mattn_fwd<D, CAP>), dim3(mask_tiles(d.Tq), d.H), dim3(256), 0, st, d);
+enum Pass { FWD, BWD_Q, BWD_KV };
+
+template <Pass P, int D, int G, int WPE, bool CAP, bool BIAS>
+hipError_t launch(const Dev& d, hipStream_t st) {
+  constexpr int RB = 32 * G;
+  const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
+  if (rows == 0) return hipSuccess;
+  const dim3 grid((rows + RB - 1) / RB * heads), block(256);
+  if constexpr (P == FWD)
+    hipLaunchKernelGGL((k_mattn_fwd<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
+  else if constexpr (P == BWD_Q)
+    hipLaunchKernelGGL((k_mattn_bwd_q<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
+  else
+    hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
   return hipGetLastError();
 }
 
-template <int D, bool CAP>
-hipError_t bwd(const Dev& d, hipStream_t st) {
-  if (d.Tq) {
-    hipLaunchKernelGGL((k_mattn_bwd_q<D, CAP>), dim3(mask_tiles(d.Tq), d.H), dim3(256), 0, st, d);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (d.Tk)
-    hipLaunchKernelGGL((k_mattn_bwd_kv<D, CAP>), dim3((d.Tk + BT - 1) / BT, d.H / d.rep),
-                       dim3(256), 0, st, d);
-  return hipGetLastError();
+template <Pass P, int D, int G, int WPE>
+hipError_t launch_mode(const Dev& d, hipStream_t st) {
+  const bool cap = d.c2 > 0.f;
+  if (cap && d.slopes) return launch<P, D, G, WPE, true, true>(d, st);
+  if (cap) return launch<P, D, G, WPE, true, false>(d, st);
+  if (d.slopes) return launch<P, D, G, WPE, false, true>(d, st);
+  return launch<P, D, G, WPE, false, false>(d, st);
+}
+
+// Rows per block.
+template <Pass P, int D>
+hipError_t launch_rows(const Dev& d, hipStream_t st) {
+  constexpr int W = P == BWD_KV ? (D == 128 ? 1 : 2) : D == 64 ? 3 : 2;
+  const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
+  if ((long)((rows + 127) / 128) * heads >= 512) return launch_mode<P, D, 4, W>(d, st);
+  return launch_mode<P, D, 2, W>(d, st);
+}
+
+template <Pass P>
+hipError_t launch_dim(const Dev& d, hipStream_t st) {
+  if (d.hd8 <= 8) return launch_rows<P, 64>(d, st);
+  if (d.hd8 <= 12) return launch_rows<P, 96>(d, st);
+  return launch_rows<P, 128>(d, st);
 }
 
 }  // namespace
@@ -525,20 +843,13 @@ size_t mattn_bwd_bytes(const pulse_attn_desc& d) {
 }
 
 hipError_t launch_mattn_fwd(const MattnArgs& a, hipStream_t st) {
-  if (a.Tq == 0) return hipSuccess;
-  const Dev d = view(a);
-  const bool cap = a.cap > 0.f;
-  if (a.hd <= 64) return cap ? fwd<64, true>(d, st) : fwd<64, false>(d, st);
-  if (a.hd <= 96) return cap ? fwd<96, true>(d, st) : fwd<96, false>(d, st);
-  return cap ? fwd<128, true>(d, st) : fwd<128, false>(d, st);
+  return launch_dim<FWD>(view(a), st);
 }
 
 hipError_t launch_mattn_bwd(const MattnArgs& a, hipStream_t st) {
   const Dev d = view(a);
-  const bool cap = a.cap > 0.f;
-  if (a.hd <= 64) return cap ? bwd<64, true>(d, st) : bwd<64, false>(d, st);
-  if (a.hd <= 96) return cap ? bwd<96, true>(d, st) : bwd<96, false>(d, st);
-  return cap ? bwd<128, true>(d, st) : bwd<128, false>(d, st);
+  const hipError_t e = launch_dim<BWD_Q>(d, st);
+  return e == hipSuccess ? launch_dim<BWD_KV>(d, st) : e;
 }
 
 }  // namespace pulse
