@@ -49,6 +49,7 @@ constexpr float GROW = 8.f;
 struct Dev {  // device view of MattnArgs
   int Tq, Tk, H, rep, hd8;
   float c1, c2;  // no cap: scale log2e; cap: scale / cap and cap log2e
+  float inv_c1;
   float scale;
   const uint16_t *q, *k, *v, *dout, *o_in;
   uint16_t *o, *dq, *dk, *dv;
@@ -85,16 +86,19 @@ __device__ __forceinline__ int swap23(int r) { return (r & ~12) | ((r & 4) << 1)
 // offset of element i of an output column from its first row (8 hl)
 __device__ __forceinline__ constexpr int elem(int i) { return 16 * (i / 8) + i % 8; }
 
-// element offset of 16-byte chunk c of row r of a [rows][D] tile; the chunks
-// of a row are permuted so that the rows that one LDS access reads fall on
+// Tiles are [rows][D] with the 16-byte chunks of a row permuted (chunk c of
+// row r at c ^ mix(r)), so that the rows that one LDS access reads fall on
 // distinct banks: {0-3, 8-11} (+4, +16) of one chunk (rows32), {0-3} of two
-// (cols32)
+// (cols32).
 template <int D>
-__device__ __forceinline__ int toff(int r, int c) {
-  const int x = D == 64 ? ((((r >> 1) & 1) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 2))
-              : D == 96 ? ((r >> 2) & 3)
-                        : ((r & 3) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 3);
-  return r * D + ((c ^ x) << 3);
+__device__ __forceinline__ int mix(int r) {
+  return D == 64 ? ((((r >> 1) & 1) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 2))
+       : D == 96 ? ((r >> 2) & 3)
+                 : ((r & 3) << 1) | ((r >> 2) & 1) | (((r >> 3) & 1) << 3);
+}
+template <int D>
+__device__ __forceinline__ int toff(int r, int c) {  // in elements
+  return r * D + ((c ^ mix<D>(r)) << 3);
 }
 
 // operand of 8 consecutive channels straight from memory (0 where absent)
@@ -104,28 +108,39 @@ __device__ __forceinline__ bf16x8 row_frag(const uint16_t* p, int c, bool ok, in
   return __builtin_bit_cast(bf16x8, v);
 }
 
-__device__ __forceinline__ v4s rd_tr(const uint16_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p));
-}
+// Fragment addresses are a lane's byte offset in the tile, changed by an xor
+// of a constant (the channels) and a constant offset (the rows): few registers
+// hold them all.
 
 // A operand of rows: lane (n, hl) gets channels 16 kk + 8 hl .. + 7 of row
-// r0 + swap23(n)
+// swap23(n) (+ rows in `at`)
 template <int D>
-__device__ __forceinline__ bf16x8 rows32(const uint16_t* t, int r0, int kk, int lane) {
-  return *reinterpret_cast<const bf16x8*>(
-      t + toff<D>(r0 + swap23(lane & 31), 2 * kk + (lane >> 5)));
+__device__ __forceinline__ int rows_base(int lane) {
+  const int r = swap23(lane & 31);
+  return r * 2 * D + (((lane >> 5) ^ mix<D>(r)) << 4);
+}
+template <int D>
+__device__ __forceinline__ bf16x8 rows32(const char* tile, int base, int kk, int at) {
+  const int x = D == 96 ? (base ^ ((kk & 1) << 5)) + 64 * (kk >> 1) : base ^ (kk << 5);
+  return *reinterpret_cast<const bf16x8*>(tile + x + at);
 }
 
-// A operand read down the tile: lane (n, hl) gets rows r0 + 8 hl .. + 7 of
-// channel d0 + n.  ds_read_b64_tr_b16: within 16 lanes, lane j receives
-// element j % 4 of the rows addressed by lanes 4 t + j / 4 (t = 0..3).
+// A operand read down the tile: lane (n, hl) gets rows 8 hl .. + 7 (+ rows in
+// `at`) of channel 32 d + n.  ds_read_b64_tr_b16: within 16 lanes, lane j
+// receives element j % 4 of the rows addressed by lanes 4 t + j / 4
+// (t = 0..3).
 template <int D>
-__device__ __forceinline__ bf16x8 cols32(const uint16_t* t, int r0, int d0, int lane) {
-  const int j = lane & 15;
-  const int col = d0 + (lane & 16) + 4 * (j & 3);
-  const int r = r0 + 8 * (lane >> 5) + (j >> 2);
-  const v4s lo = rd_tr(t + toff<D>(r, col >> 3) + (col & 7));
-  const v4s hi = rd_tr(t + toff<D>(r + 4, col >> 3) + (col & 7));
+__device__ __forceinline__ int cols_base(int lane) {
+  const int j = lane & 15, r = 8 * (lane >> 5) + (j >> 2);
+  const int c = 2 * ((lane >> 4) & 1) + ((j & 3) >> 1);
+  return r * 2 * D + ((c ^ mix<D>(r)) << 4) + 8 * (j & 1);
+}
+template <int D>
+__device__ __forceinline__ bf16x8 cols32(const char* tile, int base, int d, int at) {
+  const int x = D == 96 ? base + 64 * d : base ^ (d << 6);
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + x + at));
+  // rows + 4: one bit of their chunks' permutation changes
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + (x ^ 16) + at + 8 * D));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -185,14 +200,23 @@ struct Stage {
 #pragma unroll
     for (int u = 0; u < N; ++u) v[u] = uint4{0, 0, 0, 0};
   }
-  // the tile at p, of which rows from `valid` on and channels past hd8 keep
-  // what the registers held
+  // the tile at p, of which `valid` >= 1 rows exist: the last one stands in
+  // for those past it (no row attends them).  Channels past hd8 stay 0.
   __device__ __forceinline__ void load(int valid, int hd8) {
+    if constexpr (D == 96) {
+      const uint16_t* q = r < valid ? p : p + (valid - 1 - r) * stride;
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int cu = D == 96 ? c + 4 * u : c, ru = D == 96 ? r : r + RR * u;
-      const uint16_t* q = D == 96 ? p + 32 * u : p + RR * u * stride;
-      if (cu < hd8 && ru < valid) v[u] = *reinterpret_cast<const uint4*>(q);
+      for (int u = 0; u < N; ++u)
+        if (c + 4 * u < hd8) v[u] = *reinterpret_cast<const uint4*>(q + 32 * u);
+    } else if (c < hd8) {
+      if (valid >= KT) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] = *reinterpret_cast<const uint4*>(p + RR * u * stride);
+      } else {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+          v[u] = *reinterpret_cast<const uint4*>(p + (min(r + RR * u, valid - 1) - r) * stride);
+      }
     }
   }
   __device__ __forceinline__ void next() { p += KT * stride; }
@@ -332,12 +356,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ float ml[4][2][32];
   __shared__ int any_odd;
-  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
   int tile, h;
   block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
   const int kh = h / a.rep;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
+  const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int qrow = tile * RB + grp * 32 + n;
   MaskTile mt{0, 0, 0, 0};  // of the tile that holds the wave's rows
   if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
@@ -352,10 +376,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   }
   Score<CAP, BIAS> score(a, h);
   const bool neg = score.k < 0.f;
-  // q carries the sign of the scale, so that the largest raw product is the
-  // largest score; a scale of 0 becomes so small that scores vanish but a
-  // masked -inf stays
-  score.k = fmaxf(fabsf(score.k), 1e-37f);
+  // q carries the sign of the scale, so that a masked -inf stays one
+  score.k = fabsf(score.k);
   const Row rw = row_at(a, qrow);
   bf16x8 qf[D / 16];
 #pragma unroll
@@ -371,12 +393,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
 
   int it = 0;
   for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
-    uint16_t* Ks = buf + (it & 1) * 2 * TILE;
-    uint16_t* Vs = Ks + TILE;
+    const int stage = (it & 1) * 4 * TILE;  // bytes
+    uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     // this stage was last read two tiles ago, before the previous barrier
     if (bt.all_lo > k0 || bt.all_hi < k0 + KT) odd |= sv.clean();
     sk.store(Ks);
-    sv.store(Vs);
+    sv.store(Ks + TILE);
     __syncthreads();
     if (k0 + KT < bt.hi) {
       sk.next();
@@ -386,12 +408,13 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     }
 #pragma unroll
     for (int u = 0; u < 2 / SH; ++u) {
-      const int r0 = 32 * (SH * u + shr);  // the step's first key in the tile
-      const int kb = k0 + r0;
+      const int at = 64 * D * SH * u;  // of the step's rows, past the wave's first
+      const int r0 = 32 * (SH * u + shr), kb = k0 + r0;  // its first key
       if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
       f32x16 s = splat(0.f);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Ks, r0, kk, lane), qf[kk], s);
+      for (int kk = 0; kk < D / 16; ++kk) 
+        s = mma(rows32<D>(smem, rbase + stage, kk, at), qf[kk], s);
       const float far = (float)(rw.pos - kb - 8 * hl);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -433,7 +456,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-          acc[d] = mma(cols32<D>(Vs, r0 + 16 * ks, 32 * d, lane), p[ks], acc[d]);
+          acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks], acc[d]);
     }
   }
 
@@ -475,12 +498,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ int bad[2][KT];  // tile in which a key held a NaN or infinity
   __shared__ int odd_at[2], any_odd;
-  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
   int tile, h;
   block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
   const int kh = h / a.rep;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
+  const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int qrow = tile * RB + grp * 32 + n;
   MaskTile mt{0, 0, 0, 0};
   if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
@@ -523,15 +546,15 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
 
   int it = 0;
   for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
-    uint16_t* Ks = buf + (it & 1) * 2 * TILE;
-    uint16_t* Vs = Ks + TILE;
+    const int stage = (it & 1) * 4 * TILE;
+    uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     const bool partly = bt.all_lo > k0 || bt.all_hi < k0 + KT;
     if (partly && sk.clean(bad[it & 1], it)) {
       odd_at[it & 1] = it;
       any_odd = 1;
     }
     sk.store(Ks);
-    sv.store(Vs);
+    sv.store(Ks + TILE);
     __syncthreads();
     if (k0 + KT < bt.hi) {
       sk.next();
@@ -541,20 +564,22 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     }
 #pragma unroll
     for (int u = 0; u < 2 / SH; ++u) {
-      const int r0 = 32 * (SH * u + shr);
-      const int kb = k0 + r0;
+      const int at = 64 * D * SH * u;
+      const int r0 = 32 * (SH * u + shr), kb = k0 + r0;
       if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
-      f32x16 s = splat(0.f), dp = splat(0.f);
+      f32x16 s = splat(0.f), dp = splat(-Dq);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Ks, r0, kk, lane), qf[kk], s);
+      for (int kk = 0; kk < D / 16; ++kk) 
+        s = mma(rows32<D>(smem, rbase + stage, kk, at), qf[kk], s);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) dp = mma(rows32<D>(Vs, r0, kk, lane), df[kk], dp);
+      for (int kk = 0; kk < D / 16; ++kk) 
+        dp = mma(rows32<D>(smem, rbase + stage, kk, at + 2 * TILE), df[kk], dp);
       const float far = (float)(rw.pos - kb - 8 * hl);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float dz;
         const float p = ex2(score(s[i], l2, far - (float)elem(i), dz));
-        s[i] = p * (dp[i] - Dq);
+        s[i] = p * dp[i];
         if (CAP) s[i] *= dz;
       }
       if (mt.all_lo > kb || mt.all_hi < kb + 32) {
@@ -577,7 +602,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-          acc[d] = mma(cols32<D>(Ks, r0 + 16 * ks, 32 * d, lane), ds[ks], acc[d]);
+          acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks), ds[ks], acc[d]);
     }
   }
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
@@ -629,29 +654,33 @@ struct Hits {
 // backward over keys: dk = ds^T q, dv = p^T do, the query rows of every head
 // of the group that attend any of the block's keys streaming by
 // ---------------------------------------------------------------------------
-template <int D, int G, int WPE, bool CAP, bool BIAS>
+template <int D, int G, int WPE, bool CAP, bool BIAS, bool DK, bool DV>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
+  constexpr bool RAW = !CAP && !BIAS;  // scores are k times the product
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT];
   __shared__ __attribute__((aligned(16))) int Lo[2][KT], Len[2][KT], Pos[2][KT];
   __shared__ int any_odd;
-  uint16_t* buf = reinterpret_cast<uint16_t*>(smem);
   int tile, kh;
   block_of((a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh);
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
+  const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int kb0 = tile * RB + grp * 32, key = kb0 + n;
   if (tid() == 0) any_odd = 0;
   bf16x8 kf[D / 16], vf[D / 16];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
     kf[kk] = row_frag(a.k + key * a.kt + kh * a.kh, 2 * kk + hl, key < a.Tk, a.hd8);
-    vf[kk] = row_frag(a.v + key * a.vt + kh * a.vh, 2 * kk + hl, key < a.Tk, a.hd8);
+    if (DK) vf[kk] = row_frag(a.v + key * a.vt + kh * a.vh, 2 * kk + hl, key < a.Tk, a.hd8);
   }
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = splat(0.f);
+  for (int d = 0; d < D / 32; ++d) {
+    if (DK) dk[d] = splat(0.f);
+    if (DV) dv[d] = splat(0.f);
+  }
   Stage<D> sq, sd;
   sq.init(a.q, 0, a.qt);
   sd.init(a.dout, 0, a.dot);
@@ -683,8 +712,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   int qt = hits.next(a, lane);
   if (qt >= 0) fetch(h, qt);
   for (int it = 0; qt >= 0; ++it) {
-    uint16_t* Qs = buf + (it & 1) * 2 * TILE;
-    uint16_t* Os = Qs + TILE;
+    const int stage = (it & 1) * 4 * TILE;
+    uint16_t* Qs = reinterpret_cast<uint16_t*>(smem + stage);
     const Score<CAP, BIAS> score(a, h);
     const MaskTile mt = a.tiles[qt];
     if (mt.all_lo > hits.k0 || mt.all_hi < hits.k1) {
@@ -692,10 +721,11 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       if (sd.clean()) any_odd = 1;
     }
     sq.store(Qs);
-    sd.store(Os);
+    sd.store(Qs + TILE);
     if (tid() < KT) {
-      Ls[it & 1][tid()] = finite_or_nan(ln) * LOG2E;
-      Ds[it & 1][tid()] = finite_or_nan(dn);
+      const float l2 = finite_or_nan(ln) * LOG2E;
+      Ls[it & 1][tid()] = RAW ? -l2 * a.inv_c1 : l2;
+      Ds[it & 1][tid()] = -finite_or_nan(dn);
       Lo[it & 1][tid()] = rn.lo;
       Len[it & 1][tid()] = rn.hi - rn.lo;
       Pos[it & 1][tid()] = rn.pos;
@@ -710,51 +740,76 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     if (qn >= 0) fetch(h, qn);
 #pragma unroll
     for (int u = 0; u < 2 / SH; ++u) {
-      const int r0 = 32 * (SH * u + shr);  // the step's first row in the tile
-      const int rb = r0 + 8 * hl;
+      const int at = 64 * D * SH * u;
+      const int rb = 32 * (SH * u + shr) + 8 * hl;  // the lane's first row in the tile
       if (kb0 >= mt.hi || kb0 + 32 <= mt.lo) continue;
-      f32x16 s = splat(0.f), dp = splat(0.f);
+      // -lse / k and -D start the sums, so that p = 2^(k s) and ds = p dp
+      const float* Lr = Ls[it & 1] + rb;
+      const float* Dr = Ds[it & 1] + rb;
+      f32x16 s;
+      const bool part = mt.all_lo > kb0 || mt.all_hi < kb0 + 32;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) s = mma(rows32<D>(Qs, r0, kk, lane), kf[kk], s);
+      for (int i = 0; i < 16; ++i) s[i] = RAW ? Lr[elem(i)] : 0.f;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) dp = mma(rows32<D>(Os, r0, kk, lane), vf[kk], dp);
+      for (int kk = 0; kk < D / 16; ++kk) 
+        s = mma(rows32<D>(smem, rbase + stage, kk, at), kf[kk], s);
+      bf16x8 p[2], ds[2];
+      float dz[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = rb + elem(i);
-        float dz;
-        const float far = BIAS ? (float)(Pos[it & 1][r] - key) : 0.f;
-        const float p = ex2(score(s[i], Ls[it & 1][r], far, dz));
-        dp[i] = p * (dp[i] - Ds[it & 1][r]);
-        if (CAP) dp[i] *= dz;
-        s[i] = p;
-      }
-      if (mt.all_lo > kb0 || mt.all_hi < kb0 + 32) {
+      for (int i = 0; i < 16; ++i)
+        s[i] = RAW ? ex2(s[i] * score.k)
+                   : ex2(score(s[i], Lr[elem(i)],
+                               BIAS ? (float)(Pos[it & 1][rb + elem(i)] - key) : 0.f, dz[i]));
+      if (part) {
+        // -0 marks what is not attended
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int r = rb + elem(i);
-          if ((uint32_t)(key - Lo[it & 1][r]) >= (uint32_t)Len[it & 1][r]) s[i] = dp[i] = 0.f;
+          if ((uint32_t)(key - Lo[it & 1][r]) >= (uint32_t)Len[it & 1][r]) s[i] = -0.f;
         }
       }
-      bf16x8 p[2], ds[2];
+      if (DV) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i / 8][i % 8] = (__bf16)s[i];
-        ds[i / 8][i % 8] = (__bf16)dp[i];
+        for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = (__bf16)s[i];
+      }
+      if (DK) {
+        f32x16 dp;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dp[i] = Dr[elem(i)];
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          dp = mma(rows32<D>(smem, rbase + stage, kk, at + 2 * TILE), vf[kk], dp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          dp[i] *= s[i];
+          if (CAP) dp[i] *= dz[i];
+        }
+        if (part) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (__float_as_uint(s[i]) == 0x80000000u) dp[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i / 8][i % 8] = (__bf16)dp[i];
       }
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          dv[d] = mma(cols32<D>(Os, r0 + 16 * ks, 32 * d, lane), p[ks], dv[d]);
-          dk[d] = mma(cols32<D>(Qs, r0 + 16 * ks, 32 * d, lane), ds[ks], dk[d]);
+          if (DV)
+            dv[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks], dv[d]);
+          if (DK)
+            dk[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks), ds[ks], dk[d]);
         }
     }
     qt = qn;
   }
   float* mb = reinterpret_cast<float*>(smem);
-  write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt, tile * RB, a.Tk, a.hd8,
+  if constexpr (DK)
+    write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt, tile * RB, a.Tk, a.hd8,
                    [](int, int, float (&)[8]) {});
-  write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt, tile * RB, a.Tk, a.hd8,
+  if constexpr (DV)
+    write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt, tile * RB, a.Tk, a.hd8,
                    [&](int j, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      for (int i = 0; i < a.Tq; ++i) {
@@ -773,6 +828,9 @@ Dev view(const MattnArgs& a) {
   d.scale = a.scale;
   d.c1 = a.cap > 0.f ? a.scale / a.cap : a.scale * LOG2E;
   d.c2 = a.cap * LOG2E;
+  // a scale of 0 becomes so small that scores vanish but a masked -inf stays
+  if (fabsf(d.c1) < 1e-30f) d.c1 = 1e-30f;
+  d.inv_c1 = 1.f / d.c1;
   const auto in = [](const pulse_heads& x) { return static_cast<const uint16_t*>(x.ptr); };
   const auto out = [](const pulse_heads& x) { return static_cast<uint16_t*>(x.ptr); };
   d.q = in(a.q), d.k = in(a.k), d.v = in(a.v), d.dout = in(a.dout), d.o_in = in(a.o);
@@ -805,8 +863,14 @@ hipError_t launch(const Dev& d, hipStream_t st) {
     hipLaunchKernelGGL((k_mattn_fwd<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
   else if constexpr (P == BWD_Q)
     hipLaunchKernelGGL((k_mattn_bwd_q<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
-  else
-    hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
+  else if constexpr (D == 64)
+    hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS, true, true>), grid, block, 0, st, d);
+  else {
+    hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS, false, true>), grid, block, 0, st, d);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS, true, false>), grid, block, 0, st, d);
+  }
   return hipGetLastError();
 }
 
@@ -822,7 +886,7 @@ hipError_t launch_mode(const Dev& d, hipStream_t st) {
 // Rows per block.
 template <Pass P, int D>
 hipError_t launch_rows(const Dev& d, hipStream_t st) {
-  constexpr int W = P == BWD_KV ? (D == 128 ? 1 : 2) : D == 64 ? 3 : 2;
+  constexpr int W = P == BWD_KV ? 2 : D == 64 ? 3 : 2;
   const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
   if ((long)((rows + 127) / 128) * heads >= 512) return launch_mode<P, D, 4, W>(d, st);
   return launch_mode<P, D, 2, W>(d, st);
