@@ -59,6 +59,12 @@ struct Dev {  // device view of MattnArgs
   const float* slopes;
   float* lse;
   float* dsum;
+  // Work split further than rows and heads: `parts` blocks share a tile, each
+  // with a range of the other side (or some of the group's heads) and fp32
+  // results of its own, [parts][rows][heads][8 hd8], which a second kernel
+  // adds up.
+  int parts, head_parts;  // head_parts of them by the group's heads (dk, dv)
+  float *part0, *part1, *part_lse;
 };
 
 // The builtins, since the library functions behind threadIdx are built for
@@ -294,26 +300,37 @@ __device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
 // tensors are fetched into one L2.  Tiles run from the last, which under a
 // causal mask has the most keys (first from the first, for the kernel over
 // keys).
-__device__ __forceinline__ void block_of(int tiles, int heads, bool last, int& tile, int& head) {
-  const int nb = tiles * heads, bid = __builtin_amdgcn_workgroup_id_x();
+__device__ __forceinline__ void block_of(const Dev& a, int tiles, int heads, bool last, int& tile,
+                                         int& head, int& part) {
+  const int nb = tiles * heads * a.parts, bid = __builtin_amdgcn_workgroup_id_x();
   const int q = nb >> 3, r = nb & 7, x = bid & 7;
   const int lb = x * q + (x < r ? x : r) + (bid >> 3);
-  head = lb / tiles;
-  tile = lb - head * tiles;
+  const int hp = lb / tiles;
+  tile = lb - hp * tiles;
   if (last) tile = tiles - 1 - tile;
+  head = hp / a.parts;
+  part = hp - head * a.parts;
+}
+
+// this part's share of keys [lo, hi), whole tiles
+__device__ __forceinline__ void share(const Dev& a, int part, int& lo, int& hi) {
+  if (a.parts == 1 || hi <= lo) return;
+  const int n = ((hi - lo + a.parts - 1) / a.parts + KT - 1) / KT * KT;
+  lo += part * n;
+  hi = min(hi, lo + n);
 }
 
 constexpr int MP = 36;                      // row pitch of a merge buffer (floats)
 constexpr int MERGE = 4 * 32 * MP * 4;      // its bytes
 
 // Write the waves' column accumulators [channels][32 columns], times f, to
-// rows row0 + .. of out: 32 channels at a time meet in LDS, where the shares
-// of a group are added in order.  fix(row, chunk, o) may change 8 channels
-// before they are rounded.
+// rows row0 + .. of out (or of the part's fp32 results): 32 channels at a time
+// meet in LDS, where the shares of a group are added in order.  fix(row,
+// chunk, o) may change 8 channels before they are rounded.
 template <int D, int G, typename F>
 __device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 32], float f,
-                                           uint16_t* out, long stride, int row0, int rows, int hd8,
-                                           F fix) {
+                                           uint16_t* out, long stride, float* part, int row0,
+                                           int rows, int heads, int hd8, F fix) {
   constexpr int SH = 4 / G;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
 #pragma unroll
@@ -336,10 +353,22 @@ __device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 3
       }
       if (row >= rows || 4 * d + c >= hd8) continue;
       fix(row, 4 * d + c, o);
+      if (part) {
+        float4* q = reinterpret_cast<float4*>(part + ((long)row * heads * hd8 + 4 * d + c) * 8);
+        q[0] = make_float4(o[0], o[1], o[2], o[3]);
+        q[1] = make_float4(o[4], o[5], o[6], o[7]);
+        continue;
+      }
       *reinterpret_cast<uint4*>(out + row * stride + 32 * d + 8 * c) =
           uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
     }
   }
+}
+
+// the part's fp32 results of a head, or null where there is one part
+__device__ __forceinline__ float* part_of(const Dev& a, float* p, int part, int rows, int heads,
+                                          int head) {
+  return a.parts > 1 ? p + (((long)part * rows) * heads + head) * a.hd8 * 8 : nullptr;
 }
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
@@ -356,8 +385,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ float ml[4][2][32];
   __shared__ int any_odd;
-  int tile, h;
-  block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
+  int tile, h, part;
+  block_of(a, (a.Tq + RB - 1) / RB, a.H, true, tile, h, part);
   const int kh = h / a.rep;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
@@ -366,13 +395,15 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   MaskTile mt{0, 0, 0, 0};  // of the tile that holds the wave's rows
   if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
   const MaskTile bt = tiles_at(a, tile * RB, RB);
+  int klo = bt.lo, khi = bt.hi;
+  share(a, part, klo, khi);
   const uint16_t* vbase = a.v + kh * a.vh;
   Stage<D> sk, sv;
-  sk.init(a.k + kh * a.kh, bt.lo, a.kt);
-  sv.init(vbase, bt.lo, a.vt);
-  if (bt.lo < bt.hi) {
-    sk.load(a.Tk - bt.lo, a.hd8);
-    sv.load(a.Tk - bt.lo, a.hd8);
+  sk.init(a.k + kh * a.kh, klo, a.kt);
+  sv.init(vbase, klo, a.vt);
+  if (klo < khi) {
+    sk.load(a.Tk - klo, a.hd8);
+    sv.load(a.Tk - klo, a.hd8);
   }
   Score<CAP, BIAS> score(a, h);
   const bool neg = score.k < 0.f;
@@ -392,7 +423,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   bool odd = false;  // this thread has left values out
 
   int it = 0;
-  for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
+  for (int k0 = klo; k0 < khi; k0 += KT, ++it) {
     const int stage = (it & 1) * 4 * TILE;  // bytes
     uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     // this stage was last read two tiles ago, before the previous barrier
@@ -400,36 +431,48 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     sk.store(Ks);
     sv.store(Ks + TILE);
     __syncthreads();
-    if (k0 + KT < bt.hi) {
+    if (k0 + KT < khi) {
       sk.next();
       sv.next();
       sk.load(a.Tk - k0 - KT, a.hd8);
       sv.load(a.Tk - k0 - KT, a.hd8);
     }
+    // 32-key steps, NU of them taken together
+    constexpr int NU = D == 128 ? 2 / SH : 1;
 #pragma unroll
-    for (int u = 0; u < 2 / SH; ++u) {
-      const int at = 64 * D * SH * u;  // of the step's rows, past the wave's first
-      const int r0 = 32 * (SH * u + shr), kb = k0 + r0;  // its first key
-      if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
-      f32x16 s = splat(0.f);
+    for (int y = 0; y < 2 / SH / NU; ++y) {
+      const int kb = k0 + 32 * (shr + SH * y);  // the first key
+      const int at = 64 * D * SH * y;
+      if (kb >= mt.hi || kb + 32 * NU <= mt.lo) continue;
+      f32x16 s[NU];
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) 
-        s = mma(rows32<D>(smem, rbase + stage, kk, at), qf[kk], s);
+      for (int u = 0; u < NU; ++u) {
+        s[u] = splat(0.f);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          s[u] = mma(rows32<D>(smem, rbase + stage, kk, at + 64 * D * u), qf[kk], s[u]);
+      }
       const float far = (float)(rw.pos - kb - 8 * hl);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float dz;
-        s[i] = score(s[i], ref, far - (float)elem(i), dz);
-      }
-      if (mt.all_lo > kb || mt.all_hi < kb + 32) {
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float dz;
+          s[u][i] = score(s[u][i], ref, far - (float)(32 * u + elem(i)), dz);
+        }
+      if (mt.all_lo > kb || mt.all_hi < kb + 32 * NU) {
         const uint32_t off = kb + 8 * hl - rw.lo, len = rw.hi - rw.lo;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (off + elem(i) >= len) s[i] = -INFINITY;
-      }
-      float mx = s[0];
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+          for (int i = 0; i < 16; ++i)
+            if (off + 32 * u + elem(i) >= len) s[u][i] = -INFINITY;
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
       if (__any(mx > (l == 0.f ? LOWEST : GROW))) {
         // relative to the old reference; the first may lie below it
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -439,24 +482,30 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
         ref += up;
         l *= al;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] -= up;
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] -= up;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[d][i] *= al;
       }
-      bf16x8 p[2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = ex2(s[i]);
-        l += e;
-        p[i / 8][i % 8] = (__bf16)e;
+      for (int u = 0; u < NU; ++u) {
+        bf16x8 p[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = ex2(s[u][i]);
+          l += e;
+          p[i / 8][i % 8] = (__bf16)e;
+        }
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
+            acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 64 * D * u + 32 * D * ks + 2 * TILE),
+                         p[ks], acc[d]);
       }
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-          acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks], acc[d]);
     }
   }
 
@@ -476,15 +525,23 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
 #pragma unroll
   for (int i = 0; i < SH; ++i) t += ml[grp * SH + i][1][n] * ex2(ml[grp * SH + i][0][n] - R);
   const bool empty = rw.hi <= rw.lo;
-  if (shr == 0 && hl == 0 && qrow < a.Tq)
-    a.lse[(long)h * a.Tq + qrow] = empty ? -INFINITY : (R + __builtin_amdgcn_logf(t)) * LN2;
+  float* po = part_of(a, a.part0, part, a.Tq, a.H, h);
+  // a part in which the row attends nothing has no weight
+  const bool none = empty || (po && t == 0.f);
+  if (shr == 0 && hl == 0 && qrow < a.Tq) {
+    const float e = none ? -INFINITY : R + __builtin_amdgcn_logf(t);
+    if (po)
+      a.part_lse[((long)part * a.H + h) * a.Tq + qrow] = e;
+    else
+      a.lse[(long)h * a.Tq + qrow] = e * LN2;
+  }
   // an empty row's accumulators are 0
-  write_rows<D, G>(reinterpret_cast<float*>(smem), acc, empty ? 0.f : ex2(ref - R) / t,
-                   a.o + h * a.oh, a.ot, tile * RB, a.Tq, a.hd8,
+  write_rows<D, G>(reinterpret_cast<float*>(smem), acc, none ? 0.f : ex2(ref - R) / t,
+                   a.o + h * a.oh, a.ot, po, tile * RB, a.Tq, a.H, a.hd8,
                    [&](int row, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      const Row x = row_at(a, row);
-                     for (int j = x.lo; j < x.hi; ++j)
+                     for (int j = max(x.lo, klo); j < min(x.hi, khi); ++j)
                        add_odd(o, *reinterpret_cast<const uint4*>(vbase + j * a.vt + 8 * c), false);
                    });
 }
@@ -498,8 +555,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ int bad[2][KT];  // tile in which a key held a NaN or infinity
   __shared__ int odd_at[2], any_odd;
-  int tile, h;
-  block_of((a.Tq + RB - 1) / RB, a.H, true, tile, h);
+  int tile, h, part;
+  block_of(a, (a.Tq + RB - 1) / RB, a.H, true, tile, h, part);
   const int kh = h / a.rep;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
@@ -508,13 +565,15 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   MaskTile mt{0, 0, 0, 0};
   if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
   const MaskTile bt = tiles_at(a, tile * RB, RB);
+  int klo = bt.lo, khi = bt.hi;
+  share(a, part, klo, khi);
   const uint16_t* kbase = a.k + kh * a.kh;
   Stage<D> sk, sv;
-  sk.init(kbase, bt.lo, a.kt);
-  sv.init(a.v + kh * a.vh, bt.lo, a.vt);
-  if (bt.lo < bt.hi) {
-    sk.load(a.Tk - bt.lo, a.hd8);
-    sv.load(a.Tk - bt.lo, a.hd8);
+  sk.init(kbase, klo, a.kt);
+  sv.init(a.v + kh * a.vh, klo, a.vt);
+  if (klo < khi) {
+    sk.load(a.Tk - klo, a.hd8);
+    sv.load(a.Tk - klo, a.hd8);
   }
   if (tid() < 2 * KT) bad[tid() / KT][tid() % KT] = -1;
   if (tid() < 2) odd_at[tid()] = -1;
@@ -535,7 +594,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   Dq += __shfl_xor(Dq, 32, 64);
   float l2 = 0.f;
   if (in) {
-    if (shr == 0 && hl == 0) a.dsum[(long)h * a.Tq + qrow] = Dq;
+    if (part == 0 && shr == 0 && hl == 0) a.dsum[(long)h * a.Tq + qrow] = Dq;
     // of a row that attends something: no score of it makes a p then
     l2 = finite_or_nan(a.lse[(long)h * a.Tq + qrow]) * LOG2E;
   }
@@ -545,7 +604,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   __syncthreads();  // bad
 
   int it = 0;
-  for (int k0 = bt.lo; k0 < bt.hi; k0 += KT, ++it) {
+  for (int k0 = klo; k0 < khi; k0 += KT, ++it) {
     const int stage = (it & 1) * 4 * TILE;
     uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     const bool partly = bt.all_lo > k0 || bt.all_hi < k0 + KT;
@@ -556,7 +615,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     sk.store(Ks);
     sv.store(Ks + TILE);
     __syncthreads();
-    if (k0 + KT < bt.hi) {
+    if (k0 + KT < khi) {
       sk.next();
       sv.next();
       sk.load(a.Tk - k0 - KT, a.hd8);
@@ -606,7 +665,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     }
   }
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
-                   tile * RB, a.Tq, a.hd8, [&](int row, int c, float (&o)[8]) {
+                   part_of(a, a.part0, part, a.Tq, a.H, h), tile * RB, a.Tq, a.H, a.hd8, [&](int row, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      const Row x = row_at(a, row);
                      if (x.hi <= x.lo) return;
@@ -622,26 +681,26 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
 // [k0, k1).  Every wave of a block sees the same ones: a wave looks at 64
 // table entries at a time.
 struct Hits {
-  int base, k0, k1;
+  int base, k0, k1, first, end;  // of tiles [first, end)
   uint64_t bits;
   __device__ __forceinline__ void look(const Dev& a, int lane) {
     const int t = base + lane;
     bool hit = false;
-    if (t < mask_tiles(a.Tq)) {
+    if (t < end) {
       const MaskTile m = a.tiles[t];
       hit = m.lo < k1 && m.hi > k0;
     }
     bits = __ballot(hit);
   }
   __device__ __forceinline__ void start(const Dev& a, int lane) {
-    base = 0;
+    base = first;
     look(a, lane);
   }
   // the next tile, or -1
   __device__ __forceinline__ int next(const Dev& a, int lane) {
     while (bits == 0) {
       base += 64;
-      if (base >= mask_tiles(a.Tq)) return -1;
+      if (base >= end) return -1;
       look(a, lane);
     }
     const int t = base + __builtin_ctzll(bits);
@@ -662,8 +721,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT];
   __shared__ __attribute__((aligned(16))) int Lo[2][KT], Len[2][KT], Pos[2][KT];
   __shared__ int any_odd;
-  int tile, kh;
-  block_of((a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh);
+  int tile, kh, part;
+  block_of(a, (a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh, part);
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
   const int grp = w / SH, shr = w % SH;
   const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
@@ -687,6 +746,11 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   Hits hits;
   hits.k0 = tile * RB;
   hits.k1 = tile * RB + RB;
+  // the part's heads and tiles of rows
+  const int heads = a.rep / a.head_parts, row_parts = a.parts / a.head_parts;
+  const int h0 = kh * a.rep + part % a.head_parts * heads, rp = part / a.head_parts;
+  hits.first = (int)((long)mask_tiles(a.Tq) * rp / row_parts);
+  hits.end = (int)((long)mask_tiles(a.Tq) * (rp + 1) / row_parts);
   float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
   Row rn{0, 0, 0};
   __syncthreads();  // any_odd
@@ -707,7 +771,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       }
     }
   };
-  int h = kh * a.rep;
+  int h = h0;
   hits.start(a, lane);
   int qt = hits.next(a, lane);
   if (qt >= 0) fetch(h, qt);
@@ -732,7 +796,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     }
     __syncthreads();
     int qn = hits.next(a, lane);
-    if (qn < 0 && h + 1 < (kh + 1) * a.rep) {
+    if (qn < 0 && h + 1 < h0 + heads) {
       ++h;
       hits.start(a, lane);
       qn = hits.next(a, lane);
@@ -806,10 +870,14 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   }
   float* mb = reinterpret_cast<float*>(smem);
   if constexpr (DK)
-    write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt, tile * RB, a.Tk, a.hd8,
+    write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt,
+                     part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), tile * RB, a.Tk,
+                     a.H / a.rep, a.hd8,
                    [](int, int, float (&)[8]) {});
   if constexpr (DV)
-    write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt, tile * RB, a.Tk, a.hd8,
+    write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt,
+                     part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), tile * RB, a.Tk,
+                     a.H / a.rep, a.hd8,
                    [&](int j, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      for (int i = 0; i < a.Tq; ++i) {
@@ -847,23 +915,108 @@ Dev view(const MattnArgs& a) {
   d.tiles = reinterpret_cast<const MaskTile*>(d.rows + a.Tq);
   d.slopes = a.slopes;
   d.lse = a.lse;
-  d.dsum = static_cast<float*>(a.ws);
   return d;
 }
 
+// ---------------------------------------------------------------------------
+// joining the parts
+// ---------------------------------------------------------------------------
+
+// out = sum of the parts, in order (blockIdx.y: dq or dk; dv)
+__global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int heads, int hd8,
+                                                   const float* p0, const float* p1, uint16_t* o0,
+                                                   uint16_t* o1, long t0, long h0, long t1,
+                                                   long h1) {
+  const bool y = __builtin_amdgcn_workgroup_id_y();
+  const float* p = y ? p1 : p0;
+  uint16_t* out = y ? o1 : o0;
+  const long ts = y ? t1 : t0, hs = y ? h1 : h0;
+  const long n = rows * heads * hd8;
+  const long e = (long)__builtin_amdgcn_workgroup_id_x() * 256 + tid();
+  if (e >= n) return;
+  float o[8] = {};
+  for (int i = 0; i < parts; ++i) {
+    const float4* q = reinterpret_cast<const float4*>(p + (i * n + e) * 8);
+    const float4 a = q[0], b = q[1];
+    o[0] += a.x, o[1] += a.y, o[2] += a.z, o[3] += a.w;
+    o[4] += b.x, o[5] += b.y, o[6] += b.z, o[7] += b.w;
+  }
+  const long rh = e / hd8, row = rh / heads;
+  const int c = e - rh * hd8, h = rh - row * heads;
+  *reinterpret_cast<uint4*>(out + row * ts + h * hs + 8 * c) =
+      uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+}
+
+// o = sum o_p 2^(lse_p - lse), lse = log2 sum 2^lse_p over the forward's parts
+__global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
+  const long n = (long)a.Tq * a.H * a.hd8;
+  const long e = (long)__builtin_amdgcn_workgroup_id_x() * 256 + tid();
+  if (e >= n) return;
+  const long rh = e / a.hd8;
+  const int c = e - rh * a.hd8, row = rh / a.H, h = rh - (long)row * a.H;
+  const Row x = row_at(a, row);
+  const bool empty = x.hi <= x.lo;
+  const float* l = a.part_lse + (long)h * a.Tq + row;
+  const long lp = (long)a.H * a.Tq;
+  float R = l[0], t = 0.f, o[8] = {};
+  for (int i = 1; i < a.parts; ++i) R = fmaxf(R, l[i * lp]);
+  for (int i = 0; i < a.parts; ++i) {
+    const float w = ex2(l[i * lp] - R);
+    t += w;
+    if (w == 0.f) continue;  // what it has may be infinite
+    const float4* q = reinterpret_cast<const float4*>(a.part0 + (i * n + e) * 8);
+    const float4 u = q[0], v = q[1];
+    o[0] += w * u.x, o[1] += w * u.y, o[2] += w * u.z, o[3] += w * u.w;
+    o[4] += w * v.x, o[5] += w * v.y, o[6] += w * v.z, o[7] += w * v.w;
+  }
+  const float f = 1.f / t;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = empty ? 0.f : o[i] * f;
+  *reinterpret_cast<uint4*>(a.o + row * a.ot + h * a.oh + 8 * c) =
+      uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+  if (c == 0)
+    a.lse[(long)h * a.Tq + row] = empty ? -INFINITY : (R + __builtin_amdgcn_logf(t)) * LN2;
+}
+
 enum Pass { FWD, BWD_Q, BWD_KV };
+
+struct Plan {
+  int group;              // groups of 32 rows per block
+  int parts, head_parts;  // as in Dev
+};
+
+// How a pass is spread over the GPU (256 CUs, two or three blocks each).
+Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
+  const int rows = p == BWD_KV ? Tk : Tq, heads = p == BWD_KV ? KV : H;
+  const int other = p == BWD_KV ? Tq : Tk;
+  Plan x{4, 1, 1};
+  long blocks = (long)((rows + 127) / 128) * heads;
+  if (p == BWD_KV && blocks < 1024 && H > KV) {
+    x.parts = x.head_parts = H / KV;
+    blocks *= x.parts;
+  }
+  if (blocks < 512) {
+    x.group = 2;
+    blocks = (long)((rows + 63) / 64) * heads * x.parts;
+  }
+  if (blocks > 0 && blocks < 256) {
+    const long most = other / 512, want = 512 / blocks;
+    const long n = want < most ? want : most;
+    if (n > 1) x.parts *= (int)(n < 16 ? n : 16);
+  }
+  return x;
+}
 
 template <Pass P, int D, int G, int WPE, bool CAP, bool BIAS>
 hipError_t launch(const Dev& d, hipStream_t st) {
   constexpr int RB = 32 * G;
   const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
-  if (rows == 0) return hipSuccess;
-  const dim3 grid((rows + RB - 1) / RB * heads), block(256);
+  const dim3 grid((long)((rows + RB - 1) / RB) * heads * d.parts), block(256);
   if constexpr (P == FWD)
     hipLaunchKernelGGL((k_mattn_fwd<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
   else if constexpr (P == BWD_Q)
     hipLaunchKernelGGL((k_mattn_bwd_q<D, G, WPE, CAP, BIAS>), grid, block, 0, st, d);
-  else if constexpr (D == 64)
+  else if constexpr (D < 128)
     hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS, true, true>), grid, block, 0, st, d);
   else {
     hipLaunchKernelGGL((k_mattn_bwd_kv<D, G, WPE, CAP, BIAS, false, true>), grid, block, 0, st, d);
@@ -883,37 +1036,88 @@ hipError_t launch_mode(const Dev& d, hipStream_t st) {
   return launch<P, D, G, WPE, false, false>(d, st);
 }
 
-// Rows per block.
 template <Pass P, int D>
-hipError_t launch_rows(const Dev& d, hipStream_t st) {
+hipError_t launch_rows(const Dev& d, int group, hipStream_t st) {
   constexpr int W = P == BWD_KV ? 2 : D == 64 ? 3 : 2;
-  const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
-  if ((long)((rows + 127) / 128) * heads >= 512) return launch_mode<P, D, 4, W>(d, st);
-  return launch_mode<P, D, 2, W>(d, st);
+  return group == 4 ? launch_mode<P, D, 4, W>(d, st) : launch_mode<P, D, 2, W>(d, st);
 }
 
 template <Pass P>
-hipError_t launch_dim(const Dev& d, hipStream_t st) {
-  if (d.hd8 <= 8) return launch_rows<P, 64>(d, st);
-  if (d.hd8 <= 12) return launch_rows<P, 96>(d, st);
-  return launch_rows<P, 128>(d, st);
+hipError_t launch_dim(const Dev& d, int group, hipStream_t st) {
+  if (d.hd8 <= 8) return launch_rows<P, 64>(d, group, st);
+  if (d.hd8 <= 12) return launch_rows<P, 96>(d, group, st);
+  return launch_rows<P, 128>(d, group, st);
+}
+
+size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace of a pass: D of every row (backward), then the parts' results.
+struct Space {
+  size_t dsum, part0, part1, lse, bytes;
+};
+Space space(Pass p, const Plan& x, int Tq, int Tk, int H, int KV, int hd) {
+  Space s{};
+  size_t at = p == FWD ? 0 : al256((size_t)H * Tq * 4);
+  if (x.parts > 1) {
+    const size_t one = al256((size_t)x.parts * (p == BWD_KV ? (size_t)Tk * KV : (size_t)Tq * H) *
+                             hd * 4);
+    s.part0 = at;
+    at += one;
+    if (p == BWD_KV) s.part1 = at, at += one;
+    if (p == FWD) s.lse = at, at += al256((size_t)x.parts * H * Tq * 4);
+  }
+  s.bytes = at;
+  return s;
+}
+
+template <Pass P>
+hipError_t run(const MattnArgs& a, hipStream_t st) {
+  const int rows = P == BWD_KV ? a.Tk : a.Tq, heads = P == BWD_KV ? a.KV : a.H;
+  if (rows == 0) return hipSuccess;
+  const Plan x = plan(P, a.Tq, a.Tk, a.H, a.KV);
+  const Space s = space(P, x, a.Tq, a.Tk, a.H, a.KV, a.hd);
+  char* ws = static_cast<char*>(a.ws);
+  Dev d = view(a);
+  d.parts = x.parts, d.head_parts = x.head_parts;
+  d.dsum = reinterpret_cast<float*>(ws);
+  d.part0 = reinterpret_cast<float*>(ws + s.part0);
+  d.part1 = reinterpret_cast<float*>(ws + s.part1);
+  d.part_lse = reinterpret_cast<float*>(ws + s.lse);
+  const hipError_t e = launch_dim<P>(d, x.group, st);
+  if (e != hipSuccess || x.parts == 1) return e;
+  const long n = (long)rows * heads * d.hd8;
+  const dim3 grid((n + 255) / 256, P == BWD_KV ? 2 : 1);
+  if (P == FWD)
+    hipLaunchKernelGGL(k_mattn_join, grid, dim3(256), 0, st, d);
+  else if (P == BWD_Q)
+    hipLaunchKernelGGL(k_mattn_sum, grid, dim3(256), 0, st, x.parts, (long)rows, heads, d.hd8,
+                       d.part0, d.part0, d.dq, d.dq, d.dqt, d.dqh, d.dqt, d.dqh);
+  else
+    hipLaunchKernelGGL(k_mattn_sum, grid, dim3(256), 0, st, x.parts, (long)rows, heads, d.hd8,
+                       d.part0, d.part1, d.dk, d.dv, d.dkt, d.dkh, d.dvt, d.dvh);
+  return hipGetLastError();
+}
+
+template <Pass P>
+size_t bytes(const pulse_attn_desc& d) {
+  return space(P, plan(P, d.queries, d.keys, d.heads, d.kv_heads), d.queries, d.keys, d.heads,
+               d.kv_heads, d.head_dim)
+      .bytes;
 }
 
 }  // namespace
 
-size_t mattn_fwd_bytes(const pulse_attn_desc&) { return 0; }
+size_t mattn_fwd_bytes(const pulse_attn_desc& d) { return bytes<FWD>(d); }
 size_t mattn_bwd_bytes(const pulse_attn_desc& d) {
-  return (size_t)d.heads * d.queries * sizeof(float);
+  const size_t q = bytes<BWD_Q>(d), kv = bytes<BWD_KV>(d);
+  return q > kv ? q : kv;  // one after the other
 }
 
-hipError_t launch_mattn_fwd(const MattnArgs& a, hipStream_t st) {
-  return launch_dim<FWD>(view(a), st);
-}
+hipError_t launch_mattn_fwd(const MattnArgs& a, hipStream_t st) { return run<FWD>(a, st); }
 
 hipError_t launch_mattn_bwd(const MattnArgs& a, hipStream_t st) {
-  const Dev d = view(a);
-  const hipError_t e = launch_dim<BWD_Q>(d, st);
-  return e == hipSuccess ? launch_dim<BWD_KV>(d, st) : e;
+  const hipError_t e = run<BWD_Q>(a, st);
+  return e == hipSuccess ? run<BWD_KV>(a, st) : e;
 }
 
 }  // namespace pulse

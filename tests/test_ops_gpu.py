@@ -272,6 +272,7 @@ def _case(lens, pad, heads, kv, dim, kind, seed, key_lens=None):
     g = _gen(seed)
     tq = sum(lens) + pad
     tk = sum(key_lens) if key_lens else tq
+    key_lens = key_lens[:len(lens)] if key_lens else None  # the rest is of no document
     q, do = (_randn(g, tq, heads, dim).to(BF) for _ in range(2))
     k, v = (_randn(g, tk, kv, dim).to(BF) for _ in range(2))
     prefix = [n // 3 for n in (key_lens or lens)]
@@ -320,6 +321,37 @@ def test_attn_other_keys_and_shared_heads(heads, kv, lens, key_lens, kind):
     plan = ops.Attn(sum(lens), heads, 72, keys=sum(key_lens), kv_heads=kv)
     ref = _attn_ref(q, k, v, do, rows, 1 / math.sqrt(72), 0.0, None)
     _attn_check(_attn_run(plan, mask, q, k, v, do), ref, f"{lens} over {key_lens}")
+
+
+@pytest.mark.parametrize("lens,key_lens,kind,cap", [
+    ([1], [5000], "causal", 0.0), ([3, 1], [2500, 2601], "doc", 9.0), ([70], [4096], "prefix", 0.0),
+    ([2600], [33], "doc", 0.0), ([1500, 1200], [1, 130], "causal", 0.0), ([40], [3, ], "causal", 0.0),
+    ([1] * 5, [1, 3000, 64, 0, 999], "doc", 0.0),
+])
+def test_attn_few_rows_over_a_long_axis(lens, key_lens, kind, cap):
+    """Few blocks: the other side is split and the parts are joined."""
+    log(f"case attention {lens} over {key_lens} {kind} in parts")
+    for heads, kv, dim in ((2, 1, 64), (3, 3, 88), (1, 1, 128)):
+        q, k, v, do, mask, rows = _case(lens, 2, heads, kv, dim, kind, dim, key_lens + [7])
+        slopes = torch.tensor([0.01, 0.02, 0.0])[:heads] if cap else None
+        plan = ops.Attn(len(rows), heads, dim, keys=sum(key_lens) + 7, kv_heads=kv, cap=cap)
+        ref = _attn_ref(q, k, v, do, rows, 1 / math.sqrt(dim), cap, slopes)
+        _attn_check(_attn_run(plan, mask, q, k, v, do, slopes), ref, f"{lens} over {key_lens}")
+
+
+def test_attn_nan_in_one_part():
+    """A value that is not finite in a long axis stays with what attends it."""
+    q, k, v, do, mask, rows = _case([40, 9], 1, 2, 1, 64, "causal", 21, [3000, 1500])
+    plan = ops.Attn(50, 2, 64, keys=4500, kv_heads=1)
+    v[2990, 0, 5] = math.inf  # of the rows placed there and later
+    v[3100] = math.nan        # of the second document
+    o, _ = plan.forward(q.cuda(), k.cuda(), v.cuda(), mask)
+    ref = _attn_ref(q, k, v, do, rows, 0.125, 0.0, None)["o"]
+    o = o.cpu().double()
+    assert torch.equal(torch.isnan(o), torch.isnan(ref))
+    assert torch.equal(torch.isinf(o), torch.isinf(ref))
+    ok = torch.isfinite(ref)
+    assert rel_l2(o[ok], ref[ok]) <= ATTN_TOL
 
 
 def test_attn_own_rows():
