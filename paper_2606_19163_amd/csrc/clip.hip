@@ -9,10 +9,53 @@
 namespace pulse {
 namespace {
 
-__device__ __forceinline__ float get(const float* p, int i) { return p[i]; }
-__device__ __forceinline__ float get(const uint16_t* p, int i) { return bf2f(p[i]); }
-__device__ __forceinline__ void set(float* p, int i, float v) { p[i] = v; }
-__device__ __forceinline__ void set(uint16_t* p, int i, float v) { p[i] = f2bf(v); }
+// 16 bytes as fp32 and back
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  __device__ static __forceinline__ void get(uint4 w, float* v) {
+    v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y);
+    v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+  }
+  __device__ static __forceinline__ uint4 put(const float* v) {
+    return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                 __float_as_uint(v[3])};
+  }
+  __device__ static __forceinline__ float one(float x) { return x; }
+  __device__ static __forceinline__ float back(float x) { return x; }
+};
+template <>
+struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  __device__ static __forceinline__ void get(uint4 w, float* v) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(x[i] << 16);
+      v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+    }
+  }
+  __device__ static __forceinline__ uint4 put(const float* v) {
+    return uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+  }
+  __device__ static __forceinline__ float one(uint16_t x) { return bf2f(x); }
+  __device__ static __forceinline__ uint16_t back(float x) { return f2bf(x); }
+};
+
+// A chunk is up to `head` elements before the first 16-byte boundary, whole
+// 16-byte words, and a tail.
+template <typename T>
+struct Cut {
+  int head, words;
+  __device__ __forceinline__ explicit Cut(const ClipChunk& c) {
+    const int off = (int)(reinterpret_cast<uintptr_t>(c.g) & 15) / (int)sizeof(T);
+    head = min(c.n, off ? Vec<T>::N - off : 0);
+    words = (c.n - head) / Vec<T>::N;
+  }
+  __device__ __forceinline__ int tail() const { return head + words * Vec<T>::N; }
+};
 
 // sum over the 256 threads, the same on every thread
 __device__ __forceinline__ double block_sum(double v) {
@@ -24,13 +67,35 @@ __device__ __forceinline__ double block_sum(double v) {
   return w[0] + w[1] + w[2] + w[3];
 }
 
+constexpr int UN = 4;  // words in flight per thread
+
 template <typename T>
 __device__ __forceinline__ double squares(const ClipChunk& c) {
   const T* g = static_cast<const T*>(c.g);
+  const Cut<T> k(c);
   double s = 0.;
-  for (int i = threadIdx.x; i < c.n; i += 256) {
-    const double v = get(g, i);
-    s = fma(v, v, s);
+  const auto add = [&](float x) { s = fma((double)x, (double)x, s); };
+  if ((int)threadIdx.x < k.head) add(Vec<T>::one(g[threadIdx.x]));
+  for (int i = k.tail() + threadIdx.x; i < c.n; i += 256) add(Vec<T>::one(g[i]));
+  const uint4* p = reinterpret_cast<const uint4*>(g + k.head);
+  int w = threadIdx.x;
+  for (; w + 256 * (UN - 1) < k.words; w += 256 * UN) {
+    uint4 q[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) q[u] = p[w + 256 * u];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      float v[Vec<T>::N];
+      Vec<T>::get(q[u], v);
+#pragma unroll
+      for (int i = 0; i < Vec<T>::N; ++i) add(v[i]);
+    }
+  }
+  for (; w < k.words; w += 256) {
+    float v[Vec<T>::N];
+    Vec<T>::get(p[w], v);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N; ++i) add(v[i]);
   }
   return s;
 }
@@ -39,7 +104,34 @@ template <typename T>
 __device__ __forceinline__ void scale(const ClipChunk& c, float f) {
   const T* g = static_cast<const T*>(c.g);
   T* o = static_cast<T*>(c.o);
-  for (int i = threadIdx.x; i < c.n; i += 256) set(o, i, get(g, i) * f);
+  const Cut<T> k(c);
+  if ((int)threadIdx.x < k.head) o[threadIdx.x] = Vec<T>::back(Vec<T>::one(g[threadIdx.x]) * f);
+  for (int i = k.tail() + threadIdx.x; i < c.n; i += 256) o[i] = Vec<T>::back(Vec<T>::one(g[i]) * f);
+  const uint4* p = reinterpret_cast<const uint4*>(g + k.head);
+  const auto turn = [&](uint4 w) {
+    float v[Vec<T>::N];
+    Vec<T>::get(w, v);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N; ++i) v[i] *= f;
+    return Vec<T>::put(v);
+  };
+  T* d = o + k.head;
+  if (reinterpret_cast<uintptr_t>(d) & 15) {
+    // the output is aligned otherwise: element by element
+    for (int i = threadIdx.x; i < k.words * Vec<T>::N; i += 256)
+      d[i] = Vec<T>::back(Vec<T>::one(g[k.head + i]) * f);
+    return;
+  }
+  uint4* q = reinterpret_cast<uint4*>(d);
+  int w = threadIdx.x;
+  for (; w + 256 * (UN - 1) < k.words; w += 256 * UN) {
+    uint4 x[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) x[u] = p[w + 256 * u];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) q[w + 256 * u] = turn(x[u]);
+  }
+  for (; w < k.words; w += 256) q[w] = turn(p[w]);
 }
 
 __global__ __launch_bounds__(256) void k_clip_sum(const ClipChunk* chunks, int count,
@@ -62,7 +154,8 @@ __global__ __launch_bounds__(256) void k_clip_scale(const ClipChunk* chunks, int
   if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
   const float r = max_norm / (n + eps);
   const float f = r > 1.f ? 1.f : r;  // NaN stays
-  for (int c = blockIdx.x; c < count; c += gridDim.x) {
+  // from the last chunk: what the sum read last is still in cache
+  for (int c = count - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
     const ClipChunk k = chunks[c];
     if (f == 1.f && k.g == k.o) continue;
     if (k.dtype == PULSE_BF16)
