@@ -19,6 +19,8 @@ from __future__ import annotations
 import ctypes
 import math
 
+import torch
+
 from .stage import BF16, F32, E_INVALID_ARG, PulseError, _check, lib as _lib
 
 __all__ = ["Rope", "Mask", "Attn", "GradClip", "rope_freqs", "grid_positions", "MaskRow"]
@@ -56,6 +58,10 @@ class AttnDesc(ctypes.Structure):
 class ClipTensor(ctypes.Structure):
     _fields_ = [("grad", _vp), ("out", _vp), ("n", _i64), ("dtype", ctypes.c_int)]
 
+
+# torch.cuda.current_stream() builds an object that only its handle is read from
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 _bound = None
 
@@ -102,7 +108,6 @@ def _bad(msg):
 
 
 def _dtype(dt):
-    import torch
     if dt == torch.bfloat16:
         return BF16
     if dt == torch.float32:
@@ -110,48 +115,45 @@ def _dtype(dt):
     _bad(f"dtype must be torch.bfloat16 or torch.float32, not {dt}")
 
 
-def _current(t):
-    """Kernels run on the current device: a tensor of another is refused."""
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        _bad(f"a tensor is on {t.device}, not on the current GPU")
-
-
-def _heads(t, name, shape, dtype):
-    if t.shape != shape or t.dtype != dtype:
+def _heads(t, name, shape, dtype, dev):
+    """The view [tokens, heads, dim] `t` of GPU `dev`, where the call runs."""
+    if t.dtype is not dtype or t.shape != shape:
         _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
     s0, s1, s2 = t.stride()
-    if s2 != 1 and t.shape[2] != 1:
+    if s2 != 1 and shape[2] != 1:
         _bad(f"{name}: the channels of a head must be contiguous")
-    _current(t)
+    if t.get_device() != dev:
+        _bad(f"{name} is on {t.device}, not on the current GPU")
     # the stride of an axis of one element is never used
     return Heads(t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0)
 
 
-def _flat(t, name, n, dtype):
+def _flat(t, name, n, dtype, dev):
     """Pointer of a contiguous tensor of n elements (None stays NULL)."""
     if t is None:
         return None
-    if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         _bad(f"{name} must be contiguous {dtype} with {n} elements, not {t.dtype} "
              f"{tuple(t.shape)}")
-    _current(t)
+    if t.get_device() != dev:
+        _bad(f"{name} is on {t.device}, not on the current GPU")
     return t.data_ptr()
 
 
 class _On:
-    """torch's current stream, or `stream` made current, so that allocations
-    belong to the stream the work runs on."""
+    """(device, stream handle) of torch's current stream, or of `stream` made
+    current, so that what a call allocates belongs to the stream it runs on."""
+
+    __slots__ = ("ctx",)
 
     def __init__(self, stream):
-        import torch
         self.ctx = None if stream is None else torch.cuda.stream(stream)
 
     def __enter__(self):
-        import torch
         if self.ctx is not None:
             self.ctx.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        dev = torch.cuda.current_device()
+        return dev, _raw_stream(dev)
 
     def __exit__(self, *exc):
         if self.ctx is not None:
@@ -161,7 +163,6 @@ class _On:
 def rope_freqs(axis_dim, base=10000.0, device="cuda"):
     """freq[p] = base^(-2 i / n) for pair i of an axis of n channels, the axes
     one after another (fp32)."""
-    import torch
     parts = [base ** (-torch.arange(0, n, 2, dtype=torch.float64) / max(n, 1)) for n in axis_dim]
     return torch.cat(parts).float().to(device)
 
@@ -169,7 +170,6 @@ def rope_freqs(axis_dim, base=10000.0, device="cuda"):
 def grid_positions(shapes, device="cuda"):
     """Positions [tokens, axes] of documents whose tokens are grids (time,
     height, width or any other number of axes) in row-major order."""
-    import torch
     out = [torch.cartesian_prod(*[torch.arange(n) for n in s]).reshape(-1, len(s)) for s in shapes]
     return torch.cat(out).float().to(device)
 
@@ -178,7 +178,6 @@ class Rope:
     """Rotary positions of ``heads`` heads; ``axis_dim``: channels per axis."""
 
     def __init__(self, heads, head_dim, axis_dim, pairs="adjacent", dtype=None):
-        import torch
         self.dtype = torch.bfloat16 if dtype is None else dtype
         if pairs not in _PAIRS:
             _bad(f"pairs must be one of {sorted(_PAIRS)}")
@@ -194,16 +193,16 @@ class Rope:
                                 ctypes.byref(none), None))
 
     def _run(self, x, pos, freq, out, backward, stream):
-        import torch
         n = x.shape[0]
         shape = (n, self.heads, self.dim)
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
             if out is None:
                 out = torch.empty(shape, dtype=self.dtype, device=x.device)
-            hx, hy = _heads(x, "x", shape, self.dtype), _heads(out, "out", shape, self.dtype)
+            hx = _heads(x, "x", shape, self.dtype, dev)
+            hy = _heads(out, "out", shape, self.dtype, dev)
             _check(lib().pulse_rope(
-                self.desc, n, backward, hx, _flat(pos, "pos", n * self.axes, torch.float32),
-                _flat(freq, "freq", self.half, torch.float32), hy, s))
+                self.desc, n, backward, hx, _flat(pos, "pos", n * self.axes, torch.float32, dev),
+                _flat(freq, "freq", self.half, torch.float32, dev), hy, s))
         return out
 
     def forward(self, x, pos, freq, out=None, stream=None):
@@ -219,7 +218,6 @@ class Mask:
     """Which of ``keys`` keys each of ``queries`` rows attends."""
 
     def __init__(self, queries, keys=None, docs=0, causal=False, device="cuda"):
-        import torch
         self.queries, self.keys = queries, queries if keys is None else keys
         self.docs = docs
         self.desc = MaskDesc(queries, self.keys, docs, 1 if causal else 0)
@@ -233,20 +231,22 @@ class Mask:
 
     def build(self, offsets, key_offsets=None, prefix=None, stream=None):
         """From int32 ``offsets`` [docs + 1] on the GPU; returns ``rows``."""
-        import torch
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
+            if self.buffer.get_device() != dev:
+                _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
             _check(lib().pulse_mask_build(
-                self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32),
-                _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32),
-                _flat(prefix, "prefix", self.docs, torch.int32), self.ptr, self.bytes, s))
+                self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
+                _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
+                _flat(prefix, "prefix", self.docs, torch.int32, dev), self.ptr, self.bytes, s))
         return self.rows
 
     def from_rows(self, rows, stream=None):
         """From the caller's int32 [queries, 4] (it may be ``self.rows``)."""
-        import torch
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
+            if self.buffer.get_device() != dev:
+                _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
             _check(lib().pulse_mask_from_rows(
-                self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32), self.ptr,
+                self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
                 self.bytes, s))
         return self.rows
 
@@ -265,16 +265,17 @@ class Attn:
         self.qs = (queries, heads, head_dim)
         self.ks = (self.keys, self.kv, head_dim)
 
-    def _mask(self, mask):
+    def _mask(self, mask, dev):
         if mask.queries != self.queries or mask.keys != self.keys:
             _bad(f"the mask is of {mask.queries} rows and {mask.keys} keys")
+        if mask.buffer.get_device() != dev:
+            _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
         return mask.ptr
 
     def forward(self, q, k, v, mask, slopes=None, out=None, lse=None, stream=None):
         """(o, lse): o [queries, heads, head_dim], lse [heads, queries] fp32."""
-        import torch
         bf = torch.bfloat16
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
             if out is None:
                 out = torch.empty(self.qs, dtype=bf, device=q.device)
             if lse is None:
@@ -283,18 +284,18 @@ class Attn:
             if self.fwd_bytes:
                 ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
             _check(lib().pulse_attn_forward(
-                self.desc, _heads(q, "q", self.qs, bf), _heads(k, "k", self.ks, bf),
-                _heads(v, "v", self.ks, bf), self._mask(mask),
-                _flat(slopes, "slopes", self.heads, torch.float32), _heads(out, "out", self.qs, bf),
-                _flat(lse, "lse", self.heads * self.queries, torch.float32),
+                self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
+                _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev),
+                _flat(slopes, "slopes", self.heads, torch.float32, dev),
+                _heads(out, "out", self.qs, bf, dev),
+                _flat(lse, "lse", self.heads * self.queries, torch.float32, dev),
                 ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
         return out, lse
 
     def backward(self, dout, q, k, v, o, lse, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
-        import torch
         bf = torch.bfloat16
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
             if out is None:
                 out = [torch.empty(n, dtype=bf, device=q.device)
                        for n in (self.qs, self.ks, self.ks)]
@@ -303,12 +304,13 @@ class Attn:
             if self.bwd_bytes:
                 ws = torch.empty(self.bwd_bytes, dtype=torch.uint8, device=q.device)
             _check(lib().pulse_attn_backward(
-                self.desc, _heads(dout, "dout", self.qs, bf), _heads(q, "q", self.qs, bf),
-                _heads(k, "k", self.ks, bf), _heads(v, "v", self.ks, bf),
-                _heads(o, "o", self.qs, bf),
-                _flat(lse, "lse", self.heads * self.queries, torch.float32), self._mask(mask),
-                _flat(slopes, "slopes", self.heads, torch.float32), _heads(dq, "dq", self.qs, bf),
-                _heads(dk, "dk", self.ks, bf), _heads(dv, "dv", self.ks, bf),
+                self.desc, _heads(dout, "dout", self.qs, bf, dev), _heads(q, "q", self.qs, bf, dev),
+                _heads(k, "k", self.ks, bf, dev), _heads(v, "v", self.ks, bf, dev),
+                _heads(o, "o", self.qs, bf, dev),
+                _flat(lse, "lse", self.heads * self.queries, torch.float32, dev),
+                self._mask(mask, dev), _flat(slopes, "slopes", self.heads, torch.float32, dev),
+                _heads(dq, "dq", self.qs, bf, dev),
+                _heads(dk, "dk", self.ks, bf, dev), _heads(dv, "dv", self.ks, bf, dev),
                 ws.data_ptr() if ws is not None else None, self.bwd_bytes, s))
         return dq, dk, dv
 
@@ -319,20 +321,22 @@ class GradClip:
     once, so they must stay where they are from step to step."""
 
     def __init__(self, grads, outs=None):
-        import torch
         self.h = _vp()
         grads = list(grads)
         outs = grads if outs is None else list(outs)
         if len(grads) != len(outs):
             _bad(f"{len(grads)} gradients and {len(outs)} outputs")
+        if not all(t.is_cuda for t in grads + outs):
+            _bad("a gradient or an output is not on a GPU")
+        dev = torch.cuda.current_device() if grads else -1
         arr = (ClipTensor * max(len(grads), 1))()
         for i, (g, o) in enumerate(zip(grads, outs)):
             if g.dtype != o.dtype or g.numel() != o.numel():
                 _bad(f"gradient {i} and its output differ in type or size")
             if not g.is_contiguous() or not o.is_contiguous():
                 _bad(f"gradient {i} or its output is not contiguous")
-            _current(g)
-            _current(o)
+            if g.get_device() != dev or o.get_device() != dev:
+                _bad(f"gradient {i} or its output is not on the current GPU")
             arr[i] = ClipTensor(g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g.dtype))
         self.grads, self.outs = grads, outs
         self.device = grads[0].device if grads else "cuda"
@@ -354,10 +358,9 @@ class GradClip:
     def run(self, max_norm, eps=1e-6, norm=None, stream=None):
         """Clip to ``max_norm``; returns the norm before it, fp32 [1].  Calls
         share one workspace: order the streams that they run on."""
-        import torch
-        with _On(stream) as s:
+        with _On(stream) as (dev, s):
             if norm is None:
                 norm = torch.empty(1, dtype=torch.float32, device=self.device)
             _check(lib().pulse_clip_run(self.h, max_norm, eps,
-                                        _flat(norm, "norm", 1, torch.float32), s))
+                                        _flat(norm, "norm", 1, torch.float32, dev), s))
         return norm

@@ -242,11 +242,11 @@ def test_binding_refuses_before_the_library():
     m = ops.Mask(10, docs=1, device="cpu")
     assert m.rows.shape == (10, 4)
     with pytest.raises(S.PulseError):  # not on a GPU
-        ops._heads(torch.zeros(4, 2, 64, dtype=torch.bfloat16), "x", (4, 2, 64), torch.bfloat16)
+        ops._heads(torch.zeros(4, 2, 64, dtype=torch.bfloat16), "x", (4, 2, 64), torch.bfloat16, 0)
     with pytest.raises(S.PulseError):
-        ops._heads(torch.zeros(4, 2, 64), "x", (4, 2, 64), torch.bfloat16)
+        ops._heads(torch.zeros(4, 2, 64), "x", (4, 2, 64), torch.bfloat16, 0)
     with pytest.raises(S.PulseError):
-        ops._flat(torch.zeros(4, 2).t(), "x", 8, torch.float32)
+        ops._flat(torch.zeros(4, 2).t(), "x", 8, torch.float32, 0)
     with pytest.raises(S.PulseError):
         ops.GradClip([torch.zeros(4)])
     with pytest.raises(S.PulseError):
