@@ -167,6 +167,17 @@ __device__ __forceinline__ bool clean8(uint4& w) {
   return odd;
 }
 
+// whether there are any: the largest magnitude, as integers
+__device__ __forceinline__ bool odd8(uint4 w) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+  return m[0] >= 0x7f80 || m[1] >= 0x7f80;
+}
+
 // o += those of 8 values that are NaN or infinite (a weight p > 0 leaves them
 // what they are); with `nan` they make it NaN
 __device__ __forceinline__ void add_odd(float (&o)[8], uint4 w, bool nan) {
@@ -237,6 +248,10 @@ struct Stage {
   __device__ __forceinline__ bool clean(int* bad = nullptr, int tag = 0) {
     bool any = false;
 #pragma unroll
+    for (int u = 0; u < N; ++u) any |= odd8(v[u]);
+    if (!__any(any)) return false;
+    any = false;
+#pragma unroll
     for (int u = 0; u < N; ++u) {
       const bool b = clean8(v[u]);
       any |= b;
@@ -245,6 +260,16 @@ struct Stage {
     return any;
   }
 };
+
+// Between an MFMA and the VALU work that it covers: the scheduler, left to
+// itself, puts every MFMA before the VALU work that does not depend on it.  LDS
+// reads and scalar work may pass.  Backward of 8 x 1024 tokens of 16 heads of
+// 88: 235 us without, 220 us with; at 64 channels, where three waves share a
+// SIMD, 1062 and 1091 us (8192 tokens of 16 heads), so not there.
+template <int D>
+__device__ __forceinline__ void in_order() {
+  if constexpr (D > 64) __builtin_amdgcn_sched_barrier(0x104);
+}
 
 // Scores.  t = z - ref from a raw product, all in the log2 domain.
 template <bool CAP, bool BIAS>
@@ -282,6 +307,22 @@ __device__ __forceinline__ Row row_at(const Dev& a, int i) {
   const pulse_mask_row r = a.rows[i];
   return Row{r.lo, r.hi, r.pos};
 }
+
+// Bit e of the result: key k + e is attended, for e in 0..31.
+__device__ __forceinline__ uint32_t attended(const Row& r, int k) {
+  const int lo = min(max(r.lo - k, 0), 32), hi = min(max(r.hi - k, 0), 32);
+  const uint32_t below = (uint32_t)((uint64_t{1} << hi) - 1);
+  return below & ~(uint32_t)((uint64_t{1} << lo) - 1);
+}
+// all ones if bit e of m is set, else 0
+__device__ __forceinline__ uint32_t bit(uint32_t m, int e) {
+  return (uint32_t)((int32_t)(m << (31 - e)) >> 31);
+}
+__device__ __forceinline__ float keep_or(uint32_t on, float x, uint32_t other) {
+  return __uint_as_float((__float_as_uint(x) & on) | (other & ~on));
+}
+constexpr uint32_t NEG_INF = 0xff800000u;
+constexpr int PAST = 1 << 30;  // lo of a row past the last
 
 // mask entry of rows [r0, r0 + n), n a multiple of the table's tile
 __device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
@@ -392,8 +433,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   const int grp = w / SH, shr = w % SH;
   const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int qrow = tile * RB + grp * 32 + n;
-  MaskTile mt{0, 0, 0, 0};  // of the tile that holds the wave's rows
-  if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
   const MaskTile bt = tiles_at(a, tile * RB, RB);
   int klo = bt.lo, khi = bt.hi;
   share(a, part, klo, khi);
@@ -410,6 +449,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   // q carries the sign of the scale, so that a masked -inf stays one
   score.k = fabsf(score.k);
   const Row rw = row_at(a, qrow);
+  const bool past = qrow >= a.Tq;  // nothing of such a row is kept
   bf16x8 qf[D / 16];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
@@ -443,7 +483,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     for (int y = 0; y < 2 / SH / NU; ++y) {
       const int kb = k0 + 32 * (shr + SH * y);  // the first key
       const int at = 64 * D * SH * y;
-      if (kb >= mt.hi || kb + 32 * NU <= mt.lo) continue;
+      if (!__any(rw.lo < kb + 32 * NU && rw.hi > kb)) continue;
       f32x16 s[NU];
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
@@ -460,13 +500,13 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
           float dz;
           s[u][i] = score(s[u][i], ref, far - (float)(32 * u + elem(i)), dz);
         }
-      if (mt.all_lo > kb || mt.all_hi < kb + 32 * NU) {
-        const uint32_t off = kb + 8 * hl - rw.lo, len = rw.hi - rw.lo;
+      if (!__all(past || (rw.lo <= kb && rw.hi >= kb + 32 * NU))) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < NU; ++u) {
+          const uint32_t on = attended(rw, kb + 32 * u + 8 * hl);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (off + 32 * u + elem(i) >= len) s[u][i] = -INFINITY;
+          for (int i = 0; i < 16; ++i) s[u][i] = keep_or(bit(on, elem(i)), s[u][i], NEG_INF);
+        }
       }
       float mx = s[0][0];
 #pragma unroll
@@ -562,8 +602,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   const int grp = w / SH, shr = w % SH;
   const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int qrow = tile * RB + grp * 32 + n;
-  MaskTile mt{0, 0, 0, 0};
-  if (qrow - n < a.Tq) mt = a.tiles[(qrow - n) / MASK_TILE];
   const MaskTile bt = tiles_at(a, tile * RB, RB);
   int klo = bt.lo, khi = bt.hi;
   share(a, part, klo, khi);
@@ -580,6 +618,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   if (tid() == 0) any_odd = 0;
   const Score<CAP, BIAS> score(a, h);
   const Row rw = row_at(a, qrow);
+  const bool past = qrow >= a.Tq;  // nothing of such a row is kept
   const bool in = qrow < a.Tq;
   bf16x8 qf[D / 16], df[D / 16];
   float Dq = 0.f;
@@ -625,27 +664,33 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     for (int u = 0; u < 2 / SH; ++u) {
       const int at = 64 * D * SH * u;
       const int r0 = 32 * (SH * u + shr), kb = k0 + r0;
-      if (kb >= mt.hi || kb + 32 <= mt.lo) continue;
+      if (!__any(rw.lo < kb + 32 && rw.hi > kb)) continue;
       f32x16 s = splat(0.f), dp = splat(-Dq);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) 
         s = mma(rows32<D>(smem, rbase + stage, kk, at), qf[kk], s);
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) 
-        dp = mma(rows32<D>(smem, rbase + stage, kk, at + 2 * TILE), df[kk], dp);
+      // p under the MFMAs of dp
       const float far = (float)(rw.pos - kb - 8 * hl);
+      float dz[16];
+      constexpr int NK = D / 16;
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        in_order<D>();
+        dp = mma(rows32<D>(smem, rbase + stage, kk, at + 2 * TILE), df[kk], dp);
+        in_order<D>();
+#pragma unroll
+        for (int i = 16 * kk / NK; i < 16 * (kk + 1) / NK; ++i)
+          s[i] = ex2(score(s[i], l2, far - (float)elem(i), dz[i]));
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float dz;
-        const float p = ex2(score(s[i], l2, far - (float)elem(i), dz));
-        s[i] = p * dp[i];
-        if (CAP) s[i] *= dz;
+        s[i] *= dp[i];
+        if (CAP) s[i] *= dz[i];
       }
-      if (mt.all_lo > kb || mt.all_hi < kb + 32) {
-        const uint32_t off = kb + 8 * hl - rw.lo, len = rw.hi - rw.lo;
+      if (!__all(past || (rw.lo <= kb && rw.hi >= kb + 32))) {
+        const uint32_t on = attended(rw, kb + 8 * hl);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (off + elem(i) >= len) s[i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[i] = keep_or(bit(on, elem(i)), s[i], 0);
       }
       if (partly && odd_at[it & 1] == it) {
         // a cleared key's score is not what it was; the rows that attend it
@@ -719,7 +764,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   constexpr bool RAW = !CAP && !BIAS;  // scores are k times the product
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT];
-  __shared__ __attribute__((aligned(16))) int Lo[2][KT], Len[2][KT], Pos[2][KT];
+  __shared__ __attribute__((aligned(16))) int Lo[2][KT], Hi[2][KT], Pos[2][KT];
   __shared__ int any_odd;
   int tile, kh, part;
   block_of(a, (a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh, part);
@@ -764,7 +809,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     sd.load(a.Tq - qt * KT, a.hd8);
     if (tid() < KT) {
       const int i = qt * KT + tid();
-      rn = row_at(a, i);
+      rn = i < a.Tq ? row_at(a, i) : Row{PAST, 0, 0};
       if (i < a.Tq) {
         ln = a.lse[(long)h * a.Tq + i];
         dn = a.dsum[(long)h * a.Tq + i];
@@ -787,11 +832,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     sq.store(Qs);
     sd.store(Qs + TILE);
     if (tid() < KT) {
-      const float l2 = finite_or_nan(ln) * LOG2E;
+      // a row past the last has p = 0 and is not masked
+      const float l2 = rn.lo == PAST ? INFINITY : finite_or_nan(ln) * LOG2E;
       Ls[it & 1][tid()] = RAW ? -l2 * a.inv_c1 : l2;
-      Ds[it & 1][tid()] = -finite_or_nan(dn);
+      Ds[it & 1][tid()] = rn.lo == PAST ? 0.f : -finite_or_nan(dn);
       Lo[it & 1][tid()] = rn.lo;
-      Len[it & 1][tid()] = rn.hi - rn.lo;
+      Hi[it & 1][tid()] = rn.hi;
       Pos[it & 1][tid()] = rn.pos;
     }
     __syncthreads();
@@ -807,11 +853,17 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       const int at = 64 * D * SH * u;
       const int rb = 32 * (SH * u + shr) + 8 * hl;  // the lane's first row in the tile
       if (kb0 >= mt.hi || kb0 + 32 <= mt.lo) continue;
+      bool part = mt.all_lo > kb0 || mt.all_hi < kb0 + 32;
+      if (part) {
+        // the step's rows (lane n: row n) against the wave's keys
+        const int lo = Lo[it & 1][rb - 8 * hl + n], hi = Hi[it & 1][rb - 8 * hl + n];
+        if (!__any(lo < kb0 + 32 && hi > kb0)) continue;
+        part = !__all(lo == PAST || (lo <= kb0 && hi >= kb0 + 32));
+      }
       // -lse / k and -D start the sums, so that p = 2^(k s) and ds = p dp
       const float* Lr = Ls[it & 1] + rb;
       const float* Dr = Ds[it & 1] + rb;
       f32x16 s;
-      const bool part = mt.all_lo > kb0 || mt.all_hi < kb0 + 32;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = RAW ? Lr[elem(i)] : 0.f;
 #pragma unroll
@@ -819,52 +871,65 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
         s = mma(rows32<D>(smem, rbase + stage, kk, at), kf[kk], s);
       bf16x8 p[2], ds[2];
       float dz[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        s[i] = RAW ? ex2(s[i] * score.k)
-                   : ex2(score(s[i], Lr[elem(i)],
-                               BIAS ? (float)(Pos[it & 1][rb + elem(i)] - key) : 0.f, dz[i]));
-      if (part) {
-        // -0 marks what is not attended
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int r = rb + elem(i);
-          if ((uint32_t)(key - Lo[it & 1][r]) >= (uint32_t)Len[it & 1][r]) s[i] = -0.f;
-        }
-      }
-      if (DV) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = (__bf16)s[i];
-      }
+      f32x16 dp;
       if (DK) {
-        f32x16 dp;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dp[i] = Dr[elem(i)];
+      }
+      // p under the MFMAs of dp
+      constexpr int NK = D / 16;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
+      for (int kk = 0; kk < NK; ++kk) {
+        if (DK) {
+          in_order<D>();
           dp = mma(rows32<D>(smem, rbase + stage, kk, at + 2 * TILE), vf[kk], dp);
+          in_order<D>();
+        }
+#pragma unroll
+        for (int i = 16 * kk / NK; i < 16 * (kk + 1) / NK; ++i)
+          s[i] = RAW ? ex2(s[i] * score.k)
+                     : ex2(score(s[i], Lr[elem(i)],
+                                 BIAS ? (float)(Pos[it & 1][rb + elem(i)] - key) : 0.f, dz[i]));
+      }
+      if (DK) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           dp[i] *= s[i];
           if (CAP) dp[i] *= dz[i];
         }
-        if (part) {
+      }
+      if (part) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (__float_as_uint(s[i]) == 0x80000000u) dp[i] = 0.f;
+        for (int i = 0; i < 16; ++i) {
+          const int r = rb + elem(i);
+          // no short cut: a branch per element costs more than the compares
+          const bool out = (key < Lo[it & 1][r]) | (key >= Hi[it & 1][r]);
+          s[i] = out ? 0.f : s[i];
+          if (DK) dp[i] = out ? 0.f : dp[i];
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) ds[i / 8][i % 8] = (__bf16)dp[i];
       }
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
+      for (int i = 0; i < 16; ++i) {
+        if (DV) p[i / 8][i % 8] = (__bf16)s[i];
+      }
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          if (DV)
+      for (int i = 0; i < 16; ++i) {
+        if (DK) ds[i / 8][i % 8] = (__bf16)dp[i];
+      }
+      if (DV) {
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
             dv[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks], dv[d]);
-          if (DK)
+      }
+      if (DK) {
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
             dk[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks), ds[ks], dk[d]);
-        }
+      }
     }
     qt = qn;
   }
