@@ -139,22 +139,26 @@ pulse_status pulse_attn_sizes(const pulse_attn_desc* desc, size_t* forward_bytes
  * p = softmax over the keys that row i attends; o_i = sum_j p_ij v_j.  A row
  * that attends nothing gives o = 0.  Keys a row does not attend do not reach
  * it, NaN and infinities included.  lse [heads][Tq] receives log sum_j
- * exp(z_ij), -inf for empty rows.  Scores, sums and accumulators are fp32;
- * p is rounded to bf16 as the operand of p v.  `mask` is the buffer filled by
+ * exp(z_ij), -inf for empty rows.  o_low (bf16 [Tq][heads][head_dim],
+ * contiguous, 16-byte aligned, or NULL) receives what the rounding of o left
+ * out, for the backward.  Scores, sums and accumulators are fp32; p is rounded
+ * to bf16 as the operand of p v.  `mask` is the buffer filled by
  * pulse_mask_build or _from_rows with the same Tq and Tk.  Outputs must not
  * overlap inputs.  The workspace is 256-byte aligned (NULL if it needs 0). */
 pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* q,
                                 const pulse_heads* k, const pulse_heads* v, const void* mask,
                                 const float* slopes, const pulse_heads* o, float* lse,
-                                void* workspace, size_t workspace_bytes, void* stream);
+                                void* o_low, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Gradients from dout, the forward's inputs, its o and its lse.  dk and dv
+/* Gradients from dout, the forward's inputs, its o, lse and o_low (NULL: o as
+ * rounded stands for the output in rowsum(dout o), which costs dq and dk about
+ * a tenth of their accuracy).  ds is rounded to bf16 as an operand.  dk and dv
  * sum over the query heads that share a key head; keys nobody attends get 0,
  * rows that attend nothing get dq = 0 and give nothing. */
 pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads* dout,
                                  const pulse_heads* q, const pulse_heads* k,
                                  const pulse_heads* v, const pulse_heads* o, const float* lse,
-                                 const void* mask, const float* slopes, const pulse_heads* dq,
+                                 const void* o_low, const void* mask, const float* slopes, const pulse_heads* dq,
                                  const pulse_heads* dk, const pulse_heads* dv, void* workspace,
                                  size_t workspace_bytes, void* stream);
 

@@ -58,6 +58,7 @@ struct Dev {  // device view of MattnArgs
   const MaskTile* tiles;
   const float* slopes;
   float* lse;
+  uint16_t* o_low;  // [Tq][H][8 hd8] or null
   float* dsum;
   // Work split further than rows and heads: `parts` blocks share a tile, each
   // with a range of the other side (or some of the group's heads) and fp32
@@ -364,14 +365,26 @@ __device__ __forceinline__ void share(const Dev& a, int part, int& lo, int& hi) 
 constexpr int MP = 36;                      // row pitch of a merge buffer (floats)
 constexpr int MERGE = 4 * 32 * MP * 4;      // its bytes
 
+// 8 values rounded to bf16, and what that leaves out, rounded
+__device__ __forceinline__ uint4 rounded(const float (&o)[8]) {
+  return uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+}
+__device__ __forceinline__ uint4 left_out(const float (&o)[8]) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = o[i] - bf2f(f2bf(o[i]));
+  return rounded(r);
+}
+
 // Write the waves' column accumulators [channels][32 columns], times f, to
-// rows row0 + .. of out (or of the part's fp32 results): 32 channels at a time
-// meet in LDS, where the shares of a group are added in order.  fix(row,
+// rows row0 + .. of out (or of the part's fp32 results), and to `low` what the
+// rounding leaves out: 32 channels at a time meet in LDS, where the shares of a group are added in order.  fix(row,
 // chunk, o) may change 8 channels before they are rounded.
 template <int D, int G, typename F>
 __device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 32], float f,
-                                           uint16_t* out, long stride, float* part, int row0,
-                                           int rows, int heads, int hd8, F fix) {
+                                           uint16_t* out, long stride, float* part,
+                                           uint16_t* low, int row0, int rows, int heads, int hd8,
+                                           F fix) {
   constexpr int SH = 4 / G;
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
 #pragma unroll
@@ -400,8 +413,9 @@ __device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 3
         q[1] = make_float4(o[4], o[5], o[6], o[7]);
         continue;
       }
-      *reinterpret_cast<uint4*>(out + row * stride + 32 * d + 8 * c) =
-          uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+      *reinterpret_cast<uint4*>(out + row * stride + 32 * d + 8 * c) = rounded(o);
+      if (low)
+        *reinterpret_cast<uint4*>(low + ((long)row * heads * hd8 + 4 * d + c) * 8) = left_out(o);
     }
   }
 }
@@ -577,7 +591,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   }
   // an empty row's accumulators are 0
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, none ? 0.f : ex2(ref - R) / t,
-                   a.o + h * a.oh, a.ot, po, tile * RB, a.Tq, a.H, a.hd8,
+                   a.o + h * a.oh, a.ot, po, a.o_low ? a.o_low + (long)h * a.hd8 * 8 : nullptr,
+                   tile * RB, a.Tq, a.H, a.hd8,
                    [&](int row, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      const Row x = row_at(a, row);
@@ -627,8 +642,11 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     qf[kk] = row_frag(a.q + qrow * a.qt + h * a.qh, 2 * kk + hl, in, a.hd8);
     df[kk] = row_frag(a.dout + qrow * a.dot + h * a.doh, 2 * kk + hl, in, a.hd8);
     const bf16x8 ov = row_frag(a.o_in + qrow * a.ot + h * a.oh, 2 * kk + hl, in, a.hd8);
+    // with what o's rounding left out: D is a difference's second term
+    const bf16x8 ol = row_frag(a.o_low + ((long)qrow * a.H + h) * a.hd8 * 8, 2 * kk + hl,
+                               in && a.o_low, a.hd8);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) Dq += (float)df[kk][t] * (float)ov[t];
+    for (int t = 0; t < 8; ++t) Dq += (float)df[kk][t] * ((float)ov[t] + (float)ol[t]);
   }
   Dq += __shfl_xor(Dq, 32, 64);
   float l2 = 0.f;
@@ -710,7 +728,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     }
   }
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
-                   part_of(a, a.part0, part, a.Tq, a.H, h), tile * RB, a.Tq, a.H, a.hd8, [&](int row, int c, float (&o)[8]) {
+                   part_of(a, a.part0, part, a.Tq, a.H, h), nullptr, tile * RB, a.Tq, a.H, a.hd8,
+                   [&](int row, int c, float (&o)[8]) {
                      if (!any_odd) return;
                      const Row x = row_at(a, row);
                      if (x.hi <= x.lo) return;
@@ -936,12 +955,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   float* mb = reinterpret_cast<float*>(smem);
   if constexpr (DK)
     write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt,
-                     part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), tile * RB, a.Tk,
+                     part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
                      a.H / a.rep, a.hd8,
                    [](int, int, float (&)[8]) {});
   if constexpr (DV)
     write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt,
-                     part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), tile * RB, a.Tk,
+                     part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
                      a.H / a.rep, a.hd8,
                    [&](int j, int c, float (&o)[8]) {
                      if (!any_odd) return;
@@ -980,6 +999,7 @@ Dev view(const MattnArgs& a) {
   d.tiles = reinterpret_cast<const MaskTile*>(d.rows + a.Tq);
   d.slopes = a.slopes;
   d.lse = a.lse;
+  d.o_low = static_cast<uint16_t*>(a.o_low);
   return d;
 }
 
@@ -1008,8 +1028,7 @@ __global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int hea
   }
   const long rh = e / hd8, row = rh / heads;
   const int c = e - rh * hd8, h = rh - row * heads;
-  *reinterpret_cast<uint4*>(out + row * ts + h * hs + 8 * c) =
-      uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+  *reinterpret_cast<uint4*>(out + row * ts + h * hs + 8 * c) = rounded(o);
 }
 
 // o = sum o_p 2^(lse_p - lse), lse = log2 sum 2^lse_p over the forward's parts
@@ -1037,8 +1056,8 @@ __global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
   const float f = 1.f / t;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = empty ? 0.f : o[i] * f;
-  *reinterpret_cast<uint4*>(a.o + row * a.ot + h * a.oh + 8 * c) =
-      uint4{pack2(o[0], o[1]), pack2(o[2], o[3]), pack2(o[4], o[5]), pack2(o[6], o[7])};
+  *reinterpret_cast<uint4*>(a.o + row * a.ot + h * a.oh + 8 * c) = rounded(o);
+  if (a.o_low) *reinterpret_cast<uint4*>(a.o_low + e * 8) = left_out(o);
   if (c == 0)
     a.lse[(long)h * a.Tq + row] = empty ? -INFINITY : (R + __builtin_amdgcn_logf(t)) * LN2;
 }

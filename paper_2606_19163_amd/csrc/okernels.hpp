@@ -49,6 +49,7 @@ struct MattnArgs {
   const void* mask;
   const float* slopes;
   float* lse;
+  void* o_low;  // or null
   void* ws;
 };
 

@@ -224,23 +224,25 @@ pulse_status pulse_attn_sizes(const pulse_attn_desc* desc, size_t* forward_bytes
 pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* q,
                                 const pulse_heads* k, const pulse_heads* v, const void* mask,
                                 const float* slopes, const pulse_heads* o, float* lse,
-                                void* workspace, size_t workspace_bytes, void* stream) {
+                                void* o_low, void* workspace, size_t workspace_bytes, void* stream) {
   OCHK(check_attn(desc));
   OCHK(check_attn_inputs(desc, q, k, v, mask, slopes));
   OCHK(check_heads(o, "o", desc->queries, desc->heads, desc->head_dim, 2, true));
   if (desc->queries && !lse) return ofail(PULSE_E_INVALID_ARG, "lse is NULL");
   if (!aligned(lse, 4)) return ofail(PULSE_E_INVALID_ARG, "lse is not 4-byte aligned");
+  if (!aligned(o_low, 16)) return ofail(PULSE_E_INVALID_ARG, "o_low is not 16-byte aligned");
   OCHK(check_ws(workspace, workspace_bytes, mattn_fwd_bytes(*desc)));
   MattnArgs a = attn_args(desc, q, k, v, mask, slopes, workspace);
   a.o = *o;
   a.lse = lse;
+  a.o_low = o_low;
   return launched(launch_mattn_fwd(a, static_cast<hipStream_t>(stream)), "attention forward");
 }
 
 pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads* dout,
                                  const pulse_heads* q, const pulse_heads* k,
                                  const pulse_heads* v, const pulse_heads* o, const float* lse,
-                                 const void* mask, const float* slopes, const pulse_heads* dq,
+                                 const void* o_low, const void* mask, const float* slopes, const pulse_heads* dq,
                                  const pulse_heads* dk, const pulse_heads* dv, void* workspace,
                                  size_t workspace_bytes, void* stream) {
   OCHK(check_attn(desc));
@@ -252,10 +254,12 @@ pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads*
   OCHK(check_heads(dv, "dv", desc->keys, desc->kv_heads, desc->head_dim, 2, true));
   if (desc->queries && !lse) return ofail(PULSE_E_INVALID_ARG, "lse is NULL");
   if (!aligned(lse, 4)) return ofail(PULSE_E_INVALID_ARG, "lse is not 4-byte aligned");
+  if (!aligned(o_low, 16)) return ofail(PULSE_E_INVALID_ARG, "o_low is not 16-byte aligned");
   OCHK(check_ws(workspace, workspace_bytes, mattn_bwd_bytes(*desc)));
   MattnArgs a = attn_args(desc, q, k, v, mask, slopes, workspace);
   a.o = *o, a.dout = *dout, a.dq = *dq, a.dk = *dk, a.dv = *dv;
   a.lse = const_cast<float*>(lse);
+  a.o_low = const_cast<void*>(o_low);
   return launched(launch_mattn_bwd(a, static_cast<hipStream_t>(stream)), "attention backward");
 }
 

@@ -23,7 +23,7 @@ import torch
 
 from .stage import BF16, F32, E_INVALID_ARG, PulseError, _check, lib as _lib
 
-__all__ = ["Rope", "Mask", "Attn", "GradClip", "rope_freqs", "grid_positions", "MaskRow"]
+__all__ = ["Rope", "Mask", "Attn", "Saved", "GradClip", "rope_freqs", "grid_positions", "MaskRow"]
 
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
@@ -83,11 +83,11 @@ def lib():
         ad = ctypes.POINTER(AttnDesc)
         L.pulse_attn_sizes.argtypes = [ad, _szp, _szp]
         L.pulse_attn_sizes.restype = st
-        L.pulse_attn_forward.argtypes = [ad, hp, hp, hp, _vp, _vp, hp, _vp, _vp, ctypes.c_size_t,
-                                         _vp]
+        L.pulse_attn_forward.argtypes = [ad, hp, hp, hp, _vp, _vp, hp, _vp, _vp, _vp,
+                                         ctypes.c_size_t, _vp]
         L.pulse_attn_forward.restype = st
-        L.pulse_attn_backward.argtypes = [ad, hp, hp, hp, hp, hp, _vp, _vp, _vp, hp, hp, hp, _vp,
-                                          ctypes.c_size_t, _vp]
+        L.pulse_attn_backward.argtypes = [ad, hp, hp, hp, hp, hp, _vp, _vp, _vp, _vp, hp, hp, hp,
+                                          _vp, ctypes.c_size_t, _vp]
         L.pulse_attn_backward.restype = st
         L.pulse_clip_create.argtypes = [ctypes.POINTER(ClipTensor), _i32, ctypes.POINTER(_vp)]
         L.pulse_clip_create.restype = st
@@ -251,6 +251,27 @@ class Mask:
         return self.rows
 
 
+class Saved:
+    """What a forward leaves for its backward beside the output: the scores'
+    log sum exp (``lse``, fp32 [heads, queries]) and what the rounding of the
+    output left out."""
+
+    __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr")
+
+    def __init__(self, heads, queries, head_dim, device):
+        n = -(-heads * queries // 4) * 4  # the second part is 16-byte aligned
+        self.buffer = torch.empty(n + heads * queries * head_dim // 2, dtype=torch.float32,
+                                  device=device)
+        self.shape = (heads, queries, head_dim)
+        self.lse_ptr = self.buffer.data_ptr()
+        self.low_ptr = self.lse_ptr + 4 * n
+
+    @property
+    def lse(self):
+        h, t, _ = self.shape
+        return self.buffer[:h * t].view(h, t)
+
+
 class Attn:
     """Attention of ``queries`` rows and ``heads`` heads under a mask (bf16)."""
 
@@ -272,14 +293,15 @@ class Attn:
             _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
         return mask.ptr
 
-    def forward(self, q, k, v, mask, slopes=None, out=None, lse=None, stream=None):
-        """(o, lse): o [queries, heads, head_dim], lse [heads, queries] fp32."""
+    def forward(self, q, k, v, mask, slopes=None, out=None, saved=None, stream=None):
+        """(o, saved): o [queries, heads, head_dim] and what the backward needs
+        beside it (into ``saved`` of an earlier call, if given)."""
         bf = torch.bfloat16
         with _On(stream) as (dev, s):
             if out is None:
                 out = torch.empty(self.qs, dtype=bf, device=q.device)
-            if lse is None:
-                lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
+            if saved is None:
+                saved = Saved(self.heads, self.queries, self.dim, q.device)
             ws = None
             if self.fwd_bytes:
                 ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
@@ -287,12 +309,18 @@ class Attn:
                 self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
                 _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev),
                 _flat(slopes, "slopes", self.heads, torch.float32, dev),
-                _heads(out, "out", self.qs, bf, dev),
-                _flat(lse, "lse", self.heads * self.queries, torch.float32, dev),
+                _heads(out, "out", self.qs, bf, dev), *self._saved(saved, dev),
                 ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
-        return out, lse
+        return out, saved
 
-    def backward(self, dout, q, k, v, o, lse, mask, slopes=None, out=None, stream=None):
+    def _saved(self, saved, dev):
+        if saved.shape != (self.heads, self.queries, self.dim):
+            _bad(f"saved is of heads, queries and head_dim {saved.shape}")
+        if saved.buffer.get_device() != dev:
+            _bad(f"saved is on {saved.buffer.device}, not on the current GPU")
+        return saved.lse_ptr, saved.low_ptr
+
+    def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
         bf = torch.bfloat16
         with _On(stream) as (dev, s):
@@ -306,11 +334,10 @@ class Attn:
             _check(lib().pulse_attn_backward(
                 self.desc, _heads(dout, "dout", self.qs, bf, dev), _heads(q, "q", self.qs, bf, dev),
                 _heads(k, "k", self.ks, bf, dev), _heads(v, "v", self.ks, bf, dev),
-                _heads(o, "o", self.qs, bf, dev),
-                _flat(lse, "lse", self.heads * self.queries, torch.float32, dev),
-                self._mask(mask, dev), _flat(slopes, "slopes", self.heads, torch.float32, dev),
-                _heads(dq, "dq", self.qs, bf, dev),
-                _heads(dk, "dk", self.ks, bf, dev), _heads(dv, "dv", self.ks, bf, dev),
+                _heads(o, "o", self.qs, bf, dev), *self._saved(saved, dev), self._mask(mask, dev),
+                _flat(slopes, "slopes", self.heads, torch.float32, dev),
+                _heads(dq, "dq", self.qs, bf, dev), _heads(dk, "dk", self.ks, bf, dev),
+                _heads(dv, "dv", self.ks, bf, dev),
                 ws.data_ptr() if ws is not None else None, self.bwd_bytes, s))
         return dq, dk, dv
 

@@ -244,11 +244,11 @@ def _see_mm(a, b, see):
 def _attn_run(plan, mask, q, k, v, g, slopes=None):
     q, k, v, g = (x.cuda() for x in (q, k, v, g))
     sl = None if slopes is None else slopes.cuda()
-    o, lse = plan.forward(q, k, v, mask, slopes=sl)
-    dq, dk, dv = plan.backward(g, q, k, v, o, lse, mask, slopes=sl)
+    o, saved = plan.forward(q, k, v, mask, slopes=sl)
+    dq, dk, dv = plan.backward(g, q, k, v, o, saved, mask, slopes=sl)
     torch.cuda.synchronize()
     return {n: x.cpu().double() for n, x in
-            dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv).items()}
+            dict(o=o, lse=saved.lse, dq=dq, dk=dk, dv=dv).items()}
 
 
 def _attn_check(got, ref, label):
@@ -420,14 +420,14 @@ def test_attn_strides():
     mask = ops.Mask(t, docs=2, causal=True)
     mask.build(_dev([0, 90, 140]))
     plan = ops.Attn(t, h, d, kv_heads=2)
-    o, lse = plan.forward(q, k, v, mask)
+    o, saved = plan.forward(q, k, v, mask)
     o2 = torch.empty(h, t, d, dtype=BF, device="cuda").transpose(0, 1)
     plan.forward(q.contiguous(), k.contiguous(), v.contiguous(), mask, out=o2)
     assert torch.equal(o, o2)
-    a = plan.backward(do, q, k, v, o, lse, mask)
+    a = plan.backward(do, q, k, v, o, saved, mask)
     dqkv = torch.full_like(qkv, 7.0)
     out = dqkv.split([h, 2, 2], dim=1)
-    plan.backward(do.contiguous(), q, k, v, o2, lse, mask, out=out)
+    plan.backward(do.contiguous(), q, k, v, o2, saved, mask, out=out)
     for x, y in zip(a, out):
         assert torch.equal(x, y)
     one = v[:1].expand(t, 2, d)
@@ -487,10 +487,10 @@ def test_attn_large_scores_and_scales():
     for scale, mul in ((4.0, 4.0), (0.0, 1.0), (-0.125, 1.0)):
         plan = ops.Attn(150, 2, 64, scale=scale)
         qs = (q.float() * mul).to(BF)
-        o, lse = plan.forward(qs.cuda(), k.cuda(), v.cuda(), mask)
+        o, saved = plan.forward(qs.cuda(), k.cuda(), v.cuda(), mask)
         ref = _attn_ref(qs, k, v, do, rows, scale, 0.0, None)
         assert rel_l2(o.cpu().double(), ref["o"]) <= ATTN_TOL, scale
-        assert rel_l2(lse.cpu().double(), ref["lse"]) <= 1e-6, scale
+        assert rel_l2(saved.lse.cpu().double(), ref["lse"]) <= 1e-6, scale
 
 
 def test_attn_streams_and_graph():
@@ -502,15 +502,15 @@ def test_attn_streams_and_graph():
     d = [x.cuda() for x in (q, k, v, do)]
     st = torch.cuda.Stream()
     st.wait_stream(torch.cuda.current_stream())
-    o, lse = plan.forward(*d[:3], mask, stream=st)
-    dq, dk, dv = plan.backward(d[3], *d[:3], o, lse, mask, stream=st)
+    o, saved = plan.forward(*d[:3], mask, stream=st)
+    dq, dk, dv = plan.backward(d[3], *d[:3], o, saved, mask, stream=st)
     torch.cuda.synchronize()
     for n, x in dict(o=o, dq=dq, dk=dk, dv=dv).items():
         assert torch.equal(x.cpu().double(), first[n]), n
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        o, lse = plan.forward(*d[:3], mask)
-        dq, dk, dv = plan.backward(d[3], *d[:3], o, lse, mask)
+        o, saved = plan.forward(*d[:3], mask)
+        dq, dk, dv = plan.backward(d[3], *d[:3], o, saved, mask)
     for seed in (1, 2, 3):
         g = _gen(seed)
         new = [_randn(g, *x.shape).to(BF) for x in d]

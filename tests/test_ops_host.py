@@ -133,20 +133,20 @@ def test_attn_descriptors(kw, status):
 def _attn_calls(d, **kw):
     """Both calls with plausible arguments but for those given."""
     q, k = ops.Heads(P, 256, 64), ops.Heads(P, 128, 64)
-    a = dict(q=q, k=k, v=k, o=q, dout=q, dq=q, dk=k, dv=k, mask=P, slopes=P, lse=P, ws=P,
+    a = dict(q=q, k=k, v=k, o=q, dout=q, dq=q, dk=k, dv=k, mask=P, slopes=P, lse=P, low=P, ws=P,
              nbytes=1 << 40)
     a.update(kw)
     L = ops.lib()
     return (L.pulse_attn_forward(d, a["q"], a["k"], a["v"], a["mask"], a["slopes"], a["o"],
-                                 a["lse"], a["ws"], a["nbytes"], None),
+                                 a["lse"], a["low"], a["ws"], a["nbytes"], None),
             L.pulse_attn_backward(d, a["dout"], a["q"], a["k"], a["v"], a["o"], a["lse"],
-                                  a["mask"], a["slopes"], a["dq"], a["dk"], a["dv"], a["ws"],
+                                  a["low"], a["mask"], a["slopes"], a["dq"], a["dk"], a["dv"], a["ws"],
                                   a["nbytes"], None))
 
 
 @pytest.mark.parametrize("kw", [
     dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(mask=None), dict(lse=None),
-    dict(mask=P + 4), dict(slopes=P + 1), dict(lse=P + 2), dict(q=ops.Heads(None, 256, 64)),
+    dict(mask=P + 4), dict(slopes=P + 1), dict(lse=P + 2), dict(low=P + 8), dict(q=ops.Heads(None, 256, 64)),
     dict(k=ops.Heads(P + 8, 128, 64)), dict(v=ops.Heads(P, 130, 64)),
     dict(q=ops.Heads(P, 256, -64)),
 ])
