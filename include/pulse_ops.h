@@ -123,7 +123,8 @@ pulse_status pulse_mask_from_rows(const pulse_mask_desc* desc, const pulse_mask_
 typedef struct {
   int32_t queries, keys;   /* Tq, Tk as in the mask                          */
   int32_t heads, kv_heads; /* query head h reads key head h / (heads /
-                              kv_heads); 1 <= kv_heads, dividing heads <= 1024 */
+                              kv_heads); 1 <= kv_heads, dividing heads <= 1024;
+                              Tq heads and Tk kv_heads at most 2^30          */
   int32_t head_dim;        /* a multiple of 8, 8..128                        */
   float scale;             /* of the scores (finite)                         */
   float cap;               /* 0: none; else scores become cap tanh(s / cap)  */
@@ -158,9 +159,10 @@ pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* 
 pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads* dout,
                                  const pulse_heads* q, const pulse_heads* k,
                                  const pulse_heads* v, const pulse_heads* o, const float* lse,
-                                 const void* o_low, const void* mask, const float* slopes, const pulse_heads* dq,
-                                 const pulse_heads* dk, const pulse_heads* dv, void* workspace,
-                                 size_t workspace_bytes, void* stream);
+                                 const void* o_low, const void* mask, const float* slopes,
+                                 const pulse_heads* dq, const pulse_heads* dk,
+                                 const pulse_heads* dv, void* workspace, size_t workspace_bytes,
+                                 void* stream);
 
 /* ---- gradient norm and clipping ------------------------------------------- */
 

@@ -362,8 +362,8 @@ __device__ __forceinline__ void share(const Dev& a, int part, int& lo, int& hi) 
   hi = min(hi, lo + n);
 }
 
-constexpr int MP = 36;                      // row pitch of a merge buffer (floats)
-constexpr int MERGE = 4 * 32 * MP * 4;      // its bytes
+constexpr int MP = 36;                  // row pitch of a merge buffer (floats)
+constexpr int MERGE = 4 * 32 * MP * 4;  // its bytes
 
 // 8 values rounded to bf16, and what that leaves out, rounded
 __device__ __forceinline__ uint4 rounded(const float (&o)[8]) {
@@ -378,8 +378,9 @@ __device__ __forceinline__ uint4 left_out(const float (&o)[8]) {
 
 // Write the waves' column accumulators [channels][32 columns], times f, to
 // rows row0 + .. of out (or of the part's fp32 results), and to `low` what the
-// rounding leaves out: 32 channels at a time meet in LDS, where the shares of a group are added in order.  fix(row,
-// chunk, o) may change 8 channels before they are rounded.
+// rounding leaves out: 32 channels at a time meet in LDS, where the shares of
+// a group are added in order.  fix(row, chunk, o) may change 8 channels before
+// they are rounded.
 template <int D, int G, typename F>
 __device__ __forceinline__ void write_rows(float* buf, const f32x16 (&acc)[D / 32], float f,
                                            uint16_t* out, long stride, float* part,
@@ -432,7 +433,16 @@ template <int D>
 constexpr int SMEM = max_of(4 * KT * D * 2, MERGE);
 
 // ---------------------------------------------------------------------------
-// forward
+// Forward: o^T += v^T p^T with the running reference and sum of a row in the
+// lane that holds its column, so that a step's only exchange between lanes is
+// the vote on the reference.
+// Bound by the vector units and the matrix units in turn, which overlap little
+// within a wave: a 32 x 32 step of D = 64 is 107 quarter-cycles of vector work
+// (exponential, scale and subtract, sum, maximum, rounding: 16 scores a lane)
+// and 64 of MFMA, of 160 in all.  8192 tokens of 16 heads: D = 64 335 us (820
+// TFLOP/s), D = 128 565 us (975 TFLOP/s).  64 rows per wave instead of 32 run
+// at one wave per SIMD and were slower (D = 128: 637 TFLOP/s), 8 waves per block
+// too (16 x 256 tokens of 12 heads: 16.8 us instead of 13.1).
 // ---------------------------------------------------------------------------
 template <int D, int G, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
@@ -491,7 +501,10 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
       sk.load(a.Tk - k0 - KT, a.hd8);
       sv.load(a.Tk - k0 - KT, a.hd8);
     }
-    // 32-key steps, NU of them taken together
+    // 32-key steps, NU of them taken together where two waves share a SIMD and
+    // a step has MFMAs enough to cover the exponentials of another: 8192 tokens
+    // of 16 heads, D = 128: 548 us with two, 586 with one; D = 64: 355 and 341;
+    // 8 x 1024 tokens, D = 88: 75 and 71
     constexpr int NU = D == 128 ? 2 / SH : 1;
 #pragma unroll
     for (int y = 0; y < 2 / SH / NU; ++y) {
@@ -557,8 +570,9 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks)
-            acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 64 * D * u + 32 * D * ks + 2 * TILE),
-                         p[ks], acc[d]);
+            acc[d] = mma(
+                cols32<D>(smem, cbase + stage, d, at + 64 * D * u + 32 * D * ks + 2 * TILE), p[ks],
+                acc[d]);
       }
     }
   }
@@ -602,7 +616,10 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
 }
 
 // ---------------------------------------------------------------------------
-// backward over query rows: D = rowsum(do o), dq = ds k
+// Backward over query rows: D = rowsum(do o), dq = ds k.  Three products a
+// step; a row's lse and D sit in the lane of its column, and -D starts the sum
+// of dp.  Bound as the forward is: about 1000 TFLOP/s over its three products
+// at 8192 tokens of 16 heads.
 // ---------------------------------------------------------------------------
 template <int D, int G, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
@@ -685,7 +702,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
       if (!__any(rw.lo < kb + 32 && rw.hi > kb)) continue;
       f32x16 s = splat(0.f), dp = splat(-Dq);
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) 
+      for (int kk = 0; kk < D / 16; ++kk)
         s = mma(rows32<D>(smem, rbase + stage, kk, at), qf[kk], s);
       // p under the MFMAs of dp
       const float far = (float)(rw.pos - kb - 8 * hl);
@@ -742,40 +759,53 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
 }
 
 // The tiles of query rows, in order, some of whose rows attend some of keys
-// [k0, k1).  Every wave of a block sees the same ones: a wave looks at 64
-// table entries at a time.
+// [k0, k1), and of these every step-th from the first-th on.  Every wave of a
+// block sees the same ones: a wave looks at 64 table entries at a time.
 struct Hits {
-  int base, k0, k1, first, end;  // of tiles [first, end)
+  int base, k0, k1, first, step, skip;
   uint64_t bits;
   __device__ __forceinline__ void look(const Dev& a, int lane) {
     const int t = base + lane;
     bool hit = false;
-    if (t < end) {
+    if (t < mask_tiles(a.Tq)) {
       const MaskTile m = a.tiles[t];
       hit = m.lo < k1 && m.hi > k0;
     }
     bits = __ballot(hit);
   }
   __device__ __forceinline__ void start(const Dev& a, int lane) {
-    base = first;
+    base = 0;
+    skip = first;
     look(a, lane);
   }
   // the next tile, or -1
   __device__ __forceinline__ int next(const Dev& a, int lane) {
-    while (bits == 0) {
-      base += 64;
-      if (base >= end) return -1;
-      look(a, lane);
+    for (;;) {
+      while (bits == 0) {
+        base += 64;
+        if (base >= mask_tiles(a.Tq)) return -1;
+        look(a, lane);
+      }
+      const int t = base + __builtin_ctzll(bits);
+      bits &= bits - 1;
+      if (skip-- == 0) {
+        skip = step - 1;
+        return t;
+      }
     }
-    const int t = base + __builtin_ctzll(bits);
-    bits &= bits - 1;
-    return t;
   }
 };
 
 // ---------------------------------------------------------------------------
-// backward over keys: dk = ds^T q, dv = p^T do, the query rows of every head
-// of the group that attend any of the block's keys streaming by
+// Backward over keys: dk = ds^T q, dv = p^T do, the query rows of every head
+// of the group that attend any of the block's keys streaming by.  Computing s
+// and dp again here costs two products of seven, but needs neither atomics
+// (whose order would change results) nor partial sums of dq per key tile.
+// Both accumulators and both operands of D = 128 do not fit the registers of
+// two waves per SIMD: dv and dk then have a pass each, with s computed in both
+// (8192 tokens of 16 heads: 1370 us instead of 1489; at D = 96 one pass, 143
+// us, and two, 174, 8 x 1024 tokens).  About 900 TFLOP/s over its products.
+// The whole backward at 8192 tokens of 16 heads: D = 64 1020 us, D = 128 2150.
 // ---------------------------------------------------------------------------
 template <int D, int G, int WPE, bool CAP, bool BIAS, bool DK, bool DV>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
@@ -810,11 +840,11 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   Hits hits;
   hits.k0 = tile * RB;
   hits.k1 = tile * RB + RB;
-  // the part's heads and tiles of rows
-  const int heads = a.rep / a.head_parts, row_parts = a.parts / a.head_parts;
-  const int h0 = kh * a.rep + part % a.head_parts * heads, rp = part / a.head_parts;
-  hits.first = (int)((long)mask_tiles(a.Tq) * rp / row_parts);
-  hits.end = (int)((long)mask_tiles(a.Tq) * (rp + 1) / row_parts);
+  // the part's heads, and its share of the tiles of rows
+  const int heads = a.rep / a.head_parts;
+  const int h0 = kh * a.rep + part % a.head_parts * heads;
+  hits.first = part / a.head_parts;
+  hits.step = a.parts / a.head_parts;
   float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
   Row rn{0, 0, 0};
   __syncthreads();  // any_odd
@@ -886,7 +916,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = RAW ? Lr[elem(i)] : 0.f;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) 
+      for (int kk = 0; kk < D / 16; ++kk)
         s = mma(rows32<D>(smem, rbase + stage, kk, at), kf[kk], s);
       bf16x8 p[2], ds[2];
       float dz[16];
@@ -930,9 +960,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         if (DV) p[i / 8][i % 8] = (__bf16)s[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
         if (DK) ds[i / 8][i % 8] = (__bf16)dp[i];
       }
       if (DV) {
@@ -940,7 +967,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks)
-            dv[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks], dv[d]);
+            dv[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks + 2 * TILE), p[ks],
+                        dv[d]);
       }
       if (DK) {
 #pragma unroll
@@ -956,22 +984,20 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   if constexpr (DK)
     write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt,
                      part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
-                     a.H / a.rep, a.hd8,
-                   [](int, int, float (&)[8]) {});
+                     a.H / a.rep, a.hd8, [](int, int, float (&)[8]) {});
   if constexpr (DV)
     write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt,
                      part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
-                     a.H / a.rep, a.hd8,
-                   [&](int j, int c, float (&o)[8]) {
-                     if (!any_odd) return;
-                     for (int i = 0; i < a.Tq; ++i) {
-                       const Row x = row_at(a, i);
-                       if (j < x.lo || j >= x.hi) continue;
-                       for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
-                         add_odd(o, *reinterpret_cast<const uint4*>(a.dout + i * a.dot +
-                                                                    g * a.doh + 8 * c), false);
-                     }
-                   });
+                     a.H / a.rep, a.hd8, [&](int j, int c, float (&o)[8]) {
+                       if (!any_odd) return;
+                       for (int i = 0; i < a.Tq; ++i) {
+                         const Row x = row_at(a, i);
+                         if (j < x.lo || j >= x.hi) continue;
+                         for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
+                           add_odd(o, *reinterpret_cast<const uint4*>(a.dout + i * a.dot +
+                                                                      g * a.doh + 8 * c), false);
+                       }
+                     });
 }
 
 Dev view(const MattnArgs& a) {
@@ -1007,7 +1033,8 @@ Dev view(const MattnArgs& a) {
 // joining the parts
 // ---------------------------------------------------------------------------
 
-// out = sum of the parts, in order (blockIdx.y: dq or dk; dv)
+// out = sum of the parts, in order (workgroup y: dq or dk; dv).  Memory-bound:
+// each partial is read once.
 __global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int heads, int hd8,
                                                    const float* p0, const float* p1, uint16_t* o0,
                                                    uint16_t* o1, long t0, long h0, long t1,
@@ -1031,7 +1058,8 @@ __global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int hea
   *reinterpret_cast<uint4*>(out + row * ts + h * hs + 8 * c) = rounded(o);
 }
 
-// o = sum o_p 2^(lse_p - lse), lse = log2 sum 2^lse_p over the forward's parts
+// o = sum o_p 2^(lse_p - lse), lse = log2 sum 2^lse_p over the forward's parts;
+// memory-bound
 __global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
   const long n = (long)a.Tq * a.H * a.hd8;
   const long e = (long)__builtin_amdgcn_workgroup_id_x() * 256 + tid();
@@ -1069,7 +1097,28 @@ struct Plan {
   int parts, head_parts;  // as in Dev
 };
 
-// How a pass is spread over the GPU (256 CUs, two or three blocks each).
+// How a pass is spread over the GPU (256 CUs, two or three blocks each); us
+// of forward and backward in what follows.
+//
+// Shared key heads: a block over keys takes one of the heads that share them
+// where it would have to stream all of them, while there are fewer than 1024
+// blocks.  12240 tokens, 16 heads on 2, D = 64: 1505 with, 3135 without; at
+// 1024 blocks (65536 tokens in 128 documents, 16 heads on 4) 854 and 652.
+//
+// Blocks of 128 rows where there are 512 of them, else of 64.  4096 tokens of
+// 16 heads (512 blocks) in 16 documents: 15.9 + 39.1 with 128 rows, 16.4 +
+// 50.7 with 64; 4001 of 12 heads (384) in 21 documents of 60 to 958: 37.5 +
+// 106.9 and 28.3 + 92.4 (D = 128: 51.7 + 204 and 47.5 + 185; where all
+// documents are alike, 10 % the other way).
+//
+// Fewer than 256 blocks: in parts along the other side, up to one block per
+// CU, of 256 rows or more (512 beyond 8 parts), where that takes at least 1024
+// rows off each block, since the second kernel costs 4 us.  1 row on 16384
+// keys, 8 heads: 26 + 46 in parts, 189 + 302 without; 2048 on 2048, 2 heads,
+// D = 64, in one document 18 + 41 and 27 + 73, in 4 documents, of which a part
+// may see none, 13 + 28 and 10 + 27.  Two blocks per CU gain 10 % on one
+// document and lose 40 % on four; 1024 on 1024 in two parts or more: 12 + 24
+// and 10 + 27 on two documents, 20 + 52 and 17 + 44 with 12 heads.
 Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
   const int rows = p == BWD_KV ? Tk : Tq, heads = p == BWD_KV ? KV : H;
   const int other = p == BWD_KV ? Tq : Tk;
@@ -1084,9 +1133,11 @@ Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
     blocks = (long)((rows + 63) / 64) * heads * x.parts;
   }
   if (blocks > 0 && blocks < 256) {
-    const long most = other / 512, want = 512 / blocks;
-    const long n = want < most ? want : most;
-    if (n > 1) x.parts *= (int)(n < 16 ? n : 16);
+    const long most = max_of(other / 512, other / 256 < 8 ? other / 256 : 8);
+    long n = 256 / blocks;
+    if (n > most) n = most;
+    if (n > 64) n = 64;
+    if (n > 1 && other - other / n >= 1024) x.parts *= (int)n;
   }
   return x;
 }
@@ -1122,7 +1173,10 @@ hipError_t launch_mode(const Dev& d, hipStream_t st) {
 
 template <Pass P, int D>
 hipError_t launch_rows(const Dev& d, int group, hipStream_t st) {
-  constexpr int W = P == BWD_KV ? 2 : D == 64 ? 3 : 2;
+  // waves per SIMD.  Three at D = 64: 16 x 256 tokens of 12 heads, backward
+  // 38.8 us, with two 40.6; at 96, and over keys, three spill (8 x 1024 tokens
+  // of 16 heads of 88, backward: 220 us with two, 338 with three over rows).
+  constexpr int W = P != BWD_KV && D == 64 ? 3 : 2;
   return group == 4 ? launch_mode<P, D, 4, W>(d, st) : launch_mode<P, D, 2, W>(d, st);
 }
 

@@ -108,6 +108,9 @@ pulse_status check_attn(const pulse_attn_desc* d) {
     return ofail(PULSE_E_SHAPE, "queries and keys must be in [0, 2^24]");
   if (d->heads < 1 || d->heads > MAX_HEADS || d->kv_heads < 1 || d->heads % d->kv_heads)
     return ofail(PULSE_E_SHAPE, "heads must be in [1, %d] and a multiple of kv_heads", MAX_HEADS);
+  // a launch has less than 2^32 threads
+  if ((int64_t)d->queries * d->heads > 1 << 30 || (int64_t)d->keys * d->kv_heads > 1 << 30)
+    return ofail(PULSE_E_SHAPE, "queries * heads and keys * kv_heads must be at most 2^30");
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8)
     return ofail(PULSE_E_SHAPE, "head_dim must be a multiple of 8 in [8, 128]");
   if (!std::isfinite(d->scale)) return ofail(PULSE_E_INVALID_ARG, "scale must be finite");
@@ -242,9 +245,10 @@ pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* 
 pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads* dout,
                                  const pulse_heads* q, const pulse_heads* k,
                                  const pulse_heads* v, const pulse_heads* o, const float* lse,
-                                 const void* o_low, const void* mask, const float* slopes, const pulse_heads* dq,
-                                 const pulse_heads* dk, const pulse_heads* dv, void* workspace,
-                                 size_t workspace_bytes, void* stream) {
+                                 const void* o_low, const void* mask, const float* slopes,
+                                 const pulse_heads* dq, const pulse_heads* dk,
+                                 const pulse_heads* dv, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
   OCHK(check_attn(desc));
   OCHK(check_attn_inputs(desc, q, k, v, mask, slopes));
   OCHK(check_heads(dout, "dout", desc->queries, desc->heads, desc->head_dim, 2, false));

@@ -339,6 +339,21 @@ def test_attn_few_rows_over_a_long_axis(lens, key_lens, kind, cap):
         _attn_check(_attn_run(plan, mask, q, k, v, do, slopes), ref, f"{lens} over {key_lens}")
 
 
+@pytest.mark.parametrize("lens,key_lens,heads,kv,kind", [
+    ([1], [20011], 2, 1, "doc"),              # many parts for a row
+    ([1, 0, 3, 1], [9000, 40, 0, 7011], 4, 4, "doc"),   # parts that see nothing of a document
+    ([3000, 1, 2511], [90, 30, 81], 2, 1, "doc"),       # a document's rows fall to all parts
+    ([1025], [1025], 2, 2, "causal"),
+])
+def test_attn_many_parts(lens, key_lens, heads, kv, kind):
+    """The other side in up to 64 parts, for the keys every n-th tile of rows."""
+    log(f"case attention {lens} over {key_lens}, {heads} heads on {kv}, {kind} in many parts")
+    q, k, v, do, mask, rows = _case(lens, 3, heads, kv, 64, kind, 17, key_lens + [5])
+    plan = ops.Attn(len(rows), heads, 64, keys=sum(key_lens) + 5, kv_heads=kv)
+    ref = _attn_ref(q, k, v, do, rows, 0.125, 0.0, None)
+    _attn_check(_attn_run(plan, mask, q, k, v, do), ref, f"{lens} over {key_lens}")
+
+
 def test_attn_nan_in_one_part():
     """A value that is not finite in a long axis stays with what attends it."""
     q, k, v, do, mask, rows = _case([40, 9], 1, 2, 1, 64, "causal", 21, [3000, 1500])

@@ -130,6 +130,16 @@ def test_attn_descriptors(kw, status):
     _refused(ops.lib().pulse_attn_sizes(None, None, None), S.E_INVALID_ARG)
 
 
+@pytest.mark.parametrize("kw,ok", [
+    (dict(queries=1 << 24, heads=64), True), (dict(queries=1 << 24, heads=66), False),
+    (dict(keys=1 << 24, heads=64, kv_heads=64), True), (dict(queries=0, keys=1 << 24, heads=512,
+                                                             kv_heads=256), False),
+])
+def test_attn_launch_limit(kw, ok):
+    r = ops.lib().pulse_attn_sizes(_attn_desc(**kw), None, None)
+    assert r == S.OK if ok else r == S.E_SHAPE
+
+
 def _attn_calls(d, **kw):
     """Both calls with plausible arguments but for those given."""
     q, k = ops.Heads(P, 256, 64), ops.Heads(P, 128, 64)
