@@ -1,7 +1,9 @@
 // Masks of packed sequences (gfx950): per query row the interval of keys it
 // attends, and per tile of 64 rows the intervals that the attention kernels
 // use to skip key tiles (nothing attended) and to leave out the comparisons
-// (everything attended).  One wave per tile, one lane per row.
+// (everything attended).  One wave per tile, one lane per row, which finds its
+// document by bisection.  Bound by that chain of loads: 4096 rows of 16
+// documents 2.8 us, 131072 of 1500 4.5, where 2 MB are written.
 #include <limits.h>
 
 #include "okernels.hpp"

@@ -1,15 +1,21 @@
 // Rotary positions with several axes (gfx950): the pair (x0, x1) of pair p of
 // token t turns by pos[t][axis(p)] * freq[p].  A block forms the cosines and
 // sines of its tokens once, in LDS, and turns all their heads with them.
-// Bound by memory: x is read and y written once.
+// Bound by memory: x is read and y written once.  15795 tokens of 16 heads of
+// 64 in fp32, forward and backward: 55 us, 96 % of a copy's rate; 8192 tokens
+// of 32 heads of 88 in bf16: 47 us, 80 %; 512 tokens of 24 heads of 64: 3.9 us
+// in the kernel, a chain of load, angle, sine and store.
 #include "common.hpp"
 #include "okernels.hpp"
 
 namespace pulse {
 namespace {
 
-constexpr int RT = 4;         // tokens per block
-constexpr int MAXP = 128;     // pairs per head
+// Tokens per block: few heads want several, short calls want many blocks.  The
+// three calls above, in a graph: 3.8, 34.1, 46.8 us with 1, 3.9, 32.5, 46.5
+// with 2, 4.0, 32.7, 47.1 with 4, 5.1, 34.0, 53.0 with 8.
+constexpr int RT = 2;
+constexpr int MAXP = 128;  // pairs per head
 
 struct RopeGeo {
   int tokens, heads, hd, R, axes;
