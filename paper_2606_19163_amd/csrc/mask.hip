@@ -3,7 +3,7 @@
 // use to skip key tiles (nothing attended) and to leave out the comparisons
 // (everything attended).  One wave per tile, one lane per row, which finds its
 // document by bisection.  Bound by that chain of loads: 4096 rows of 16
-// documents 2.8 us, 131072 of 1500 4.5, where 2 MB are written.
+// documents 3.0 us, 131072 of 1500 4.6, where 2 MB are written.
 #include <limits.h>
 
 #include "okernels.hpp"

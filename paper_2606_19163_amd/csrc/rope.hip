@@ -2,9 +2,9 @@
 // token t turns by pos[t][axis(p)] * freq[p].  A block forms the cosines and
 // sines of its tokens once, in LDS, and turns all their heads with them.
 // Bound by memory: x is read and y written once.  15795 tokens of 16 heads of
-// 64 in fp32, forward and backward: 55 us, 96 % of a copy's rate; 8192 tokens
-// of 32 heads of 88 in bf16: 47 us, 80 %; 512 tokens of 24 heads of 64: 3.9 us
-// in the kernel, a chain of load, angle, sine and store.
+// 64 in fp32, forward and backward: 56 us, 95 % of a copy's rate; 8192 tokens
+// of 32 heads of 88 in bf16: 45 us, 85 %; 512 tokens of 24 heads of 64, forward:
+// 3.5 us in the kernel, a chain of load, angle, sine and store.
 #include "common.hpp"
 #include "okernels.hpp"
 
@@ -12,8 +12,9 @@ namespace pulse {
 namespace {
 
 // Tokens per block: few heads want several, short calls want many blocks.  The
-// three calls above, in a graph: 3.8, 34.1, 46.8 us with 1, 3.9, 32.5, 46.5
-// with 2, 4.0, 32.7, 47.1 with 4, 5.1, 34.0, 53.0 with 8.
+// short call, the bf16 one and the fp32 one, in a graph: 3.8, 34.1, 46.8 us
+// with 1, 3.9, 32.5, 46.5 with 2, 4.0, 32.7, 47.1 with 4, 5.1, 34.0, 53.0
+// with 8.
 constexpr int RT = 2;
 constexpr int MAXP = 128;  // pairs per head
 
