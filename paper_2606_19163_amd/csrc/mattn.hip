@@ -300,13 +300,16 @@ struct Score {
   }
 };
 
+// Intervals become addresses of keys, and a mask in memory may hold anything
+// (one that was never built, rows written since): they are cut to the keys
+// where they are read.
 struct Row {
   int lo, hi, pos;
 };
 __device__ __forceinline__ Row row_at(const Dev& a, int i) {
   if (i >= a.Tq) return Row{0, 0, 0};
   const pulse_mask_row r = a.rows[i];
-  return Row{r.lo, r.hi, r.pos};
+  return Row{min(max(r.lo, 0), a.Tk), min(max(r.hi, 0), a.Tk), r.pos};
 }
 
 // Bit e of the result: key k + e is attended, for e in 0..31.
@@ -325,7 +328,8 @@ __device__ __forceinline__ float keep_or(uint32_t on, float x, uint32_t other) {
 constexpr uint32_t NEG_INF = 0xff800000u;
 constexpr int PAST = 1 << 30;  // lo of a row past the last
 
-// mask entry of rows [r0, r0 + n), n a multiple of the table's tile
+// mask entry of rows [r0, r0 + n), n a multiple of the table's tile, its keys
+// within [0, Tk)
 __device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
   MaskTile b{1 << 30, 0, 0, 1 << 30};
   for (int r = r0; r < r0 + n && r < a.Tq; r += MASK_TILE) {
@@ -334,6 +338,8 @@ __device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
     b.all_lo = max(b.all_lo, t.all_lo);
     b.all_hi = min(b.all_hi, t.all_hi);
   }
+  b.lo = max(b.lo, 0);
+  b.hi = min(b.hi, a.Tk);
   return b;
 }
 

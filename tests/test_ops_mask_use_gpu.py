@@ -1,0 +1,88 @@
+"""Attention under masks that hold anything: what a mask's memory says never
+makes a kernel leave its tensors, whether or not the mask was ever built."""
+
+import pytest
+import torch
+
+from paper_2606_19163_amd import ops
+from paper_2606_19163_amd import stage as S
+
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def _heads(t):
+    return ops.Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _call(mask, q, k, v, do, plan):
+    """Forward and backward at the C boundary with `mask` int32 as it is.
+    Every output lies between guards."""
+    L, d = ops.lib(), plan.desc
+    tq, h, n = q.shape
+    pad = 64
+
+    def out(shape, dtype):
+        size = 1
+        for x in shape:
+            size *= x
+        size += -size % 16
+        buf = torch.full((size + 2 * pad,), 7.0, dtype=dtype, device="cuda")
+        guards.append((buf, size))
+        return buf[pad:pad + size][:shape.numel()].view(shape)
+
+    guards = []
+    o = out(q.shape, BF)
+    lse = out(torch.Size((h, tq)), torch.float32)
+    low = out(q.shape, BF)
+    dq, dk, dv = out(q.shape, BF), out(k.shape, BF), out(v.shape, BF)
+    ws = torch.empty(max(plan.fwd_bytes, plan.bwd_bytes, 256), dtype=torch.uint8, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    assert L.pulse_attn_forward(d, _heads(q), _heads(k), _heads(v), mask.data_ptr(), None, _heads(o),
+                                lse.data_ptr(), low.data_ptr(), ws.data_ptr(), ws.numel(),
+                                st) == S.OK
+    assert L.pulse_attn_backward(d, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o),
+                                 lse.data_ptr(), low.data_ptr(), mask.data_ptr(), None, _heads(dq),
+                                 _heads(dk), _heads(dv), ws.data_ptr(), ws.numel(), st) == S.OK
+    torch.cuda.synchronize()
+    for buf, size in guards:
+        assert (buf[:pad] == 7).all() and (buf[pad + size:] == 7).all()
+
+
+def _masks(tq, tk):
+    """int32 contents of a mask: rows (lo, hi, pos, doc), then tiles (lo, hi,
+    all_lo, all_hi)."""
+    tiles = (tq + 63) // 64
+    gen = torch.Generator().manual_seed(tq)
+    big = 2 ** 31 - 1
+    yield "anything", torch.randint(-big - 1, big, (4 * (tq + tiles),), generator=gen)
+    yield "near the keys", torch.randint(-200, tk + 200, (4 * (tq + tiles),), generator=gen)
+    rows = torch.tensor([-300, tk + 5000, 3, 0]).repeat(tq)
+    yield "wide", torch.cat([rows, torch.tensor([-300, tk + 5000, tk + 1, -1]).repeat(tiles)])
+    yield "past the keys", torch.cat([rows, torch.tensor([tk + 64, big, 0, 0]).repeat(tiles)])
+    yield "before the keys", torch.cat([rows, torch.tensor([-big, -1, -big, big]).repeat(tiles)])
+    yield "all ones", torch.full((4 * (tq + tiles),), -1)
+    yield "zero", torch.zeros(4 * (tq + tiles), dtype=torch.long)
+
+
+@pytest.mark.parametrize("tq,tk,heads,kv,dim,nan", [
+    (200, 130, 3, 1, 64, False), (200, 130, 2, 2, 128, True), (70, 3000, 2, 1, 88, True),
+    (1, 1, 1, 1, 64, False), (129, 70, 256, 256, 64, False),
+])
+def test_attn_keeps_to_its_tensors(tq, tk, heads, kv, dim, nan):
+    g = torch.Generator(device="cuda").manual_seed(dim)
+
+    def randn(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(BF)
+
+    plan = ops.Attn(tq, heads, dim, keys=tk, kv_heads=kv)
+    q, do = randn(tq, heads, dim), randn(tq, heads, dim)
+    k, v = randn(tk, kv, dim), randn(tk, kv, dim)
+    if nan:  # the kernels then look at intervals once more
+        for x in (k, v, do):
+            x[::7] = float("nan")
+    for name, m in _masks(tq, tk):
+        log(f"case attention {tq}x{tk}x{heads}x{dim} under a mask of {name}")
+        _call(m.to(torch.int32).cuda(), q, k, v, do, plan)
