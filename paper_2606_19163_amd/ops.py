@@ -215,7 +215,10 @@ class Rope:
 
 
 class Mask:
-    """Which of ``keys`` keys each of ``queries`` rows attends."""
+    """Which of ``keys`` keys each of ``queries`` rows attends.  Beside the
+    rows lies a table over them that attention reads, so :class:`Attn` takes
+    a mask only once ``build`` or ``from_rows`` has filled both: after writing
+    into ``rows``, call ``from_rows(mask.rows)``."""
 
     def __init__(self, queries, keys=None, docs=0, causal=False, device="cuda"):
         self.queries, self.keys = queries, queries if keys is None else keys
@@ -228,6 +231,18 @@ class Mask:
         self.ptr = self.buffer.data_ptr()
         #: [queries, 4]: lo, hi, pos, doc of every row
         self.rows = self.buffer[:4 * queries].view(queries, 4)
+        self.stamp = None
+
+    def _stamp(self):
+        """Changes with every torch operation that writes the rows."""
+        return 0 if self.buffer.is_inference() else self.buffer._version
+
+    def check(self):
+        """Refuse a mask that was not built, or written since."""
+        if self.queries and self.stamp is None:
+            _bad("the mask was not built: call build or from_rows first")
+        if self.queries and self.stamp != self._stamp():
+            _bad("the mask's rows were written since it was built: call from_rows")
 
     def build(self, offsets, key_offsets=None, prefix=None, stream=None):
         """From int32 ``offsets`` [docs + 1] on the GPU; returns ``rows``."""
@@ -238,6 +253,7 @@ class Mask:
                 self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
                 _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
                 _flat(prefix, "prefix", self.docs, torch.int32, dev), self.ptr, self.bytes, s))
+        self.stamp = self._stamp()
         return self.rows
 
     def from_rows(self, rows, stream=None):
@@ -248,6 +264,7 @@ class Mask:
             _check(lib().pulse_mask_from_rows(
                 self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
                 self.bytes, s))
+        self.stamp = self._stamp()
         return self.rows
 
 
@@ -289,6 +306,7 @@ class Attn:
     def _mask(self, mask, dev):
         if mask.queries != self.queries or mask.keys != self.keys:
             _bad(f"the mask is of {mask.queries} rows and {mask.keys} keys")
+        mask.check()
         if mask.buffer.get_device() != dev:
             _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
         return mask.ptr

@@ -86,3 +86,20 @@ def test_attn_keeps_to_its_tensors(tq, tk, heads, kv, dim, nan):
     for name, m in _masks(tq, tk):
         log(f"case attention {tq}x{tk}x{heads}x{dim} under a mask of {name}")
         _call(m.to(torch.int32).cuda(), q, k, v, do, plan)
+
+
+def test_attn_takes_a_mask_once_it_is_built():
+    q = torch.randn(70, 2, 64, device="cuda").to(BF)
+    plan, m = ops.Attn(70, 2, 64), ops.Mask(70, docs=1)
+    with pytest.raises(S.PulseError, match="not built"):
+        plan.forward(q, q, q, m)
+    m.build(torch.tensor([0, 70], dtype=torch.int32, device="cuda"))
+    o, saved = plan.forward(q, q, q, m)
+    m.rows[:, 1] = 60
+    with pytest.raises(S.PulseError, match="from_rows"):
+        plan.forward(q, q, q, m)
+    m.from_rows(m.rows)
+    p, _ = plan.forward(q, q, q, m)
+    m.build(torch.tensor([0, 70], dtype=torch.int32, device="cuda"))
+    again, _ = plan.forward(q, q, q, m)
+    assert torch.equal(o, again) and not torch.equal(o, p)
