@@ -139,13 +139,15 @@ pulse_status pulse_attn_sizes(const pulse_attn_desc* desc, size_t* forward_bytes
  * [heads] or NULL; they are constants of the model and get no gradient);
  * p = softmax over the keys that row i attends; o_i = sum_j p_ij v_j.  A row
  * that attends nothing gives o = 0.  Keys a row does not attend do not reach
- * it, NaN and infinities included.  lse [heads][Tq] receives log sum_j
- * exp(z_ij), -inf for empty rows.  o_low (bf16 [Tq][heads][head_dim],
- * contiguous, 16-byte aligned, or NULL) receives what the rounding of o left
- * out, for the backward.  Scores, sums and accumulators are fp32; p is rounded
- * to bf16 as the operand of p v.  `mask` is the buffer filled by
- * pulse_mask_build or _from_rows with the same Tq and Tk.  Outputs must not
- * overlap inputs.  The workspace is 256-byte aligned (NULL if it needs 0). */
+ * it, NaN and infinities included; what it attends does, here and in the
+ * gradients: where the formula gives no finite value, neither do they.
+ * lse [heads][Tq] receives log sum_j exp(z_ij), -inf for empty rows.  o_low
+ * (bf16 [Tq][heads][head_dim], contiguous, 16-byte aligned, or NULL) receives
+ * what the rounding of o left out, for the backward.  Scores, sums and
+ * accumulators are fp32; p is rounded to bf16 as the operand of p v.  `mask`
+ * is the buffer filled by pulse_mask_build or _from_rows with the same Tq and
+ * Tk.  Outputs must not overlap inputs.  The workspace is 256-byte aligned
+ * (NULL if it needs 0). */
 pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* q,
                                 const pulse_heads* k, const pulse_heads* v, const void* mask,
                                 const float* slopes, const pulse_heads* o, float* lse,

@@ -41,11 +41,13 @@ SOURCES = ["igemm2.hip", "norm.hip", "misc.hip", "probe.hip", "attn.hip",
            "tnorm.hip", "mask.hip", "rope.hip", "mattn.hip", "clip.hip", "stage.cpp",
            "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp"]
 
-# Attention's softmax takes maxima of MFMA results: with the IEEE mode bit
-# off (and no NaN semantics to keep) fmaxf needs no quieting copy of each
-# operand, which halves the VALU work of the row maxima.
-SOURCE_FLAGS = {"attn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
-                "mattn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}
+# The stages' attention takes maxima of MFMA results: with the IEEE mode bit
+# off fmaxf needs no quieting copy of each operand, which halves the VALU work
+# of the row maxima.  The compiler grants that only together with leave to
+# assume that there is no NaN.  attn.hip promises nothing about NaN and takes
+# both; mattn.hip does (what a row attends reaches it, NaN included) and takes
+# neither: its scores come out of an fma, whose maxima need no copy.
+SOURCE_FLAGS = {"attn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}
 
 
 # Host-only sanitizer build of the orchestration code (CPU tests only): each

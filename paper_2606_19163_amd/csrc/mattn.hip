@@ -68,12 +68,10 @@ struct Dev {  // device view of MattnArgs
   float *part0, *part1, *part_lse;
 };
 
-// The builtins, since the library functions behind threadIdx are built for
-// the IEEE mode that this file turns off and would stay calls.
 // The value is opaque: knowing its range, the compiler splits every LDS
 // address into parts that it keeps in registers across the loops, and spills.
 __device__ __forceinline__ int tid() {
-  int t = __builtin_amdgcn_workitem_id_x();
+  int t = threadIdx.x;
   asm("" : "+v"(t));
   return t;
 }
@@ -350,7 +348,7 @@ __device__ __forceinline__ MaskTile tiles_at(const Dev& a, int r0, int n) {
 // keys).
 __device__ __forceinline__ void block_of(const Dev& a, int tiles, int heads, bool last, int& tile,
                                          int& head, int& part) {
-  const int nb = tiles * heads * a.parts, bid = __builtin_amdgcn_workgroup_id_x();
+  const int nb = tiles * heads * a.parts, bid = blockIdx.x;
   const int q = nb >> 3, r = nb & 7, x = bid & 7;
   const int lb = x * q + (x < r ? x : r) + (bid >> 3);
   const int hp = lb / tiles;
@@ -1058,12 +1056,12 @@ __global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int hea
                                                    const float* p0, const float* p1, uint16_t* o0,
                                                    uint16_t* o1, long t0, long h0, long t1,
                                                    long h1) {
-  const bool y = __builtin_amdgcn_workgroup_id_y();
+  const bool y = blockIdx.y;
   const float* p = y ? p1 : p0;
   uint16_t* out = y ? o1 : o0;
   const long ts = y ? t1 : t0, hs = y ? h1 : h0;
   const long n = rows * heads * hd8;
-  const long e = (long)__builtin_amdgcn_workgroup_id_x() * 256 + tid();
+  const long e = (long)blockIdx.x * 256 + tid();
   if (e >= n) return;
   float o[8] = {};
   for (int i = 0; i < parts; ++i) {
@@ -1081,7 +1079,7 @@ __global__ __launch_bounds__(256) void k_mattn_sum(int parts, long rows, int hea
 // memory-bound
 __global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
   const long n = (long)a.Tq * a.H * a.hd8;
-  const long e = (long)__builtin_amdgcn_workgroup_id_x() * 256 + tid();
+  const long e = (long)blockIdx.x * 256 + tid();
   if (e >= n) return;
   const long rh = e / a.hd8;
   const int c = e - rh * a.hd8, row = rh / a.H, h = rh - (long)row * a.H;
