@@ -152,14 +152,21 @@ __device__ __forceinline__ bf16x8 cols32(const char* tile, int base, int d, int 
 __device__ __forceinline__ bool odd_lo(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }
 __device__ __forceinline__ bool odd_hi(uint32_t x) { return (x & 0x7f800000u) == 0x7f800000u; }
 
-// NaN and infinities among 8 values become 0; whether there were any
+// NaN and infinities among 8 values become 0, or with MAX infinities the
+// largest finite value of their sign; whether there were any
+template <bool MAX>
 __device__ __forceinline__ bool clean8(uint4& w) {
   uint32_t x[4] = {w.x, w.y, w.z, w.w};
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const bool lo = odd_lo(x[i]), hi = odd_hi(x[i]);
-    x[i] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+    if (MAX) {  // the value below an infinity, as an integer
+      if ((x[i] & 0x7fffu) == 0x7f80u) x[i] -= 1u;
+      if ((x[i] & 0x7fff0000u) == 0x7f800000u) x[i] -= 0x10000u;
+    }
+    const bool l0 = odd_lo(x[i]), h0 = odd_hi(x[i]);
+    x[i] &= (l0 ? 0xffff0000u : ~0u) & (h0 ? 0xffffu : ~0u);
     odd |= lo | hi;
   }
   w = uint4{x[0], x[1], x[2], x[3]};
@@ -242,8 +249,9 @@ struct Stage {
       *reinterpret_cast<uint4*>(
           t + (D == 96 ? toff<D>(r, c + 4 * u) : toff<D>(r + RR * u, c))) = v[u];
   }
-  // NaN and infinities become 0; whether there were any.  bad[row] = tag for
-  // the rows that held one.
+  // NaN and infinities become 0 (MAX: see clean8); whether there were any.
+  // bad[row] = tag for the rows that held one.
+  template <bool MAX = false>
   __device__ __forceinline__ bool clean(int* bad = nullptr, int tag = 0) {
     bool any = false;
 #pragma unroll
@@ -252,7 +260,7 @@ struct Stage {
     any = false;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const bool b = clean8(v[u]);
+      const bool b = clean8<MAX>(v[u]);
       any |= b;
       if (bad && b) bad[D == 96 ? r : r + RR * u] = tag;
     }
@@ -818,7 +826,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   // Pos: a row's place, from the block's first key
   __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT], Pos[2][KT];
   __shared__ __attribute__((aligned(16))) int Lo[2][KT], Hi[2][KT];
-  __shared__ int any_odd;
+  __shared__ int any_odd, any_odd_q;
   int tile, kh, part;
   block_of(a, (a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh, part);
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
@@ -826,7 +834,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int kb0 = tile * RB + grp * 32, key = kb0 + n;
   const float kfn = (float)(grp * 32 + n);  // as Pos
-  if (tid() == 0) any_odd = 0;
+  if (tid() == 0) any_odd = any_odd_q = 0;
   bf16x8 kf[D / 16], vf[D / 16];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
@@ -880,7 +888,10 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     const Score<CAP, BIAS> score(a, h);
     const MaskTile mt = a.tiles[qt];
     if (mt.all_lo > hits.k0 || mt.all_hi < hits.k1) {
-      sq.clean();  // a row with such a q has no finite lse
+      // A row with such a q has no finite lse, but under a cap, where infinite
+      // scores are +-cap: the largest finite q gives the same p and ds = 0,
+      // and dk its NaN (0 inf) at the end.
+      if (sq.template clean<CAP>() && CAP) any_odd_q = 1;
       if (sd.clean()) any_odd = 1;
     }
     sq.store(Qs);
@@ -997,23 +1008,28 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     }
     qt = qn;
   }
+  // o += the values left out of x (q or dout) in the rows that attend key j
+  const auto add_left = [&](const uint16_t* x, long xt, long xh, bool nan, int j, int c,
+                            float (&o)[8]) {
+    for (int i = 0; i < a.Tq; ++i) {
+      const Row r = row_at(a, i);
+      if (j < r.lo || j >= r.hi) continue;
+      for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
+        add_odd(o, *reinterpret_cast<const uint4*>(x + i * xt + g * xh + 8 * c), nan);
+    }
+  };
   float* mb = reinterpret_cast<float*>(smem);
   if constexpr (DK)
     write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt,
                      part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
-                     a.H / a.rep, a.hd8, [](int, int, float (&)[8]) {});
+                     a.H / a.rep, a.hd8, [&](int j, int c, float (&o)[8]) {
+                       if (CAP && any_odd_q) add_left(a.q, a.qt, a.qh, true, j, c, o);
+                     });
   if constexpr (DV)
     write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt,
                      part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
                      a.H / a.rep, a.hd8, [&](int j, int c, float (&o)[8]) {
-                       if (!any_odd) return;
-                       for (int i = 0; i < a.Tq; ++i) {
-                         const Row x = row_at(a, i);
-                         if (j < x.lo || j >= x.hi) continue;
-                         for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
-                           add_odd(o, *reinterpret_cast<const uint4*>(a.dout + i * a.dot +
-                                                                      g * a.doh + 8 * c), false);
-                       }
+                       if (any_odd) add_left(a.dout, a.dot, a.doh, false, j, c, o);
                      });
 }
 

@@ -77,18 +77,11 @@ def _values(x, name, value, cap, kind, dim, lens=LENS, heads=2, kv=1, key_lens=N
     _same_values(got, ref, f"{name} {value} cap {cap} {kind} dim {dim}")
 
 
-def _values_fit(name, value, cap):
-    # an infinite query under a cap has a test of its own
-    return not (name == "q" and cap and math.isinf(value))
-
-
 @pytest.mark.parametrize("dim", [64, 88, 128])
 @pytest.mark.parametrize("cap", [0.0, 5.0])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("name", ["q", "k", "v", "do"])
 def test_attn_values_reach_what_attends_them(name, value, cap, dim):
-    if not _values_fit(name, value, cap):
-        return
     log(f"case attention {name} {value} cap {cap} dim {dim}")
     for kind in ("doc", "causal"):
         # a one-token document, one inside a tile, one that crosses a tile
@@ -114,8 +107,7 @@ def test_attn_values_in_parts(name, x, value):
     """Few rows on a long axis, where the work is joined from parts."""
     log(f"case attention {name} {value} in parts")
     for cap in (0.0, 20.0):
-        if _values_fit(name, value, cap):
-            _values(x, name, value, cap, "causal", 64, [40, 9], 2, 1, [3000, 1500])
+        _values(x, name, value, cap, "causal", 64, [40, 9], 2, 1, [3000, 1500])
 
 
 def test_attn_values_over_many_rows():
