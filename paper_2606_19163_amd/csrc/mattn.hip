@@ -306,16 +306,18 @@ struct Score {
   }
 };
 
-// Intervals become addresses of keys, and a mask in memory may hold anything
-// (one that was never built, rows written since): they are cut to the keys
-// where they are read.
+// A mask in memory may hold anything (one that was never built, rows written
+// since).  Rows are compared with and are left as they are: cutting them waits
+// for their load, which the kernel over keys has in flight across a tile (1 x
+// 4096 tokens of 12 heads: 199 us instead of 165).  What becomes an address is
+// cut to the keys: tiles_at, and the walks over a row's keys.
 struct Row {
   int lo, hi, pos;
 };
 __device__ __forceinline__ Row row_at(const Dev& a, int i) {
   if (i >= a.Tq) return Row{0, 0, 0};
   const pulse_mask_row r = a.rows[i];
-  return Row{min(max(r.lo, 0), a.Tk), min(max(r.hi, 0), a.Tk), r.pos};
+  return Row{r.lo, r.hi, r.pos};
 }
 
 // Bit e of the result: key k + e is attended, for e in 0..31.
@@ -765,7 +767,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
                      const float e = finite_or_nan(a.lse[(long)h * a.Tq + row]) * 0.f;
 #pragma unroll
                      for (int t = 0; t < 8; ++t) o[t] += e;
-                     for (int j = x.lo; j < x.hi; ++j)
+                     for (int j = max(x.lo, 0); j < min(x.hi, a.Tk); ++j)
                        add_odd(o, *reinterpret_cast<const uint4*>(kbase + j * a.kt + 8 * c), true);
                    });
 }
