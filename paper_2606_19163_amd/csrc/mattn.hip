@@ -196,6 +196,46 @@ __device__ __forceinline__ void add_odd(float (&o)[8], uint4 w, bool nan) {
   }
 }
 
+// Whether nothing added to them can change 8 sums any more
+__device__ __forceinline__ bool all_nan(const float (&o)[8]) {
+  bool n = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) n &= o[i] != o[i];
+  return n;
+}
+
+// The tiles of keys (or rows) [lo, hi) that a block has left values out of: one
+// bit for every 2^shift keys, a tile or more.  What is added at the end is
+// looked for in these only, so that one NaN costs a tile and not all of them.
+// It lies in LDS with its range, of which the loops then hold nothing.
+struct Left {
+  uint32_t w[64];
+  int lo, hi, shift, any;
+  // before the barrier that precedes the first mark
+  __device__ __forceinline__ void init(int t, int first, int end) {
+    if (t < 64) w[t] = 0;
+    if (t == 0) {
+      lo = first, hi = end, any = 0, shift = 6;
+      while ((end - first - 1) >> shift >= 64 * 32) ++shift;
+    }
+  }
+  // some of the tile that starts at `first`
+  __device__ __forceinline__ void mark(int first) {
+    const int b = (first - lo) >> shift;
+    atomicOr(&w[b >> 5], 1u << (b & 31));
+    any = 1;
+  }
+  // f(first, end) of the marked tiles, until it returns false
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int i = 0; i < 64; ++i)
+      for (uint32_t x = w[i]; x; x &= x - 1) {
+        const int at = lo + ((32 * i + __builtin_ctz(x)) << shift);
+        if (!f(at, min(at + (1 << shift), hi))) return;
+      }
+  }
+};
+
 // x, or NaN where x is not finite
 __device__ __forceinline__ float finite_or_nan(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -463,7 +503,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ float ml[4][2][32];
-  __shared__ int any_odd;
+  __shared__ Left left;
   int tile, h, part;
   block_of(a, (a.Tq + RB - 1) / RB, a.H, true, tile, h, part);
   const int kh = h / a.rep;
@@ -482,6 +522,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     sk.load(a.Tk - klo, a.hd8);
     sv.load(a.Tk - klo, a.hd8);
   }
+  left.init(tid(), klo, khi);
   Score<CAP, BIAS> score(a, h);
   const bool neg = score.k < 0.f;
   // q carries the sign of the scale, so that a masked -inf stays one
@@ -498,14 +539,14 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   f32x16 acc[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) acc[d] = splat(0.f);
-  bool odd = false;  // this thread has left values out
+  __syncthreads();  // left
 
   int it = 0;
   for (int k0 = klo; k0 < khi; k0 += KT, ++it) {
     const int stage = (it & 1) * 4 * TILE;  // bytes
     uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     // this stage was last read two tiles ago, before the previous barrier
-    if (bt.all_lo > k0 || bt.all_hi < k0 + KT) odd |= sv.clean();
+    if ((bt.all_lo > k0 || bt.all_hi < k0 + KT) && sv.clean()) left.mark(k0);
     sk.store(Ks);
     sv.store(Ks + TILE);
     __syncthreads();
@@ -592,7 +633,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   }
 
   // merge: R = max ref, l = sum l 2^(ref - R), o = sum o 2^(ref - R) / l
-  if (tid() == 0) any_odd = 0;
   l += __shfl_xor(l, 32, 64);
   if (l == 0.f) ref = LOWEST;
   if (hl == 0) {
@@ -600,7 +640,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     ml[w][1][n] = l;
   }
   __syncthreads();  // also: every wave is done with the tiles
-  if (odd) any_odd = 1;
   float R = ref, t = 0.f;
 #pragma unroll
   for (int i = 0; i < SH; ++i) R = fmaxf(R, ml[grp * SH + i][0][n]);
@@ -622,10 +661,14 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
                    a.o + h * a.oh, a.ot, po, a.o_low ? a.o_low + (long)h * a.hd8 * 8 : nullptr,
                    tile * RB, a.Tq, a.H, a.hd8,
                    [&](int row, int c, float (&o)[8]) {
-                     if (!any_odd) return;
+                     if (!left.any) return;
                      const Row x = row_at(a, row);
-                     for (int j = max(x.lo, klo); j < min(x.hi, khi); ++j)
-                       add_odd(o, *reinterpret_cast<const uint4*>(vbase + j * a.vt + 8 * c), false);
+                     left.each([&](int first, int end) {
+                       for (int j = max(x.lo, first); j < min(x.hi, end); ++j)
+                         add_odd(o, *reinterpret_cast<const uint4*>(vbase + j * a.vt + 8 * c),
+                                 false);
+                       return !all_nan(o);
+                     });
                    });
 }
 
@@ -640,7 +683,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
   __shared__ int bad[2][KT];  // tile in which a key held a NaN or infinity
-  __shared__ int odd_at[2], any_odd;
+  __shared__ int odd_at[2];
+  __shared__ Left left;
   int tile, h, part;
   block_of(a, (a.Tq + RB - 1) / RB, a.H, true, tile, h, part);
   const int kh = h / a.rep;
@@ -661,7 +705,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   }
   if (tid() < 2 * KT) bad[tid() / KT][tid() % KT] = -1;
   if (tid() < 2) odd_at[tid()] = -1;
-  if (tid() == 0) any_odd = 0;
+  left.init(tid(), klo, khi);
   const Score<CAP, BIAS> score(a, h);
   const Row rw = row_at(a, qrow);
   const bool past = qrow >= a.Tq;  // nothing of such a row is kept
@@ -689,7 +733,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   f32x16 acc[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) acc[d] = splat(0.f);
-  __syncthreads();  // bad
+  __syncthreads();  // bad, left
 
   int it = 0;
   for (int k0 = klo; k0 < khi; k0 += KT, ++it) {
@@ -698,7 +742,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     const bool partly = bt.all_lo > k0 || bt.all_hi < k0 + KT;
     if (partly && sk.clean(bad[it & 1], it)) {
       odd_at[it & 1] = it;
-      any_odd = 1;
+      left.mark(k0);
     }
     sk.store(Ks);
     sv.store(Ks + TILE);
@@ -761,14 +805,18 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
                    part_of(a, a.part0, part, a.Tq, a.H, h), nullptr, tile * RB, a.Tq, a.H, a.hd8,
                    [&](int row, int c, float (&o)[8]) {
-                     if (!any_odd) return;
+                     if (!left.any) return;
                      const Row x = row_at(a, row);
                      if (x.hi <= x.lo) return;
                      const float e = finite_or_nan(a.lse[(long)h * a.Tq + row]) * 0.f;
 #pragma unroll
                      for (int t = 0; t < 8; ++t) o[t] += e;
-                     for (int j = max(x.lo, 0); j < min(x.hi, a.Tk); ++j)
-                       add_odd(o, *reinterpret_cast<const uint4*>(kbase + j * a.kt + 8 * c), true);
+                     left.each([&](int first, int end) {
+                       for (int j = max(x.lo, first); j < min(x.hi, end); ++j)
+                         add_odd(o, *reinterpret_cast<const uint4*>(kbase + j * a.kt + 8 * c),
+                                 true);
+                       return !all_nan(o);
+                     });
                    });
 }
 
@@ -828,7 +876,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   // Pos: a row's place, from the block's first key
   __shared__ __attribute__((aligned(16))) float Ls[2][KT], Ds[2][KT], Pos[2][KT];
   __shared__ __attribute__((aligned(16))) int Lo[2][KT], Hi[2][KT];
-  __shared__ int any_odd, any_odd_q;
+  __shared__ int odd_q, odd_do;  // whether values of q and dout were left out
+  __shared__ Left left;
   int tile, kh, part;
   block_of(a, (a.Tk + RB - 1) / RB, a.H / a.rep, false, tile, kh, part);
   const int lane = tid() & 63, w = tid() >> 6, n = lane & 31, hl = lane >> 5;
@@ -836,7 +885,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   const int rbase = rows_base<D>(lane) + shr * 64 * D, cbase = cols_base<D>(lane) + shr * 64 * D;
   const int kb0 = tile * RB + grp * 32, key = kb0 + n;
   const float kfn = (float)(grp * 32 + n);  // as Pos
-  if (tid() == 0) any_odd = any_odd_q = 0;
+  if (tid() == 0) odd_q = odd_do = 0;
+  left.init(tid(), 0, a.Tq);
   bf16x8 kf[D / 16], vf[D / 16];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
@@ -862,7 +912,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   hits.step = a.parts / a.head_parts;
   float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
   Row rn{0, 0, 0};
-  __syncthreads();  // any_odd
+  __syncthreads();  // left, odd_q, odd_do
 
   // (h, qt) is the tile in the registers, which goes to LDS next
   const auto fetch = [&](int h, int qt) {
@@ -893,8 +943,14 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       // A row with such a q has no finite lse, but under a cap, where infinite
       // scores are +-cap: the largest finite q gives the same p and ds = 0,
       // and dk its NaN (0 inf) at the end.
-      if (sq.template clean<CAP>() && CAP) any_odd_q = 1;
-      if (sd.clean()) any_odd = 1;
+      if (sq.template clean<CAP>() && CAP) {
+        left.mark(qt * KT);
+        odd_q = 1;
+      }
+      if (sd.clean()) {
+        left.mark(qt * KT);
+        odd_do = 1;
+      }
     }
     sq.store(Qs);
     sd.store(Qs + TILE);
@@ -1013,25 +1069,28 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   // o += the values left out of x (q or dout) in the rows that attend key j
   const auto add_left = [&](const uint16_t* x, long xt, long xh, bool nan, int j, int c,
                             float (&o)[8]) {
-    for (int i = 0; i < a.Tq; ++i) {
-      const Row r = row_at(a, i);
-      if (j < r.lo || j >= r.hi) continue;
-      for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
-        add_odd(o, *reinterpret_cast<const uint4*>(x + i * xt + g * xh + 8 * c), nan);
-    }
+    left.each([&](int first, int end) {
+      for (int i = first; i < end; ++i) {
+        const Row r = row_at(a, i);
+        if (j < r.lo || j >= r.hi) continue;
+        for (int g = h0; g < h0 + heads; ++g)
+          add_odd(o, *reinterpret_cast<const uint4*>(x + i * xt + g * xh + 8 * c), nan);
+      }
+      return !all_nan(o);
+    });
   };
   float* mb = reinterpret_cast<float*>(smem);
   if constexpr (DK)
     write_rows<D, G>(mb, dk, a.scale, a.dk + kh * a.dkh, a.dkt,
                      part_of(a, a.part0, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
                      a.H / a.rep, a.hd8, [&](int j, int c, float (&o)[8]) {
-                       if (CAP && any_odd_q) add_left(a.q, a.qt, a.qh, true, j, c, o);
+                       if (CAP && odd_q) add_left(a.q, a.qt, a.qh, true, j, c, o);
                      });
   if constexpr (DV)
     write_rows<D, G>(mb, dv, 1.f, a.dv + kh * a.dvh, a.dvt,
                      part_of(a, a.part1, part, a.Tk, a.H / a.rep, kh), nullptr, tile * RB, a.Tk,
                      a.H / a.rep, a.hd8, [&](int j, int c, float (&o)[8]) {
-                       if (any_odd) add_left(a.dout, a.dot, a.doh, false, j, c, o);
+                       if (odd_do) add_left(a.dout, a.dot, a.doh, false, j, c, o);
                      });
 }
 

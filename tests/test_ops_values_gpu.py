@@ -114,3 +114,41 @@ def test_attn_values_over_many_rows():
     """Many rows on few keys: the gradients of the keys come from parts."""
     for name, x in (("do", [1990]), ("q", [77]), ("k", [3]), ("v", [60])):
         _values(x, name, math.nan, 0.0, "doc", 64, [2600, 300], 1, 1, [33, 90])
+
+
+def _time(f):
+    """Best of three, in ms."""
+    best = math.inf
+    for _ in range(3):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("name,rows", [("do", [9000]), ("do", None), ("v", [200]), ("v", None),
+                                       ("k", [200]), ("k", None)])
+def test_attn_values_do_not_stall_a_step(name, rows):
+    """A diverged step (one NaN, or nothing but NaN) takes about as long as
+    another: 3 times is allowed for what looks at the values once more."""
+    t, h, d = 16384, 4, 64
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = {n: torch.randn(t, h, d, generator=gen, device="cuda").bfloat16()
+         for n in ("q", "k", "v", "do")}
+    mask = ops.Mask(t, docs=2, causal=True)
+    mask.build(torch.tensor([0, 15000, 16384], dtype=torch.int32, device="cuda"))
+    plan = ops.Attn(t, h, d)
+
+    def step():
+        o, saved = plan.forward(x["q"], x["k"], x["v"], mask)
+        plan.backward(x["do"], x["q"], x["k"], x["v"], o, saved, mask)
+
+    step()
+    clean = _time(step)
+    x[name][slice(None) if rows is None else rows] = math.nan
+    odd = _time(step)
+    log(f"  {name} {rows}: {clean:.2f} ms, with NaN {odd:.2f} ms")
+    assert odd <= 3 * clean
