@@ -25,6 +25,8 @@
 // (0 NaN = NaN).  In a tile that some row attends only in part, such values
 // are cleared in the operand that is summed over, and the rows that do attend
 // them get them at the end.
+#include <type_traits>
+
 #include "common.hpp"
 #include "okernels.hpp"
 
@@ -49,8 +51,8 @@ constexpr float GROW = 8.f;
 struct Dev {  // device view of MattnArgs
   int Tq, Tk, H, rep, hd8;
   float c1, c2;  // no cap: scale log2e; cap: scale / cap and cap log2e
-  float inv_c1;
-  float scale;
+  float inv_c1;  // no cap
+  float scale, cap;
   const uint16_t *q, *k, *v, *dout, *o_in;
   uint16_t *o, *dq, *dk, *dv;
   long qt, qh, kt, kh, vt, vh, ot, oh, dot, doh, dqt, dqh, dkt, dkh, dvt, dvh;
@@ -319,25 +321,47 @@ __device__ __forceinline__ void in_order() {
 }
 
 // Scores.  t = z - ref from a raw product, all in the log2 domain.
-template <bool CAP, bool BIAS>
+//
+// LOW: tanh(x) = 1 - 2 r with r = 1 / (1 + e^(2x)), so that 1 - tanh^2 =
+// 4 r (1 - r); e^(2x) may overflow to inf: r = 0.  Near 0 it is a difference
+// of numbers near 1, which leaves an error of 1.5e-7 cap whatever the score:
+// up to caps of CAP_LOW that is less than 2e-5.  ANY: beyond, scores of |x| <
+// 1/4 come from the series of tanh, whose error there is 1e-8 of the score
+// (8192 tokens of 16 heads, D = 64, forward and backward: 751 and 2161 us, LOW
+// 476 and 1506).
+enum Cap { NONE, LOW, ANY };
+constexpr float CAP_LOW = 128.f;
+
+template <int CAP, bool BIAS>
 struct Score {
-  float k;     // of the raw product: scale log2e; capped: scale / cap 2 log2e
-  float c2;    // cap log2e
-  float sl;    // slope log2e
+  float k;   // of the raw product: scale log2e; capped: scale / cap 2 log2e
+  float c2;  // cap log2e
+  float c1;  // ANY: scale / cap
+  float kz;  // ANY: scale log2e
+  float sl;  // slope log2e
   __device__ __forceinline__ Score(const Dev& a, int h) {
     k = CAP ? a.c1 * (2.f * LOG2E) : a.c1;
     c2 = a.c2;
+    c1 = a.c1;
+    kz = a.scale * LOG2E;
     sl = BIAS ? a.slopes[h] * LOG2E : 0.f;
   }
   // far: the signed distance |pos - j|; dz receives d z / d (scale q.k)
   __device__ __forceinline__ float operator()(float raw, float ref, float far, float& dz) const {
     float t;
     if (CAP) {
-      // tanh(x) = 1 - 2 r with r = 1 / (1 + e^(2x)), 1 - tanh^2 = 4 r (1 - r);
-      // e^(2x) may overflow to inf: r = 0
       const float r = __builtin_amdgcn_rcpf(1.f + ex2(raw * k));
       dz = 4.f * r * (1.f - r);
       t = fmaf(-2.f * c2, r, c2 - ref);
+      if (CAP == ANY) {
+        const float x = raw * c1, y = x * x;
+        // tanh(x) / x
+        float g = fmaf(y, 62.f / 2835.f, -17.f / 315.f);
+        g = fmaf(y, fmaf(y, fmaf(y, g, 2.f / 15.f), -1.f / 3.f), 1.f);
+        const bool near = y < 0.0625f;
+        dz = near ? fmaf(-y, g * g, 1.f) : dz;
+        t = near ? fmaf(raw * kz, g, -ref) : t;
+      }
     } else {
       dz = 1.f;
       t = fmaf(raw, k, -ref);
@@ -498,7 +522,7 @@ constexpr int SMEM = max_of(4 * KT * D * 2, MERGE);
 // at one wave per SIMD and were slower (D = 128: 637 TFLOP/s), 8 waves per block
 // too (16 x 256 tokens of 12 heads: 16.8 us instead of 13.1).
 // ---------------------------------------------------------------------------
-template <int D, int G, int WPE, bool CAP, bool BIAS>
+template <int D, int G, int WPE, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
@@ -524,9 +548,12 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
   }
   left.init(tid(), klo, khi);
   Score<CAP, BIAS> score(a, h);
+  // q carries the sign of the scale.  With the sign in the scale D = 64 needs
+  // 131 registers instead of 128, three waves per SIMD instead of four: 8192
+  // tokens of 16 heads 367 us, 347 so.
   const bool neg = score.k < 0.f;
-  // q carries the sign of the scale, so that a masked -inf stays one
   score.k = fabsf(score.k);
+  score.kz = fabsf(score.kz);
   const Row rw = row_at(a, qrow);
   const bool past = qrow >= a.Tq;  // nothing of such a row is kept
   bf16x8 qf[D / 16];
@@ -678,7 +705,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
 // of dp.  Bound as the forward is: about 1000 TFLOP/s over its three products
 // at 8192 tokens of 16 heads.
 // ---------------------------------------------------------------------------
-template <int D, int G, int WPE, bool CAP, bool BIAS>
+template <int D, int G, int WPE, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
@@ -869,7 +896,7 @@ struct Hits {
 // us, and two, 174, 8 x 1024 tokens).  About 900 TFLOP/s over its products.
 // The whole backward at 8192 tokens of 16 heads: D = 64 1020 us, D = 128 2150.
 // ---------------------------------------------------------------------------
-template <int D, int G, int WPE, bool CAP, bool BIAS, bool DK, bool DV>
+template <int D, int G, int WPE, int CAP, bool BIAS, bool DK, bool DV>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   constexpr int SH = 4 / G, RB = 32 * G, TILE = KT * D;
   __shared__ __attribute__((aligned(16))) char smem[SMEM<D>];
@@ -943,7 +970,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       // A row with such a q has no finite lse, but under a cap, where infinite
       // scores are +-cap: the largest finite q gives the same p and ds = 0,
       // and dk its NaN (0 inf) at the end.
-      if (sq.template clean<CAP>() && CAP) {
+      if (sq.template clean<(CAP > 0)>() && CAP) {
         left.mark(qt * KT);
         odd_q = 1;
       }
@@ -1097,12 +1124,15 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
 Dev view(const MattnArgs& a) {
   Dev d{};
   d.Tq = a.Tq, d.Tk = a.Tk, d.H = a.H, d.rep = a.H / a.KV, d.hd8 = a.hd / 8;
-  d.scale = a.scale;
+  d.scale = a.scale, d.cap = a.cap;
   d.c1 = a.cap > 0.f ? a.scale / a.cap : a.scale * LOG2E;
   d.c2 = a.cap * LOG2E;
-  // a scale of 0 becomes so small that scores vanish but a masked -inf stays
-  if (fabsf(d.c1) < 1e-30f) d.c1 = 1e-30f;
-  d.inv_c1 = 1.f / d.c1;
+  if (a.cap > 0.f) {  // of a cap so small that all but scores of 0 reach it
+    if (fabsf(d.c1) > 1e30f) d.c1 = copysignf(1e30f, d.c1);
+  } else {  // of a scale of 0, which is divided by: scores vanish all the same
+    if (fabsf(d.c1) < 1e-30f) d.c1 = 1e-30f;
+    d.inv_c1 = 1.f / d.c1;
+  }
   const auto in = [](const pulse_heads& x) { return static_cast<const uint16_t*>(x.ptr); };
   const auto out = [](const pulse_heads& x) { return static_cast<uint16_t*>(x.ptr); };
   d.q = in(a.q), d.k = in(a.k), d.v = in(a.v), d.dout = in(a.dout), d.o_in = in(a.o);
@@ -1236,7 +1266,7 @@ Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
   return x;
 }
 
-template <Pass P, int D, int G, int WPE, bool CAP, bool BIAS>
+template <Pass P, int D, int G, int WPE, int CAP, bool BIAS>
 hipError_t launch(const Dev& d, hipStream_t st) {
   constexpr int RB = 32 * G;
   const int rows = P == BWD_KV ? d.Tk : d.Tq, heads = P == BWD_KV ? d.H / d.rep : d.H;
@@ -1258,11 +1288,13 @@ hipError_t launch(const Dev& d, hipStream_t st) {
 
 template <Pass P, int D, int G, int WPE>
 hipError_t launch_mode(const Dev& d, hipStream_t st) {
-  const bool cap = d.c2 > 0.f;
-  if (cap && d.slopes) return launch<P, D, G, WPE, true, true>(d, st);
-  if (cap) return launch<P, D, G, WPE, true, false>(d, st);
-  if (d.slopes) return launch<P, D, G, WPE, false, true>(d, st);
-  return launch<P, D, G, WPE, false, false>(d, st);
+  const auto cap = [&](auto bias) {
+    constexpr bool B = decltype(bias)::value;
+    if (d.cap > CAP_LOW) return launch<P, D, G, WPE, ANY, B>(d, st);
+    if (d.cap > 0.f) return launch<P, D, G, WPE, LOW, B>(d, st);
+    return launch<P, D, G, WPE, NONE, B>(d, st);
+  };
+  return d.slopes ? cap(std::true_type{}) : cap(std::false_type{});
 }
 
 template <Pass P, int D>
