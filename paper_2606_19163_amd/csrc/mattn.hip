@@ -933,8 +933,9 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   hits.k0 = tile * RB;
   hits.k1 = tile * RB + RB;
   // the part's heads, and its share of the tiles of rows
-  const int heads = a.rep / a.head_parts;
-  const int h0 = kh * a.rep + part % a.head_parts * heads;
+  const int hp = part % a.head_parts;
+  const int h0 = kh * a.rep + a.rep * hp / a.head_parts;
+  const int heads = kh * a.rep + a.rep * (hp + 1) / a.head_parts - h0;
   hits.first = part / a.head_parts;
   hits.step = a.parts / a.head_parts;
   float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
@@ -1224,10 +1225,13 @@ struct Plan {
 // How a pass is spread over the GPU (256 CUs, two or three blocks each); us
 // of forward and backward in what follows.
 //
-// Shared key heads: a block over keys takes one of the heads that share them
-// where it would have to stream all of them, while there are fewer than 1024
-// blocks.  12240 tokens, 16 heads on 2, D = 64: 1505 with, 3135 without; at
-// 1024 blocks (65536 tokens in 128 documents, 16 heads on 4) 854 and 652.
+// Shared key heads: where there are fewer than 1024 blocks over keys, each takes
+// a part of the heads that share its keys, as many as leave 3072 blocks (one
+// at least).  12240 tokens, 16 heads on 2, D = 64: 1505 in parts, 3135 without;
+// at 1024 blocks (65536 tokens in 128 documents, 16 heads on 4) 854 and 652.
+// With 1024 left instead of 3072 the backward of 16384 tokens, 32 heads on 2,
+// D = 128, causal, takes 9442 instead of 8727.  There are fewer than 7168
+// blocks then, whose fp32 partials take less than 1 GB (128 channels).
 //
 // Blocks of 128 rows where there are 512 of them, else of 64.  4096 tokens of
 // 16 heads (512 blocks) in 16 documents: 15.9 + 39.1 with 128 rows, 16.4 +
@@ -1249,7 +1253,8 @@ Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
   Plan x{4, 1, 1};
   long blocks = (long)((rows + 127) / 128) * heads;
   if (p == BWD_KV && blocks < 1024 && H > KV) {
-    x.parts = x.head_parts = H / KV;
+    const long rep = H / KV, per = rep * blocks / 3072;
+    x.parts = x.head_parts = (int)(per > 1 ? (rep + per - 1) / per : rep);
     blocks *= x.parts;
   }
   if (blocks < 512) {

@@ -9,8 +9,9 @@ import torch
 
 from paper_2606_19163_amd import ops
 
-from gpu_util import log
-from test_ops_gpu import _attn_check, _attn_ref, _attn_run, _case
+from gpu_util import log, rel_l2
+from test_ops_gpu import ATTN_TOL, _attn_check, _attn_ref, _attn_run, _case
+from test_ops_values_gpu import _formulas
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,19 @@ def test_attn_key_blocks_that_walk_heads(dim, cap, bias):
     """1024 blocks of keys and more: each streams all the heads it serves."""
     log(f"case attention heads walked dim {dim}")
     _check([60, 69], 0, 1024, 512, dim, "causal", cap, bias)
+
+
+@pytest.mark.parametrize("heads,kv,dim,cap", [
+    (512, 64, 16, 0.0),   # 8 heads in parts of 2
+    (511, 73, 16, 20.0),  # 7 heads in parts of 1, 2, 2 and 2
+    (511, 73, 104, 0.0),
+])
+def test_attn_key_blocks_of_some_heads(heads, kv, dim, cap):
+    """Key heads whose query heads fall to parts of several heads each."""
+    log(f"case attention {heads} heads on {kv} in parts, dim {dim}")
+    q, k, v, do, mask, rows = _case([64] * 25, 1, heads, kv, dim, "doc", dim)
+    plan = ops.Attn(len(rows), heads, dim, kv_heads=kv, cap=cap)
+    ref = _formulas(q, k, v, do, rows, 1 / math.sqrt(dim), cap)
+    got = _attn_run(plan, mask, q, k, v, do)
+    for n in ("o", "dq", "dk", "dv"):
+        assert rel_l2(got[n], ref[n]) <= ATTN_TOL, n
