@@ -38,9 +38,10 @@ extern "C" {
 
 /* Heads of a token-major or head-major tensor: element (t, h, c) lies at
  * ptr + t * token_stride + h * head_stride + c (strides in elements).  ptr is
- * 16-byte aligned and both strides are multiples of 16 bytes and >= 0.  The
- * elements of an output must not overlap one another: one stride is at least
- * the head dimension and the other at least the extent of that whole axis. */
+ * 16-byte aligned and both strides are multiples of 16 bytes, >= 0 and such
+ * that neither axis extends over more than 2^47 elements.  The elements of an
+ * output must not overlap one another: one stride is at least the head
+ * dimension and the other at least the extent of that whole axis. */
 typedef struct {
   void* ptr;
   int64_t token_stride, head_stride;

@@ -37,6 +37,7 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 
 constexpr int MAX_TOKENS = 1 << 24;
 constexpr int MAX_HEADS = 1024;
+constexpr int64_t MAX_EXTENT = INT64_C(1) << 47;
 
 // a [tokens][heads][dim] view; `out`: written, so its elements are distinct
 pulse_status check_heads(const pulse_heads* x, const char* name, int tokens, int heads, int dim,
@@ -50,6 +51,10 @@ pulse_status check_heads(const pulse_heads* x, const char* name, int tokens, int
     return ofail(PULSE_E_INVALID_ARG, "%s has a stride below 0 or above 2^40", name);
   if (ts * esz % 16 || hs * esz % 16)
     return ofail(PULSE_E_INVALID_ARG, "%s has a stride that is not a multiple of 16 bytes", name);
+  // no more than an address space, so that neither these sums nor the kernels'
+  // offsets wrap around
+  if ((tokens > 1 && ts > MAX_EXTENT / (tokens - 1)) || (heads > 1 && hs > MAX_EXTENT / (heads - 1)))
+    return ofail(PULSE_E_INVALID_ARG, "%s extends over more than 2^47 elements", name);
   if (out) {
     const bool th = (heads == 1 || hs >= dim) && (tokens == 1 || ts >= (heads - 1) * hs + dim);
     const bool ht = (tokens == 1 || ts >= dim) &&
