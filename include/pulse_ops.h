@@ -158,7 +158,9 @@ pulse_status pulse_attn_forward(const pulse_attn_desc* desc, const pulse_heads* 
  * rounded stands for the output in rowsum(dout o), which costs dq and dk about
  * a tenth of their accuracy).  ds is rounded to bf16 as an operand.  dk and dv
  * sum over the query heads that share a key head; keys nobody attends get 0,
- * rows that attend nothing get dq = 0 and give nothing. */
+ * rows that attend nothing get dq = 0 and give nothing.  `mask` still holds what
+ * the forward ran under: pulse_mask_build and _from_rows overwrite a mask in
+ * place, so batches in flight need one each. */
 pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads* dout,
                                  const pulse_heads* q, const pulse_heads* k,
                                  const pulse_heads* v, const pulse_heads* o, const float* lse,

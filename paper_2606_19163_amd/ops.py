@@ -218,7 +218,9 @@ class Mask:
     """Which of ``keys`` keys each of ``queries`` rows attends.  Beside the
     rows lies a table over them that attention reads, so :class:`Attn` takes
     a mask only once ``build`` or ``from_rows`` has filled both: after writing
-    into ``rows``, call ``from_rows(mask.rows)``."""
+    into ``rows``, call ``from_rows(mask.rows)``.  Both overwrite the mask in
+    place: with several batches between forward and backward, each needs a
+    mask of its own."""
 
     def __init__(self, queries, keys=None, docs=0, causal=False, device="cuda"):
         self.queries, self.keys = queries, queries if keys is None else keys
@@ -231,7 +233,11 @@ class Mask:
         self.ptr = self.buffer.data_ptr()
         #: [queries, 4]: lo, hi, pos, doc of every row
         self.rows = self.buffer[:4 * queries].view(queries, 4)
-        self.stamp = None
+        self.stamp, self.serial = None, 0
+
+    def _built(self):
+        self.stamp = self._stamp()
+        self.serial += 1
 
     def _stamp(self):
         """Changes with every torch operation that writes the rows."""
@@ -253,7 +259,7 @@ class Mask:
                 self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
                 _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
                 _flat(prefix, "prefix", self.docs, torch.int32, dev), self.ptr, self.bytes, s))
-        self.stamp = self._stamp()
+        self._built()
         return self.rows
 
     def from_rows(self, rows, stream=None):
@@ -264,16 +270,16 @@ class Mask:
             _check(lib().pulse_mask_from_rows(
                 self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
                 self.bytes, s))
-        self.stamp = self._stamp()
+        self._built()
         return self.rows
 
 
 class Saved:
     """What a forward leaves for its backward beside the output: the scores'
-    log sum exp (``lse``, fp32 [heads, queries]) and what the rounding of the
-    output left out."""
+    log sum exp (``lse``, fp32 [heads, queries]), what the rounding of the
+    output left out, and which mask it ran under."""
 
-    __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr")
+    __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr", "mask", "serial")
 
     def __init__(self, heads, queries, head_dim, device):
         n = -(-heads * queries // 4) * 4  # the second part is 16-byte aligned
@@ -282,6 +288,7 @@ class Saved:
         self.shape = (heads, queries, head_dim)
         self.lse_ptr = self.buffer.data_ptr()
         self.low_ptr = self.lse_ptr + 4 * n
+        self.mask, self.serial = None, 0
 
     @property
     def lse(self):
@@ -329,6 +336,7 @@ class Attn:
                 _flat(slopes, "slopes", self.heads, torch.float32, dev),
                 _heads(out, "out", self.qs, bf, dev), *self._saved(saved, dev),
                 ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
+        saved.mask, saved.serial = mask, mask.serial
         return out, saved
 
     def _saved(self, saved, dev):
@@ -341,6 +349,10 @@ class Attn:
     def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
         bf = torch.bfloat16
+        if saved.mask is None:
+            _bad("saved is of no forward")
+        if saved.mask is mask and saved.serial != mask.serial:
+            _bad("the mask was built again since this forward: batches in flight need one each")
         with _On(stream) as (dev, s):
             if out is None:
                 out = [torch.empty(n, dtype=bf, device=q.device)

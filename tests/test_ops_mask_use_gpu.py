@@ -103,3 +103,28 @@ def test_attn_takes_a_mask_once_it_is_built():
     m.build(torch.tensor([0, 70], dtype=torch.int32, device="cuda"))
     again, _ = plan.forward(q, q, q, m)
     assert torch.equal(o, again) and not torch.equal(o, p)
+
+
+def _off(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def test_attn_batches_in_flight_have_a_mask_each():
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, do = (torch.randn(90, 2, 64, generator=g, device="cuda").to(BF) for _ in range(2))
+    plan, m, n = ops.Attn(90, 2, 64), ops.Mask(90, docs=2), ops.Mask(90, docs=2)
+    m.build(_off(0, 30, 90))
+    o, saved = plan.forward(q, q, q, m)
+    want = plan.backward(do, q, q, q, o, saved, m)
+    # one mask for two batches: the first one's backward would use the second's
+    m.build(_off(0, 70, 90))
+    plan.forward(q, q, q, m)
+    with pytest.raises(S.PulseError, match="built again"):
+        plan.backward(do, q, q, q, o, saved, m)
+    # a forward again, into the same saved, or another mask of the same rows
+    m.build(_off(0, 30, 90))
+    o, saved = plan.forward(q, q, q, m, saved=saved)
+    n.build(_off(0, 30, 90))
+    for mask in (m, n):
+        for x, y in zip(plan.backward(do, q, q, q, o, saved, mask), want):
+            assert torch.equal(x, y)

@@ -45,3 +45,22 @@ def test_a_mask_made_in_inference_mode():
         _attn(m)
     m.stamp = m._stamp()
     assert _attn(m) == m.ptr
+
+
+def _backward(plan, saved, mask):
+    t = torch.zeros(plan.qs, dtype=torch.bfloat16)
+    plan.backward(t, t, t, t, t, saved, mask)
+
+
+def test_a_backward_under_a_mask_built_again_is_refused():
+    """Refused before any GPU is looked for."""
+    m = ops.Mask(70, docs=2, device="cpu")
+    plan = ops.Attn(70, 2, 64)
+    saved = ops.Saved(2, 70, 64, "cpu")
+    with pytest.raises(S.PulseError, match="no forward"):
+        _backward(plan, saved, m)
+    m._built()
+    saved.mask, saved.serial = m, m.serial  # as a forward leaves it
+    m._built()
+    with pytest.raises(S.PulseError, match="built again"):
+        _backward(plan, saved, m)
