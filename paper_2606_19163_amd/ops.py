@@ -10,8 +10,10 @@ Argument marshalling only: every step runs in the library's HIP kernels, and
 loading fails loudly when the library has not been built.  Tensors are
 ``[tokens, heads, head_dim]`` with the last axis contiguous; the other two may
 be strided (the heads inside a projection's output, or head-major storage).
-Work is enqueued on ``stream`` (default: torch's current one), and what a call
-allocates belongs to that stream, so an object may be used from several.
+Gradients come from the ``backward`` methods; autograd sees none of this, so a
+call refuses inputs that require a gradient where torch records one.  Work is
+enqueued on ``stream`` (default: torch's current one), and what a call allocates
+belongs to that stream, so an object may be used from several.
 """
 
 from __future__ import annotations
@@ -140,6 +142,15 @@ def _flat(t, name, n, dtype, dev):
     return t.data_ptr()
 
 
+def _by_hand(**inputs):
+    """Refuse inputs whose gradients the caller expects from autograd."""
+    if torch.is_grad_enabled():
+        for name, t in inputs.items():
+            if t is not None and t.requires_grad:
+                _bad(f"{name} requires a gradient, which autograd would not get: call this under "
+                     "torch.no_grad() and use backward")
+
+
 class _On:
     """(device, stream handle) of torch's current stream, or of `stream` made
     current, so that what a call allocates belongs to the stream it runs on."""
@@ -207,10 +218,12 @@ class Rope:
 
     def forward(self, x, pos, freq, out=None, stream=None):
         """x turned by its positions; ``out`` may be x."""
+        _by_hand(x=x, pos=pos, freq=freq)
         return self._run(x, pos, freq, out, 0, stream)
 
     def backward(self, dout, pos, freq, out=None, stream=None):
         """The gradient of ``forward``'s input from that of its output."""
+        _by_hand(dout=dout)
         return self._run(dout, pos, freq, out, 1, stream)
 
 
@@ -322,6 +335,7 @@ class Attn:
         """(o, saved): o [queries, heads, head_dim] and what the backward needs
         beside it (into ``saved`` of an earlier call, if given)."""
         bf = torch.bfloat16
+        _by_hand(q=q, k=k, v=v, slopes=slopes)
         with _On(stream) as (dev, s):
             if out is None:
                 out = torch.empty(self.qs, dtype=bf, device=q.device)
@@ -349,6 +363,7 @@ class Attn:
     def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
         bf = torch.bfloat16
+        _by_hand(dout=dout)
         if saved.mask is None:
             _bad("saved is of no forward")
         if saved.mask is mask and saved.serial != mask.serial:
