@@ -331,15 +331,21 @@ class Attn:
             _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
         return mask.ptr
 
-    def forward(self, q, k, v, mask, slopes=None, out=None, saved=None, stream=None):
+    def forward(self, q, k, v, mask, slopes=None, out=None, saved=None, stream=None, keep=True):
         """(o, saved): o [queries, heads, head_dim] and what the backward needs
-        beside it (into ``saved`` of an earlier call, if given)."""
+        beside it (into ``saved`` of an earlier call, if given).  Without
+        ``keep`` nothing is kept for a backward and saved is None."""
         bf = torch.bfloat16
         _by_hand(q=q, k=k, v=v, slopes=slopes)
+        if saved is not None and not keep:
+            _bad("saved is given, and nothing is to be kept")
         with _On(stream) as (dev, s):
             if out is None:
                 out = torch.empty(self.qs, dtype=bf, device=q.device)
-            if saved is None:
+            lse = None
+            if not keep:
+                lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
+            elif saved is None:
                 saved = Saved(self.heads, self.queries, self.dim, q.device)
             ws = None
             if self.fwd_bytes:
@@ -348,9 +354,11 @@ class Attn:
                 self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
                 _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev),
                 _flat(slopes, "slopes", self.heads, torch.float32, dev),
-                _heads(out, "out", self.qs, bf, dev), *self._saved(saved, dev),
+                _heads(out, "out", self.qs, bf, dev),
+                *(self._saved(saved, dev) if keep else (lse.data_ptr(), None)),
                 ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
-        saved.mask, saved.serial = mask, mask.serial
+        if keep:
+            saved.mask, saved.serial = mask, mask.serial
         return out, saved
 
     def _saved(self, saved, dev):
