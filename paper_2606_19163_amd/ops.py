@@ -13,7 +13,8 @@ be strided (the heads inside a projection's output, or head-major storage).
 Gradients come from the ``backward`` methods; autograd sees none of this, so a
 call refuses inputs that require a gradient where torch records one.  Work is
 enqueued on ``stream`` (default: torch's current one), and what a call allocates
-belongs to that stream, so an object may be used from several.
+belongs to that stream.  An object may be used from several: the caller orders
+them, and the memory that an object holds is kept until all are done with it.
 """
 
 from __future__ import annotations
@@ -171,6 +172,17 @@ class _On:
             self.ctx.__exit__(*exc)
 
 
+def _home(t):
+    """The stream that the allocator thinks `t` is used on."""
+    return _raw_stream(t.get_device()) if t.is_cuda else None
+
+
+def _used_on(t, home, dev, s):
+    """`t` is used on stream s: its memory is not handed on before that is done."""
+    if s != home:
+        t.record_stream(torch.cuda.current_stream(dev))
+
+
 def rope_freqs(axis_dim, base=10000.0, device="cuda"):
     """freq[p] = base^(-2 i / n) for pair i of an axis of n channels, the axes
     one after another (fp32)."""
@@ -243,7 +255,7 @@ class Mask:
         _check(lib().pulse_mask_sizes(ctypes.byref(self.desc), ctypes.byref(n)))
         self.bytes = n.value
         self.buffer = torch.empty(max(n.value // 4, 4), dtype=torch.int32, device=device)
-        self.ptr = self.buffer.data_ptr()
+        self.ptr, self.home = self.buffer.data_ptr(), _home(self.buffer)
         #: [queries, 4]: lo, hi, pos, doc of every row
         self.rows = self.buffer[:4 * queries].view(queries, 4)
         self.stamp, self.serial = None, 0
@@ -268,6 +280,7 @@ class Mask:
         with _On(stream) as (dev, s):
             if self.buffer.get_device() != dev:
                 _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
+            _used_on(self.buffer, self.home, dev, s)
             _check(lib().pulse_mask_build(
                 self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
                 _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
@@ -280,6 +293,7 @@ class Mask:
         with _On(stream) as (dev, s):
             if self.buffer.get_device() != dev:
                 _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
+            _used_on(self.buffer, self.home, dev, s)
             _check(lib().pulse_mask_from_rows(
                 self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
                 self.bytes, s))
@@ -292,7 +306,7 @@ class Saved:
     log sum exp (``lse``, fp32 [heads, queries]), what the rounding of the
     output left out, and which mask it ran under."""
 
-    __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr", "mask", "serial")
+    __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr", "home", "mask", "serial")
 
     def __init__(self, heads, queries, head_dim, device):
         n = -(-heads * queries // 4) * 4  # the second part is 16-byte aligned
@@ -301,7 +315,7 @@ class Saved:
         self.shape = (heads, queries, head_dim)
         self.lse_ptr = self.buffer.data_ptr()
         self.low_ptr = self.lse_ptr + 4 * n
-        self.mask, self.serial = None, 0
+        self.home, self.mask, self.serial = _home(self.buffer), None, 0
 
     @property
     def lse(self):
@@ -323,12 +337,13 @@ class Attn:
         self.qs = (queries, heads, head_dim)
         self.ks = (self.keys, self.kv, head_dim)
 
-    def _mask(self, mask, dev):
+    def _mask(self, mask, dev, s):
         if mask.queries != self.queries or mask.keys != self.keys:
             _bad(f"the mask is of {mask.queries} rows and {mask.keys} keys")
         mask.check()
         if mask.buffer.get_device() != dev:
             _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
+        _used_on(mask.buffer, mask.home, dev, s)
         return mask.ptr
 
     def forward(self, q, k, v, mask, slopes=None, out=None, saved=None, stream=None, keep=True):
@@ -352,20 +367,21 @@ class Attn:
                 ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
             _check(lib().pulse_attn_forward(
                 self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
-                _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev),
+                _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev, s),
                 _flat(slopes, "slopes", self.heads, torch.float32, dev),
                 _heads(out, "out", self.qs, bf, dev),
-                *(self._saved(saved, dev) if keep else (lse.data_ptr(), None)),
+                *(self._saved(saved, dev, s) if keep else (lse.data_ptr(), None)),
                 ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
         if keep:
             saved.mask, saved.serial = mask, mask.serial
         return out, saved
 
-    def _saved(self, saved, dev):
+    def _saved(self, saved, dev, s):
         if saved.shape != (self.heads, self.queries, self.dim):
             _bad(f"saved is of heads, queries and head_dim {saved.shape}")
         if saved.buffer.get_device() != dev:
             _bad(f"saved is on {saved.buffer.device}, not on the current GPU")
+        _used_on(saved.buffer, saved.home, dev, s)
         return saved.lse_ptr, saved.low_ptr
 
     def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
@@ -387,7 +403,7 @@ class Attn:
             _check(lib().pulse_attn_backward(
                 self.desc, _heads(dout, "dout", self.qs, bf, dev), _heads(q, "q", self.qs, bf, dev),
                 _heads(k, "k", self.ks, bf, dev), _heads(v, "v", self.ks, bf, dev),
-                _heads(o, "o", self.qs, bf, dev), *self._saved(saved, dev), self._mask(mask, dev),
+                _heads(o, "o", self.qs, bf, dev), *self._saved(saved, dev, s), self._mask(mask, dev, s),
                 _flat(slopes, "slopes", self.heads, torch.float32, dev),
                 _heads(dq, "dq", self.qs, bf, dev), _heads(dk, "dk", self.ks, bf, dev),
                 _heads(dv, "dv", self.ks, bf, dev),
@@ -424,6 +440,7 @@ class GradClip:
         n = ctypes.c_size_t()
         _check(lib().pulse_clip_sizes(self.h, ctypes.byref(n)))
         self.workspace = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self.home = _home(self.workspace)
         _check(lib().pulse_clip_bind(self.h, self.workspace.data_ptr(), n.value,
                                      torch.cuda.current_stream().cuda_stream))
 
@@ -439,6 +456,7 @@ class GradClip:
         """Clip to ``max_norm``; returns the norm before it, fp32 [1].  Calls
         share one workspace: order the streams that they run on."""
         with _On(stream) as (dev, s):
+            _used_on(self.workspace, self.home, dev, s)
             if norm is None:
                 norm = torch.empty(1, dtype=torch.float32, device=self.device)
             _check(lib().pulse_clip_run(self.h, max_norm, eps,

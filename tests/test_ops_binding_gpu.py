@@ -55,3 +55,41 @@ def test_forward_that_keeps_nothing(queries, keys, dim):
     assert used <= sum(-(-p // 512) * 512 for p in parts)  # the allocator's blocks
     with pytest.raises(S.PulseError, match="nothing is to be kept"):
         plan.forward(q, k, v, m, saved=saved, keep=False)
+
+
+@pytest.mark.parametrize("what", ["mask", "saved", "clip"])
+def test_memory_of_objects_used_on_another_stream(what):
+    """It is not handed on while that stream has work with it ahead."""
+    t = 2048
+    q = torch.randn(t, 4, 64, device="cuda").to(BF)
+    off = torch.tensor([0, t], dtype=torch.int32, device="cuda")
+    plan = ops.Attn(t, 4, 64)
+    side = torch.cuda.Stream()
+    keep = _mask(0, t)
+    o, s0 = plan.forward(q, q, q, keep)
+    out = [torch.empty_like(q) for _ in range(3)]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held = {"mask": ops.Mask(t, docs=1), "saved": ops.Saved(4, t, 64, "cuda"),
+            "clip": ops.GradClip([torch.ones(1 << 20, device="cuda")])}
+    held["mask"].build(off)
+    plan.forward(q, q, q, keep, saved=held["saved"])
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    if what == "mask":
+        plan.forward(q, q, q, held["mask"], out=out[0], saved=s0, stream=side)
+        s0.mask = None  # it would keep the mask
+    elif what == "saved":
+        plan.backward(q, q, q, q, o, held["saved"], keep, out=out, stream=side)
+    else:
+        norm = torch.empty(1, device="cuda")
+        held["clip"].run(1.0, norm=norm, stream=side)
+    busy = not side.query()
+    x = held.pop(what)
+    buf = x.workspace if what == "clip" else x.buffer
+    ptr, numel = buf.data_ptr(), buf.numel() * buf.element_size()
+    del x, buf
+    again = torch.empty(numel, dtype=torch.uint8, device="cuda").data_ptr()
+    torch.cuda.synchronize()
+    assert busy and again != ptr

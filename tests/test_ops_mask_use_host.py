@@ -10,7 +10,7 @@ from test_ops_host import built  # noqa: F401  (builds the library)
 
 
 def _attn(mask):
-    return ops.Attn(mask.queries, 2, 64, keys=mask.keys)._mask(mask, mask.buffer.get_device())
+    return ops.Attn(mask.queries, 2, 64, keys=mask.keys)._mask(mask, mask.buffer.get_device(), None)
 
 
 def test_a_mask_that_was_not_built_is_refused():
