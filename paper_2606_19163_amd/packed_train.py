@@ -50,8 +50,13 @@ class PackedAttention:
         self.clip = ops.GradClip(self.grads.values())
 
     def begin(self, lens=None):
-        """The batch's mask: every layer of a model would share it."""
-        lens = self.lens if lens is None else lens
+        """The batch's mask: every layer of a model would share it.  ``lens``:
+        as many documents of other lengths; tokens past them are padding."""
+        lens = self.lens if lens is None else list(lens)
+        if len(lens) != len(self.lens) or min(lens, default=0) < 0 or sum(lens) > self.tokens:
+            raise ValueError(f"{len(self.lens)} documents of {self.tokens} tokens at most, "
+                             f"not {lens}")
+        self.lens = lens
         off = torch.tensor([0] + lens, device="cuda").cumsum(0).int()
         return self.mask.build(off)
 
@@ -82,7 +87,8 @@ class PackedAttention:
         return dh + dqkv @ w["qkv"]
 
     def step(self, x, target, lr, max_norm):
-        """One descent step on the mean square error; (loss, gradient norm)."""
+        """One descent step on the square error, summed over channels and averaged
+        over tokens; (its mean over both, gradient norm)."""
         for g in self.grads.values():
             g.zero_()
         h, state = self.forward(x)
@@ -97,15 +103,18 @@ class PackedAttention:
 
 def batch(layer, seed):
     """Tokens and targets: every token plus its document's mean."""
+    layer.mask.check()  # layer.begin() was called
     gen = torch.Generator(device="cuda").manual_seed(seed)
     width = layer.h * layer.d
     x = torch.randn(layer.tokens, width, generator=gen, device="cuda")
     centre = torch.randn(len(layer.lens), width, generator=gen, device="cuda")
     doc = layer.mask.rows[:, 3].long()  # the mask knows each row's document
-    x = (x + centre[doc]).bfloat16()
-    mean = torch.zeros_like(centre).index_add_(0, doc, x.float())
-    mean /= torch.tensor(layer.lens, device="cuda")[:, None]
-    return x, x.float() + mean[doc]
+    inside = (doc >= 0)[:, None].float()  # padding has none
+    doc = doc.clamp(min=0)
+    x = (x + centre[doc] * inside).bfloat16()
+    mean = torch.zeros_like(centre).index_add_(0, doc, x.float() * inside)
+    mean /= torch.tensor(layer.lens, device="cuda").clamp(min=1)[:, None]
+    return x, x.float() + mean[doc] * inside
 
 
 def main(argv=None):
