@@ -143,13 +143,16 @@ def _flat(t, name, n, dtype, dev):
     return t.data_ptr()
 
 
-def _by_hand(**inputs):
-    """Refuse inputs whose gradients the caller expects from autograd."""
-    if torch.is_grad_enabled():
-        for name, t in inputs.items():
-            if t is not None and t.requires_grad:
-                _bad(f"{name} requires a gradient, which autograd would not get: call this under "
-                     "torch.no_grad() and use backward")
+def _by_hand(*inputs):
+    """Refuse inputs, (name, tensor) each, whose gradients the caller expects
+    from autograd."""
+    for name, t in inputs:
+        if t is not None and t.requires_grad:
+            _bad(f"{name} requires a gradient, which autograd would not get: call this under "
+                 "torch.no_grad() and use backward")
+
+
+_grad_on = torch.is_grad_enabled
 
 
 class _On:
@@ -230,12 +233,14 @@ class Rope:
 
     def forward(self, x, pos, freq, out=None, stream=None):
         """x turned by its positions; ``out`` may be x."""
-        _by_hand(x=x, pos=pos, freq=freq)
+        if _grad_on():
+            _by_hand(("x", x), ("pos", pos), ("freq", freq))
         return self._run(x, pos, freq, out, 0, stream)
 
     def backward(self, dout, pos, freq, out=None, stream=None):
         """The gradient of ``forward``'s input from that of its output."""
-        _by_hand(dout=dout)
+        if _grad_on():
+            _by_hand(("dout", dout))
         return self._run(dout, pos, freq, out, 1, stream)
 
 
@@ -258,21 +263,22 @@ class Mask:
         self.ptr, self.home = self.buffer.data_ptr(), _home(self.buffer)
         #: [queries, 4]: lo, hi, pos, doc of every row
         self.rows = self.buffer[:4 * queries].view(queries, 4)
+        self.inference = self.buffer.is_inference()
         self.stamp, self.serial = None, 0
+
+    def _stamp(self):
+        """Changes with every torch operation that writes the rows."""
+        return 0 if self.inference else self.buffer._version
 
     def _built(self):
         self.stamp = self._stamp()
         self.serial += 1
 
-    def _stamp(self):
-        """Changes with every torch operation that writes the rows."""
-        return 0 if self.buffer.is_inference() else self.buffer._version
-
     def check(self):
         """Refuse a mask that was not built, or written since."""
-        if self.queries and self.stamp is None:
-            _bad("the mask was not built: call build or from_rows first")
-        if self.queries and self.stamp != self._stamp():
+        if self.stamp != self._stamp() and self.queries:
+            if self.stamp is None:
+                _bad("the mask was not built: call build or from_rows first")
             _bad("the mask's rows were written since it was built: call from_rows")
 
     def build(self, offsets, key_offsets=None, prefix=None, stream=None):
@@ -351,7 +357,8 @@ class Attn:
         beside it (into ``saved`` of an earlier call, if given).  Without
         ``keep`` nothing is kept for a backward and saved is None."""
         bf = torch.bfloat16
-        _by_hand(q=q, k=k, v=v, slopes=slopes)
+        if _grad_on():
+            _by_hand(("q", q), ("k", k), ("v", v), ("slopes", slopes))
         if saved is not None and not keep:
             _bad("saved is given, and nothing is to be kept")
         with _On(stream) as (dev, s):
@@ -387,7 +394,8 @@ class Attn:
     def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
         bf = torch.bfloat16
-        _by_hand(dout=dout)
+        if _grad_on():
+            _by_hand(("dout", dout))
         if saved.mask is None:
             _bad("saved is of no forward")
         if saved.mask is mask and saved.serial != mask.serial:

@@ -44,8 +44,8 @@ def test_by_hand_under_no_grad():
     """There is nothing to refuse (what is missing then is the GPU)."""
     for ctx in (torch.no_grad(), torch.inference_mode()):
         with ctx:
-            ops._by_hand(x=_grad(3), y=None)
-    ops._by_hand(x=_grad(3).detach(), y=None)
+            assert not ops._grad_on()
+    ops._by_hand(("x", _grad(3).detach()), ("y", None))
 
 
 def test_gradients_of_gradients():
