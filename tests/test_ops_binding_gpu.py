@@ -93,3 +93,20 @@ def test_memory_of_objects_used_on_another_stream(what):
     again = torch.empty(numel, dtype=torch.uint8, device="cuda").data_ptr()
     torch.cuda.synchronize()
     assert busy and again != ptr
+
+
+@pytest.mark.parametrize("queries,keys", [(0, 0), (0, 70), (5, 0), (200, 0), (0, 5000)])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (4, 1)])
+def test_attn_without_rows_or_keys(queries, keys, heads, kv):
+    """Every output that there is, is 0."""
+    m = ops.Mask(queries, keys=keys, docs=1)
+    m.build(torch.tensor([0, queries], dtype=torch.int32, device="cuda"),
+            key_offsets=torch.tensor([0, keys], dtype=torch.int32, device="cuda"))
+    plan = ops.Attn(queries, heads, 64, keys=keys, kv_heads=kv)
+    q, k = torch.ones(plan.qs, device="cuda").to(BF), torch.ones(plan.ks, device="cuda").to(BF)
+    o, saved = plan.forward(q, k, k, m)
+    out = [torch.full_like(x, 7.0) for x in (q, k, k)]
+    plan.backward(q, q, k, k, o, saved, m, out=out)
+    assert (saved.lse == -float("inf")).all()
+    for x in (o, *out):
+        assert (x == 0).all()
