@@ -1200,7 +1200,6 @@ __global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
   for (int i = 0; i < a.parts; ++i) {
     const float w = ex2(l[i * lp] - R);
     t += w;
-    if (w == 0.f) continue;  // what it has may be infinite
     const float4* q = reinterpret_cast<const float4*>(a.part0 + (i * n + e) * 8);
     const float4 u = q[0], v = q[1];
     o[0] += w * u.x, o[1] += w * u.y, o[2] += w * u.z, o[3] += w * u.w;

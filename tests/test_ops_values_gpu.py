@@ -116,6 +116,26 @@ def test_attn_values_over_many_rows():
         _values(x, name, math.nan, 0.0, "doc", 64, [2600, 300], 1, 1, [33, 90])
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("queries,keys", [(1, 6000), (40, 6000), (40, 500)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_attn_values_of_no_weight(value, queries, keys, dim):
+    """A key that one far heavier leaves a weight of e^-200, 0 in fp32, is
+    attended all the same."""
+    log(f"case attention {value} of no weight, {queries} rows on {keys} keys, dim {dim}")
+    for heavy, at in ((10, keys - 30), (keys - 30, 10), (keys - 30, keys // 2)):
+        q, k, v, do, mask, rows = _case([queries], 2, 2, 1, dim, "doc", dim, [keys])
+        q[:, :, 0] = 16.0
+        k[:, :, 0] = 0.0
+        k[heavy, :, 0] = 13.0 * math.sqrt(dim)
+        v[at, 0, 5] = value
+        plan = ops.Attn(len(rows), 2, dim, keys=keys, kv_heads=1)
+        ref = _formulas(q, k, v, do, rows, 1 / math.sqrt(dim), 0.0)
+        assert not np.isfinite(ref["o"][:queries, :, 5]).any()
+        o, _ = plan.forward(q.cuda(), k.cuda(), v.cuda(), mask)
+        assert np.array_equal(np.isfinite(o.float().cpu().numpy()), np.isfinite(ref["o"]))
+
+
 def _time(f):
     """Best of three, in ms."""
     best = math.inf
