@@ -19,6 +19,7 @@ them, and the memory that an object holds is kept until all are done with it.
 
 from __future__ import annotations
 
+import bisect
 import ctypes
 import math
 
@@ -419,10 +420,32 @@ class Attn:
         return dq, dk, dv
 
 
+def _clashes(grads, outs):
+    """(i, j) of an output i that overlaps output j or gradient j, but for a
+    gradient that is its own output; else None.  Spans are (begin, end)."""
+    order = sorted((b, e, i) for i, (b, e) in enumerate(outs) if e > b)
+    for x, y in zip(order, order[1:]):
+        if y[0] < x[1]:
+            return x[2], y[2]
+    begins = [b for b, _, _ in order]  # disjoint from here on
+    for j, (b, e) in enumerate(grads):
+        at = max(bisect.bisect_right(begins, b) - 1, 0)
+        while e > b and at < len(order) and order[at][0] < e:
+            if order[at][1] > b and not (order[at][2] == j and order[at][:2] == (b, e)):
+                return order[at][2], j
+            at += 1
+    return None
+
+
+def _span(t):
+    return t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+
+
 class GradClip:
     """The global norm of ``grads`` (contiguous, fp32 or bf16) and their
     clipping, in place or into ``outs``.  The tensors' addresses are taken
-    once, so they must stay where they are from step to step."""
+    once, so they must stay where they are from step to step.  No output may
+    overlap another, or another tensor's gradient."""
 
     def __init__(self, grads, outs=None):
         self.h = _vp()
@@ -442,6 +465,9 @@ class GradClip:
             if g.get_device() != dev or o.get_device() != dev:
                 _bad(f"gradient {i} or its output is not on the current GPU")
             arr[i] = ClipTensor(g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g.dtype))
+        clash = _clashes([_span(g) for g in grads], [_span(o) for o in outs])
+        if clash:
+            _bad(f"output {clash[0]} overlaps output or gradient {clash[1]}")
         self.grads, self.outs = grads, outs
         self.device = grads[0].device if grads else "cuda"
         _check(lib().pulse_clip_create(arr, len(grads), ctypes.byref(self.h)))

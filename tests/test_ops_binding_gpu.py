@@ -110,3 +110,13 @@ def test_attn_without_rows_or_keys(queries, keys, heads, kv):
     assert (saved.lse == -float("inf")).all()
     for x in (o, *out):
         assert (x == 0).all()
+
+
+def test_clip_refuses_tensors_that_overlap():
+    x = torch.ones(100, device="cuda")
+    for grads, outs in (([x, x], None), ([x[:60], x[50:]], None), ([x[:50]], [x[1:51]])):
+        with pytest.raises(S.PulseError, match="overlaps"):
+            ops.GradClip(grads, outs)
+    y = torch.empty(200, device="cuda")
+    n = ops.GradClip([x, x], [y[:100], y[100:]]).run(1.0)  # read twice, written apart
+    assert abs(float(n) - 200 ** 0.5) <= 1e-5
