@@ -475,8 +475,9 @@ class GradClip:
         _check(lib().pulse_clip_sizes(self.h, ctypes.byref(n)))
         self.workspace = torch.empty(n.value, dtype=torch.uint8, device=self.device)
         self.home = _home(self.workspace)
-        _check(lib().pulse_clip_bind(self.h, self.workspace.data_ptr(), n.value,
-                                     torch.cuda.current_stream().cuda_stream))
+        s = torch.cuda.current_stream()
+        _check(lib().pulse_clip_bind(self.h, self.workspace.data_ptr(), n.value, s.cuda_stream))
+        s.synchronize()  # the table is there whichever stream the first run is on
 
     def __del__(self):
         try:

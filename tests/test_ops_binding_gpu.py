@@ -120,3 +120,17 @@ def test_clip_refuses_tensors_that_overlap():
     y = torch.empty(200, device="cuda")
     n = ops.GradClip([x, x], [y[:100], y[100:]]).run(1.0)  # read twice, written apart
     assert abs(float(n) - 200 ** 0.5) <= 1e-5
+
+
+def test_clip_runs_at_once_on_any_stream():
+    """The tensors' table is there when the object is: behind work that the
+    stream it was made on still has ahead, and without an event between."""
+    side = torch.cuda.Stream()
+    x = torch.ones(1 << 20, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)
+    clip = ops.GradClip([x])
+    assert torch.cuda.current_stream().query()
+    n = clip.run(512.0, stream=side)
+    side.synchronize()
+    assert abs(float(n) - 1024.0) <= 1e-3 and abs(float(x[0]) - 0.5) <= 1e-6
