@@ -315,14 +315,15 @@ class Saved:
 
     __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr", "home", "mask", "serial")
 
-    def __init__(self, heads, queries, head_dim, device):
+    def __init__(self, heads, queries, head_dim, device, home=None):
         n = -(-heads * queries // 4) * 4  # the second part is 16-byte aligned
         self.buffer = torch.empty(n + heads * queries * head_dim // 2, dtype=torch.float32,
                                   device=device)
         self.shape = (heads, queries, head_dim)
         self.lse_ptr = self.buffer.data_ptr()
         self.low_ptr = self.lse_ptr + 4 * n
-        self.home, self.mask, self.serial = _home(self.buffer), None, 0
+        self.home = _home(self.buffer) if home is None else home
+        self.mask, self.serial = None, 0
 
     @property
     def lse(self):
@@ -369,7 +370,7 @@ class Attn:
             if not keep:
                 lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
             elif saved is None:
-                saved = Saved(self.heads, self.queries, self.dim, q.device)
+                saved = Saved(self.heads, self.queries, self.dim, q.device, s)
             ws = None
             if self.fwd_bytes:
                 ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)

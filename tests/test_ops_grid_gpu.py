@@ -70,3 +70,10 @@ def test_attn_key_blocks_of_some_heads(heads, kv, dim, cap):
     got = _attn_run(plan, mask, q, k, v, do)
     for n in ("o", "dq", "dk", "dv"):
         assert rel_l2(got[n], ref[n]) <= ATTN_TOL, n
+
+
+@pytest.mark.parametrize("dim,bias", [(64, False), (64, True), (88, False), (88, True),
+                                      (128, False), (128, True)])
+def test_attn_blocks_of_128_under_a_large_cap(dim, bias):
+    log(f"case attention 128-row blocks dim {dim} cap 1e4 bias {bias}")
+    _check([70, 1, 50], 8, 256, 256, dim, "causal", 1e4, bias)

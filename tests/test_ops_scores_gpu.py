@@ -85,3 +85,14 @@ def test_attn_gradient_of_other_scales(scale, slopes, lens, pad):
                 assert rel_l2(got[n], ref[n]) <= ATTN_TOL, n
             else:
                 assert (got[n] == 0).all(), n
+
+
+@pytest.mark.parametrize("cap", [2.0, 50.0, 1e4])
+@pytest.mark.parametrize("scale", [0.0, -0.125, -1.0])
+def test_attn_caps_of_other_scales(scale, cap):
+    log(f"case attention scale {scale} cap {cap}")
+    q, k, v, do, mask, rows = _case([33, 70, 1], 5, 2, 1, 64, "causal", 34)
+    for slopes in (None, torch.tensor([0.25, -0.01])):
+        plan = ops.Attn(len(rows), 2, 64, kv_heads=1, scale=scale, cap=cap)
+        ref = _attn_ref(q, k, v, do, rows, scale, cap, slopes)
+        _attn_check(_attn_run(plan, mask, q, k, v, do, slopes), ref, f"scale {scale} cap {cap}")
