@@ -25,6 +25,11 @@
 // (0 NaN = NaN).  In a tile that some row attends only in part, such values
 // are cleared in the operand that is summed over, and the rows that do attend
 // them get them at the end.
+//
+// p and ds are rounded to bf16, as operands of the products that they enter; in
+// fp32 those would run at a sixteenth of the matrix units' bf16 rate.  With it
+// outputs and gradients are 0.0023 to 0.0024 (relative L2) off the float64 ones;
+// in fp32 throughout, rounded once at the end, they are 0.0017 off.
 #include <type_traits>
 
 #include "common.hpp"
@@ -66,7 +71,8 @@ struct Dev {  // device view of MattnArgs
   // with a range of the other side (or some of the group's heads) and fp32
   // results of its own, [parts][rows][heads][8 hd8], which a second kernel
   // adds up.
-  int parts, head_parts;  // head_parts of them by the group's heads (dk, dv)
+  int parts, head_parts;  // head_parts of them by the group's heads (dk, dv),
+  int head_per;           // of so many heads each, the last of what is left
   float *part0, *part1, *part_lse;
 };
 
@@ -207,33 +213,34 @@ __device__ __forceinline__ bool all_nan(const float (&o)[8]) {
 }
 
 // The tiles of keys (or rows) [lo, hi) that a block has left values out of: one
-// bit for every 2^shift keys, a tile or more.  What is added at the end is
-// looked for in these only, so that one NaN costs a tile and not all of them.
-// It lies in LDS with its range, of which the loops then hold nothing.
+// bit for every 2^shift tiles, so that 2048 bits hold the tiles of `all` keys.
+// What is added at the end is looked for in these only, so that one NaN costs
+// a tile and not all of them.  It lies in LDS with its range, of which the
+// loops then hold nothing: registers spent on it cost dq 6 % (8192 tokens of 16
+// heads, D = 64: 496 us instead of 465).
 struct Left {
   uint32_t w[64];
-  int lo, hi, shift, any;
+  int lo, hi, any;
+  __device__ static __forceinline__ int shift(int all) { return max(15 - __builtin_clz(all), 0); }
   // before the barrier that precedes the first mark
   __device__ __forceinline__ void init(int t, int first, int end) {
     if (t < 64) w[t] = 0;
-    if (t == 0) {
-      lo = first, hi = end, any = 0, shift = 6;
-      while ((end - first - 1) >> shift >= 64 * 32) ++shift;
-    }
+    if (t == 0) lo = first, hi = end, any = 0;
   }
-  // some of the tile that starts at `first`
-  __device__ __forceinline__ void mark(int first) {
-    const int b = (first - lo) >> shift;
-    atomicOr(&w[b >> 5], 1u << (b & 31));
+  // some of tile t, counted from lo
+  __device__ __forceinline__ void mark(int t, int all) {
+    t >>= shift(all);
+    atomicOr(&w[t >> 5], 1u << (t & 31));
     any = 1;
   }
   // f(first, end) of the marked tiles, until it returns false
   template <typename F>
-  __device__ __forceinline__ void each(F f) const {
+  __device__ __forceinline__ void each(int all, F f) const {
+    const int n = KT << shift(all);
     for (int i = 0; i < 64; ++i)
       for (uint32_t x = w[i]; x; x &= x - 1) {
-        const int at = lo + ((32 * i + __builtin_ctz(x)) << shift);
-        if (!f(at, min(at + (1 << shift), hi))) return;
+        const int at = lo + (32 * i + __builtin_ctz(x)) * n;
+        if (!f(at, min(at + n, hi))) return;
       }
   }
 };
@@ -515,10 +522,10 @@ constexpr int SMEM = max_of(4 * KT * D * 2, MERGE);
 // lane that holds its column, so that a step's only exchange between lanes is
 // the vote on the reference.
 // Bound by the vector units and the matrix units in turn, which overlap little
-// within a wave: a 32 x 32 step of D = 64 is 107 quarter-cycles of vector work
+// within a wave: a 32 x 32 step of D = 64 is 112 quarter-cycles of vector work
 // (exponential, scale and subtract, sum, maximum, rounding: 16 scores a lane)
-// and 64 of MFMA, of 160 in all.  8192 tokens of 16 heads: D = 64 335 us (820
-// TFLOP/s), D = 128 565 us (975 TFLOP/s).  64 rows per wave instead of 32 run
+// and 64 of MFMA, of 160 in all.  8192 tokens of 16 heads: D = 64 330 us (833
+// TFLOP/s), D = 128 565 us (973 TFLOP/s).  64 rows per wave instead of 32 run
 // at one wave per SIMD and were slower (D = 128: 637 TFLOP/s), 8 waves per block
 // too (16 x 256 tokens of 12 heads: 16.8 us instead of 13.1).
 // ---------------------------------------------------------------------------
@@ -573,7 +580,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
     const int stage = (it & 1) * 4 * TILE;  // bytes
     uint16_t* Ks = reinterpret_cast<uint16_t*>(smem + stage);
     // this stage was last read two tiles ago, before the previous barrier
-    if ((bt.all_lo > k0 || bt.all_hi < k0 + KT) && sv.clean()) left.mark(k0);
+    if ((bt.all_lo > k0 || bt.all_hi < k0 + KT) && sv.clean()) left.mark(it, a.Tk);
     sk.store(Ks);
     sv.store(Ks + TILE);
     __syncthreads();
@@ -584,9 +591,9 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
       sv.load(a.Tk - k0 - KT, a.hd8);
     }
     // 32-key steps, NU of them taken together where two waves share a SIMD and
-    // a step has MFMAs enough to cover the exponentials of another: 8192 tokens
-    // of 16 heads, D = 128: 548 us with two, 586 with one; D = 64: 355 and 341;
-    // 8 x 1024 tokens, D = 88: 75 and 71
+    // a step has MFMAs enough to cover the exponentials of another: against one
+    // at a time, 8192 tokens of 16 heads of 128 take 6 % less, of 64 4 % more,
+    // and 8 x 1024 tokens of 88 6 % more
     constexpr int NU = D == 128 ? 2 / SH : 1;
 #pragma unroll
     for (int y = 0; y < 2 / SH / NU; ++y) {
@@ -690,7 +697,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_fwd(Dev a) {
                    [&](int row, int c, float (&o)[8]) {
                      if (!left.any) return;
                      const Row x = row_at(a, row);
-                     left.each([&](int first, int end) {
+                     left.each(a.Tk, [&](int first, int end) {
                        for (int j = max(x.lo, first); j < min(x.hi, end); ++j)
                          add_odd(o, *reinterpret_cast<const uint4*>(vbase + j * a.vt + 8 * c),
                                  false);
@@ -769,7 +776,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
     const bool partly = bt.all_lo > k0 || bt.all_hi < k0 + KT;
     if (partly && sk.clean(bad[it & 1], it)) {
       odd_at[it & 1] = it;
-      left.mark(k0);
+      left.mark(it, a.Tk);
     }
     sk.store(Ks);
     sv.store(Ks + TILE);
@@ -829,16 +836,20 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_q(Dev a) {
           acc[d] = mma(cols32<D>(smem, cbase + stage, d, at + 32 * D * ks), ds[ks], acc[d]);
     }
   }
+  if (left.any) {  // set before the last barrier, if at all
+    // a row whose lse is not finite may have attended cleared keys only
+    const float e = rw.hi > rw.lo ? l2 * 0.f : 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[d][i] += e;
+  }
   write_rows<D, G>(reinterpret_cast<float*>(smem), acc, a.scale, a.dq + h * a.dqh, a.dqt,
                    part_of(a, a.part0, part, a.Tq, a.H, h), nullptr, tile * RB, a.Tq, a.H, a.hd8,
                    [&](int row, int c, float (&o)[8]) {
                      if (!left.any) return;
                      const Row x = row_at(a, row);
-                     if (x.hi <= x.lo) return;
-                     const float e = finite_or_nan(a.lse[(long)h * a.Tq + row]) * 0.f;
-#pragma unroll
-                     for (int t = 0; t < 8; ++t) o[t] += e;
-                     left.each([&](int first, int end) {
+                     left.each(a.Tk, [&](int first, int end) {
                        for (int j = max(x.lo, first); j < min(x.hi, end); ++j)
                          add_odd(o, *reinterpret_cast<const uint4*>(kbase + j * a.kt + 8 * c),
                                  true);
@@ -894,7 +905,7 @@ struct Hits {
 // two waves per SIMD: dv and dk then have a pass each, with s computed in both
 // (8192 tokens of 16 heads: 1370 us instead of 1489; at D = 96 one pass, 143
 // us, and two, 174, 8 x 1024 tokens).  About 900 TFLOP/s over its products.
-// The whole backward at 8192 tokens of 16 heads: D = 64 1020 us, D = 128 2150.
+// The whole backward at 8192 tokens of 16 heads: D = 64 1050 us, D = 128 2165.
 // ---------------------------------------------------------------------------
 template <int D, int G, int WPE, int CAP, bool BIAS, bool DK, bool DV>
 __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
@@ -934,8 +945,8 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
   hits.k1 = tile * RB + RB;
   // the part's heads, and its share of the tiles of rows
   const int hp = part % a.head_parts;
-  const int h0 = kh * a.rep + a.rep * hp / a.head_parts;
-  const int heads = kh * a.rep + a.rep * (hp + 1) / a.head_parts - h0;
+  int h = kh * a.rep + hp * a.head_per;
+  const int hend = min(h + a.head_per, (kh + 1) * a.rep);
   hits.first = part / a.head_parts;
   hits.step = a.parts / a.head_parts;
   float ln = 0.f, dn = 0.f;  // of the next tile's rows (threads 0..63)
@@ -958,7 +969,6 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       }
     }
   };
-  int h = h0;
   hits.start(a, lane);
   int qt = hits.next(a, lane);
   if (qt >= 0) fetch(h, qt);
@@ -972,11 +982,11 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
       // scores are +-cap: the largest finite q gives the same p and ds = 0,
       // and dk its NaN (0 inf) at the end.
       if (sq.template clean<(CAP > 0)>() && CAP) {
-        left.mark(qt * KT);
+        left.mark(qt, a.Tq);
         odd_q = 1;
       }
       if (sd.clean()) {
-        left.mark(qt * KT);
+        left.mark(qt, a.Tq);
         odd_do = 1;
       }
     }
@@ -993,7 +1003,7 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     }
     __syncthreads();
     int qn = hits.next(a, lane);
-    if (qn < 0 && h + 1 < h0 + heads) {
+    if (qn < 0 && h + 1 < hend) {
       ++h;
       hits.start(a, lane);
       qn = hits.next(a, lane);
@@ -1094,14 +1104,15 @@ __global__ __launch_bounds__(256, WPE) void k_mattn_bwd_kv(Dev a) {
     }
     qt = qn;
   }
-  // o += the values left out of x (q or dout) in the rows that attend key j
+  // o += the values left out of x (q or dout) in the rows that attend key j, of
+  // every head of the group: what another part adds too stays what it is
   const auto add_left = [&](const uint16_t* x, long xt, long xh, bool nan, int j, int c,
                             float (&o)[8]) {
-    left.each([&](int first, int end) {
+    left.each(a.Tq, [&](int first, int end) {
       for (int i = first; i < end; ++i) {
         const Row r = row_at(a, i);
         if (j < r.lo || j >= r.hi) continue;
-        for (int g = h0; g < h0 + heads; ++g)
+        for (int g = kh * a.rep; g < (kh + 1) * a.rep; ++g)
           add_odd(o, *reinterpret_cast<const uint4*>(x + i * xt + g * xh + 8 * c), nan);
       }
       return !all_nan(o);
@@ -1217,8 +1228,8 @@ __global__ __launch_bounds__(256) void k_mattn_join(Dev a) {
 enum Pass { FWD, BWD_Q, BWD_KV };
 
 struct Plan {
-  int group;              // groups of 32 rows per block
-  int parts, head_parts;  // as in Dev
+  int group;                        // groups of 32 rows per block
+  int parts, head_parts, head_per;  // as in Dev
 };
 
 // How a pass is spread over the GPU (256 CUs, two or three blocks each); us
@@ -1249,11 +1260,12 @@ struct Plan {
 Plan plan(Pass p, int Tq, int Tk, int H, int KV) {
   const int rows = p == BWD_KV ? Tk : Tq, heads = p == BWD_KV ? KV : H;
   const int other = p == BWD_KV ? Tq : Tk;
-  Plan x{4, 1, 1};
+  Plan x{4, 1, 1, H / KV};
   long blocks = (long)((rows + 127) / 128) * heads;
   if (p == BWD_KV && blocks < 1024 && H > KV) {
-    const long rep = H / KV, per = rep * blocks / 3072;
-    x.parts = x.head_parts = (int)(per > 1 ? (rep + per - 1) / per : rep);
+    const long per = H / KV * blocks / 3072;
+    x.head_per = per > 1 ? (int)per : 1;
+    x.parts = x.head_parts = (H / KV + x.head_per - 1) / x.head_per;
     blocks *= x.parts;
   }
   if (blocks < 512) {
@@ -1304,8 +1316,12 @@ hipError_t launch_mode(const Dev& d, hipStream_t st) {
 template <Pass P, int D>
 hipError_t launch_rows(const Dev& d, int group, hipStream_t st) {
   // waves per SIMD.  Three at D = 64: 16 x 256 tokens of 12 heads, backward
-  // 38.8 us, with two 40.6; at 96, and over keys, three spill (8 x 1024 tokens
-  // of 16 heads of 88, backward: 220 us with two, 338 with three over rows).
+  // 38.6 us, with two 40.6, though over rows up to 20 bytes a lane spill (52
+  // under a cap, 144 under one above CAP_LOW).  Three at 96, and over keys,
+  // spill more (8 x 1024 tokens of 16 heads of 88, backward: 220 us with two,
+  // 338 with three over rows).  With two, what spills is 12 to 60 bytes over
+  // keys at 96 (92 above CAP_LOW) and, under a cap, up to 60 over rows and 80
+  // over keys at 128.
   constexpr int W = P != BWD_KV && D == 64 ? 3 : 2;
   return group == 4 ? launch_mode<P, D, 4, W>(d, st) : launch_mode<P, D, 2, W>(d, st);
 }
@@ -1346,7 +1362,7 @@ hipError_t run(const MattnArgs& a, hipStream_t st) {
   const Space s = space(P, x, a.Tq, a.Tk, a.H, a.KV, a.hd);
   char* ws = static_cast<char*>(a.ws);
   Dev d = view(a);
-  d.parts = x.parts, d.head_parts = x.head_parts;
+  d.parts = x.parts, d.head_parts = x.head_parts, d.head_per = x.head_per;
   d.dsum = reinterpret_cast<float*>(ws);
   d.part0 = reinterpret_cast<float*>(ws + s.part0);
   d.part1 = reinterpret_cast<float*>(ws + s.part1);
