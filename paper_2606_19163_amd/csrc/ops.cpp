@@ -53,7 +53,8 @@ pulse_status check_heads(const pulse_heads* x, const char* name, int tokens, int
     return ofail(PULSE_E_INVALID_ARG, "%s has a stride that is not a multiple of 16 bytes", name);
   // no more than an address space, so that neither these sums nor the kernels'
   // offsets wrap around
-  if ((tokens > 1 && ts > MAX_EXTENT / (tokens - 1)) || (heads > 1 && hs > MAX_EXTENT / (heads - 1)))
+  if ((tokens > 1 && ts > MAX_EXTENT / (tokens - 1)) ||
+      (heads > 1 && hs > MAX_EXTENT / (heads - 1)))
     return ofail(PULSE_E_INVALID_ARG, "%s extends over more than 2^47 elements", name);
   if (out) {
     const bool th = (heads == 1 || hs >= dim) && (tokens == 1 || ts >= (heads - 1) * hs + dim);

@@ -156,24 +156,12 @@ def _by_hand(*inputs):
 _grad_on = torch.is_grad_enabled
 
 
-class _On:
-    """(device, stream handle) of torch's current stream, or of `stream` made
-    current, so that what a call allocates belongs to the stream it runs on."""
-
-    __slots__ = ("ctx",)
-
-    def __init__(self, stream):
-        self.ctx = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        dev = torch.cuda.current_device()
-        return dev, _raw_stream(dev)
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _here():
+    """The current GPU and the handle of its current stream.  A call given a
+    `stream` makes it current and calls itself, so that what it allocates
+    belongs to the stream it runs on."""
+    dev = torch.cuda.current_device()
+    return dev, _raw_stream(dev)
 
 
 def _home(t):
@@ -181,10 +169,10 @@ def _home(t):
     return _raw_stream(t.get_device()) if t.is_cuda else None
 
 
-def _used_on(t, home, dev, s):
-    """`t` is used on stream s: its memory is not handed on before that is done."""
-    if s != home:
-        t.record_stream(torch.cuda.current_stream(dev))
+def _used_on(t, dev):
+    """`t` is used on another stream than its own, the current one: its memory
+    is not handed on before that is done."""
+    t.record_stream(torch.cuda.current_stream(dev))
 
 
 def rope_freqs(axis_dim, base=10000.0, device="cuda"):
@@ -222,25 +210,28 @@ class Rope:
     def _run(self, x, pos, freq, out, backward, stream):
         n = x.shape[0]
         shape = (n, self.heads, self.dim)
-        with _On(stream) as (dev, s):
-            if out is None:
-                out = torch.empty(shape, dtype=self.dtype, device=x.device)
-            hx = _heads(x, "x", shape, self.dtype, dev)
-            hy = _heads(out, "out", shape, self.dtype, dev)
-            _check(lib().pulse_rope(
-                self.desc, n, backward, hx, _flat(pos, "pos", n * self.axes, torch.float32, dev),
-                _flat(freq, "freq", self.half, torch.float32, dev), hy, s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._run(x, pos, freq, out, backward, None)
+        dev, s = _here()
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=x.device)
+        hx = _heads(x, "x", shape, self.dtype, dev)
+        hy = _heads(out, "out", shape, self.dtype, dev)
+        _check(lib().pulse_rope(
+            self.desc, n, backward, hx, _flat(pos, "pos", n * self.axes, torch.float32, dev),
+            _flat(freq, "freq", self.half, torch.float32, dev), hy, s))
         return out
 
     def forward(self, x, pos, freq, out=None, stream=None):
         """x turned by its positions; ``out`` may be x."""
-        if _grad_on():
+        if _grad_on() and (x.requires_grad or pos.requires_grad or freq.requires_grad):
             _by_hand(("x", x), ("pos", pos), ("freq", freq))
         return self._run(x, pos, freq, out, 0, stream)
 
     def backward(self, dout, pos, freq, out=None, stream=None):
         """The gradient of ``forward``'s input from that of its output."""
-        if _grad_on():
+        if dout.requires_grad and _grad_on():
             _by_hand(("dout", dout))
         return self._run(dout, pos, freq, out, 1, stream)
 
@@ -284,26 +275,34 @@ class Mask:
 
     def build(self, offsets, key_offsets=None, prefix=None, stream=None):
         """From int32 ``offsets`` [docs + 1] on the GPU; returns ``rows``."""
-        with _On(stream) as (dev, s):
-            if self.buffer.get_device() != dev:
-                _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
-            _used_on(self.buffer, self.home, dev, s)
-            _check(lib().pulse_mask_build(
-                self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
-                _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
-                _flat(prefix, "prefix", self.docs, torch.int32, dev), self.ptr, self.bytes, s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.build(offsets, key_offsets, prefix)
+        dev, s = _here()
+        if self.buffer.get_device() != dev:
+            _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
+        if s != self.home:
+            _used_on(self.buffer, dev)
+        _check(lib().pulse_mask_build(
+            self.desc, _flat(offsets, "offsets", self.docs + 1, torch.int32, dev),
+            _flat(key_offsets, "key_offsets", self.docs + 1, torch.int32, dev),
+            _flat(prefix, "prefix", self.docs, torch.int32, dev), self.ptr, self.bytes, s))
         self._built()
         return self.rows
 
     def from_rows(self, rows, stream=None):
         """From the caller's int32 [queries, 4] (it may be ``self.rows``)."""
-        with _On(stream) as (dev, s):
-            if self.buffer.get_device() != dev:
-                _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
-            _used_on(self.buffer, self.home, dev, s)
-            _check(lib().pulse_mask_from_rows(
-                self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
-                self.bytes, s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.from_rows(rows)
+        dev, s = _here()
+        if self.buffer.get_device() != dev:
+            _bad(f"the mask is on {self.buffer.device}, not on the current GPU")
+        if s != self.home:
+            _used_on(self.buffer, dev)
+        _check(lib().pulse_mask_from_rows(
+            self.desc, _flat(rows, "rows", 4 * self.queries, torch.int32, dev), self.ptr,
+            self.bytes, s))
         self._built()
         return self.rows
 
@@ -348,10 +347,12 @@ class Attn:
     def _mask(self, mask, dev, s):
         if mask.queries != self.queries or mask.keys != self.keys:
             _bad(f"the mask is of {mask.queries} rows and {mask.keys} keys")
-        mask.check()
+        if mask.inference or mask.stamp != mask.buffer._version:
+            mask.check()
         if mask.buffer.get_device() != dev:
             _bad(f"the mask is on {mask.buffer.device}, not on the current GPU")
-        _used_on(mask.buffer, mask.home, dev, s)
+        if s != mask.home:
+            _used_on(mask.buffer, dev)
         return mask.ptr
 
     def forward(self, q, k, v, mask, slopes=None, out=None, saved=None, stream=None, keep=True):
@@ -359,28 +360,32 @@ class Attn:
         beside it (into ``saved`` of an earlier call, if given).  Without
         ``keep`` nothing is kept for a backward and saved is None."""
         bf = torch.bfloat16
-        if _grad_on():
+        if _grad_on() and (q.requires_grad or k.requires_grad or v.requires_grad or
+                           slopes is not None and slopes.requires_grad):
             _by_hand(("q", q), ("k", k), ("v", v), ("slopes", slopes))
         if saved is not None and not keep:
             _bad("saved is given, and nothing is to be kept")
-        with _On(stream) as (dev, s):
-            if out is None:
-                out = torch.empty(self.qs, dtype=bf, device=q.device)
-            lse = None
-            if not keep:
-                lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
-            elif saved is None:
-                saved = Saved(self.heads, self.queries, self.dim, q.device, s)
-            ws = None
-            if self.fwd_bytes:
-                ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
-            _check(lib().pulse_attn_forward(
-                self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
-                _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev, s),
-                _flat(slopes, "slopes", self.heads, torch.float32, dev),
-                _heads(out, "out", self.qs, bf, dev),
-                *(self._saved(saved, dev, s) if keep else (lse.data_ptr(), None)),
-                ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward(q, k, v, mask, slopes, out, saved, None, keep)
+        dev, s = _here()
+        if out is None:
+            out = torch.empty(self.qs, dtype=bf, device=q.device)
+        lse = None
+        if not keep:
+            lse = torch.empty((self.heads, self.queries), dtype=torch.float32, device=q.device)
+        elif saved is None:
+            saved = Saved(self.heads, self.queries, self.dim, q.device, s)
+        ws = None
+        if self.fwd_bytes:
+            ws = torch.empty(self.fwd_bytes, dtype=torch.uint8, device=q.device)
+        _check(lib().pulse_attn_forward(
+            self.desc, _heads(q, "q", self.qs, bf, dev), _heads(k, "k", self.ks, bf, dev),
+            _heads(v, "v", self.ks, bf, dev), self._mask(mask, dev, s),
+            _flat(slopes, "slopes", self.heads, torch.float32, dev),
+            _heads(out, "out", self.qs, bf, dev),
+            *(self._saved(saved, dev, s) if keep else (lse.data_ptr(), None)),
+            ws.data_ptr() if ws is not None else None, self.fwd_bytes, s))
         if keep:
             saved.mask, saved.serial = mask, mask.serial
         return out, saved
@@ -390,34 +395,39 @@ class Attn:
             _bad(f"saved is of heads, queries and head_dim {saved.shape}")
         if saved.buffer.get_device() != dev:
             _bad(f"saved is on {saved.buffer.device}, not on the current GPU")
-        _used_on(saved.buffer, saved.home, dev, s)
+        if s != saved.home:
+            _used_on(saved.buffer, dev)
         return saved.lse_ptr, saved.low_ptr
 
     def backward(self, dout, q, k, v, o, saved, mask, slopes=None, out=None, stream=None):
         """(dq, dk, dv), written into the tensors of ``out`` if given."""
         bf = torch.bfloat16
-        if _grad_on():
+        if dout.requires_grad and _grad_on():
             _by_hand(("dout", dout))
         if saved.mask is None:
             _bad("saved is of no forward")
         if saved.mask is mask and saved.serial != mask.serial:
             _bad("the mask was built again since this forward: batches in flight need one each")
-        with _On(stream) as (dev, s):
-            if out is None:
-                out = [torch.empty(n, dtype=bf, device=q.device)
-                       for n in (self.qs, self.ks, self.ks)]
-            dq, dk, dv = out
-            ws = None
-            if self.bwd_bytes:
-                ws = torch.empty(self.bwd_bytes, dtype=torch.uint8, device=q.device)
-            _check(lib().pulse_attn_backward(
-                self.desc, _heads(dout, "dout", self.qs, bf, dev), _heads(q, "q", self.qs, bf, dev),
-                _heads(k, "k", self.ks, bf, dev), _heads(v, "v", self.ks, bf, dev),
-                _heads(o, "o", self.qs, bf, dev), *self._saved(saved, dev, s), self._mask(mask, dev, s),
-                _flat(slopes, "slopes", self.heads, torch.float32, dev),
-                _heads(dq, "dq", self.qs, bf, dev), _heads(dk, "dk", self.ks, bf, dev),
-                _heads(dv, "dv", self.ks, bf, dev),
-                ws.data_ptr() if ws is not None else None, self.bwd_bytes, s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(dout, q, k, v, o, saved, mask, slopes, out)
+        dev, s = _here()
+        if out is None:
+            out = [torch.empty(n, dtype=bf, device=q.device)
+                   for n in (self.qs, self.ks, self.ks)]
+        dq, dk, dv = out
+        ws = None
+        if self.bwd_bytes:
+            ws = torch.empty(self.bwd_bytes, dtype=torch.uint8, device=q.device)
+        _check(lib().pulse_attn_backward(
+            self.desc, _heads(dout, "dout", self.qs, bf, dev), _heads(q, "q", self.qs, bf, dev),
+            _heads(k, "k", self.ks, bf, dev), _heads(v, "v", self.ks, bf, dev),
+            _heads(o, "o", self.qs, bf, dev), *self._saved(saved, dev, s),
+            self._mask(mask, dev, s),
+            _flat(slopes, "slopes", self.heads, torch.float32, dev),
+            _heads(dq, "dq", self.qs, bf, dev), _heads(dk, "dk", self.ks, bf, dev),
+            _heads(dv, "dv", self.ks, bf, dev),
+            ws.data_ptr() if ws is not None else None, self.bwd_bytes, s))
         return dq, dk, dv
 
 
@@ -491,10 +501,14 @@ class GradClip:
     def run(self, max_norm, eps=1e-6, norm=None, stream=None):
         """Clip to ``max_norm``; returns the norm before it, fp32 [1].  Calls
         share one workspace: order the streams that they run on."""
-        with _On(stream) as (dev, s):
-            _used_on(self.workspace, self.home, dev, s)
-            if norm is None:
-                norm = torch.empty(1, dtype=torch.float32, device=self.device)
-            _check(lib().pulse_clip_run(self.h, max_norm, eps,
-                                        _flat(norm, "norm", 1, torch.float32, dev), s))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.run(max_norm, eps, norm)
+        dev, s = _here()
+        if s != self.home:
+            _used_on(self.workspace, dev)
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device=self.device)
+        _check(lib().pulse_clip_run(self.h, max_norm, eps,
+                                    _flat(norm, "norm", 1, torch.float32, dev), s))
         return norm
