@@ -56,7 +56,7 @@ constexpr float GROW = 8.f;
 struct Dev {  // device view of MattnArgs
   int Tq, Tk, H, rep, hd8;
   float c1, c2;  // no cap: scale log2e; cap: scale / cap and cap log2e
-  float inv_c1;  // no cap
+  float inv_c1;  // no cap, over keys
   float scale, cap;
   const uint16_t *q, *k, *v, *dout, *o_in;
   uint16_t *o, *dq, *dk, *dv;
@@ -1139,12 +1139,8 @@ Dev view(const MattnArgs& a) {
   d.scale = a.scale, d.cap = a.cap;
   d.c1 = a.cap > 0.f ? a.scale / a.cap : a.scale * LOG2E;
   d.c2 = a.cap * LOG2E;
-  if (a.cap > 0.f) {  // of a cap so small that all but scores of 0 reach it
-    if (fabsf(d.c1) > 1e30f) d.c1 = copysignf(1e30f, d.c1);
-  } else {  // of a scale of 0, which is divided by: scores vanish all the same
-    if (fabsf(d.c1) < 1e-30f) d.c1 = 1e-30f;
-    d.inv_c1 = 1.f / d.c1;
-  }
+  // of a cap so small that all but scores of 0 reach it
+  if (a.cap > 0.f && fabsf(d.c1) > 1e30f) d.c1 = copysignf(1e30f, d.c1);
   const auto in = [](const pulse_heads& x) { return static_cast<const uint16_t*>(x.ptr); };
   const auto out = [](const pulse_heads& x) { return static_cast<uint16_t*>(x.ptr); };
   d.q = in(a.q), d.k = in(a.k), d.v = in(a.v), d.dout = in(a.dout), d.o_in = in(a.o);
@@ -1362,6 +1358,11 @@ hipError_t run(const MattnArgs& a, hipStream_t st) {
   const Space s = space(P, x, a.Tq, a.Tk, a.H, a.KV, a.hd);
   char* ws = static_cast<char*>(a.ws);
   Dev d = view(a);
+  if (P == BWD_KV && !(a.cap > 0.f)) {
+    // which divides by it: a scale of 0 becomes one at which scores vanish too
+    if (fabsf(d.c1) < 1e-30f) d.c1 = 1e-30f;
+    d.inv_c1 = 1.f / d.c1;
+  }
   d.parts = x.parts, d.head_parts = x.head_parts, d.head_per = x.head_per;
   d.dsum = reinterpret_cast<float*>(ws);
   d.part0 = reinterpret_cast<float*>(ws + s.part0);

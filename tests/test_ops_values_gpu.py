@@ -172,3 +172,17 @@ def test_attn_values_do_not_stall_a_step(name, rows):
     odd = _time(step)
     log(f"  {name} {rows}: {clean:.2f} ms, with NaN {odd:.2f} ms")
     assert odd <= 3 * clean
+
+
+@pytest.mark.parametrize("kind", ["doc", "causal"])
+@pytest.mark.parametrize("name", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_attn_values_at_a_scale_of_0(value, name, kind):
+    """0 times infinity is no score of 0."""
+    for x in ([0], [20], [100], [44, 178]):
+        q, k, v, do, mask, rows = _case(LENS, 3, 2, 1, 64, kind, 64)
+        for i in x:
+            dict(q=q, k=k, v=v, do=do)[name][i, 0, 5] = value
+        plan = ops.Attn(len(rows), 2, 64, kv_heads=1, scale=0.0)
+        ref = _formulas(q, k, v, do, rows, 0.0, 0.0)
+        _same_values(_attn_run(plan, mask, q, k, v, do), ref, f"{name} {value} {kind}")
