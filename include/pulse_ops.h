@@ -13,6 +13,12 @@
  *   pulse_attn  softmax attention under such a mask, with shared key heads,
  *               tanh-capped scores and a bias linear in the distance,
  *               forward and backward;
+ *   pulse_norm  the joint between two halves of a block: gate and residual,
+ *               the norms before and after, and the documents' scales and
+ *               shifts, forward and backward;
+ *   pulse_keep  activations kept in 8 bits until the backward pass, and the
+ *               gradients computed from them;
+ *   pulse_lin8  linear layers in 8-bit integers;
  *   pulse_clip  the global norm over many gradient tensors, and clipping.
  *
  * Conventions (as in pulse_stage.h): tensor pointers are caller-owned DEVICE
@@ -168,6 +174,176 @@ pulse_status pulse_attn_backward(const pulse_attn_desc* desc, const pulse_heads*
                                  const pulse_heads* dq, const pulse_heads* dk,
                                  const pulse_heads* dv, void* workspace, size_t workspace_bytes,
                                  void* stream);
+
+/* Rows of a token-major tensor: element (t, c) lies at ptr + t * token_stride
+ * + c (the stride in elements).  ptr is 16-byte aligned and the stride a
+ * multiple of 16 bytes, at most 2^40 and not negative. */
+typedef struct {
+  void* ptr;
+  int64_t token_stride;
+} pulse_rows;
+
+/* ---- norms of a block, with its gate and residual --------------------------- */
+
+typedef enum {
+  PULSE_NORM_NONE = 0,
+  PULSE_NORM_LAYER = 1, /* n = (v - mean) / sqrt(mean((v - mean)^2) + eps)  */
+  PULSE_NORM_RMS = 2    /* n = v / sqrt(mean(v^2) + eps)                    */
+} pulse_norm_kind;
+
+typedef struct {
+  int32_t channels;     /* a multiple of 8, 8..8192                          */
+  int32_t docs;         /* documents, 1..2^20                                */
+  int32_t pre;          /* norm of the stream, before the next half: LAYER,
+                           RMS, or NONE for a joint that only adds           */
+  int32_t post;         /* norm of y, after the last half; NONE: y itself    */
+  int32_t branch;       /* 1: y is added to the stream; 0: there is no y, h
+                           is x and is not written                           */
+  float eps;            /* >= 0                                              */
+  float residual_scale; /* r, finite                                         */
+  int32_t dtype;        /* of y, u, du, dy: PULSE_BF16 or PULSE_F32          */
+  int32_t stream_dtype; /* of x, h, dh, dx: PULSE_F32, or as dtype           */
+} pulse_norm_desc;
+
+/* What a joint applies.  Document d holds rows [offsets[d], offsets[d + 1])
+ * (int32 [docs + 1], ascending from 0; documents may be empty); rows from the
+ * last offset on are padding.  offsets NULL: docs is 1, and all rows are its.
+ * gate, scale and shift are fp32 [docs][channels] with row strides of their
+ * own (elements, a multiple of 4), each NULL for none: a gate of 1, a scale and
+ * shift of 0.  weight and bias (of the norm before the next half) and
+ * post_weight are fp32 [channels], or NULL for 1, 0 and 1.  All pointers but
+ * offsets are 16-byte aligned.  gate needs `branch`; scale, shift, weight and
+ * bias need `pre`; post_weight needs `post`. */
+typedef struct {
+  const int32_t* offsets;
+  const float *gate, *scale, *shift;
+  int64_t gate_stride, scale_stride, shift_stride;
+  const float *weight, *bias, *post_weight;
+} pulse_norm_params;
+
+/* The gradients of pulse_norm_params: fp32, contiguous, 16-byte aligned, each
+ * NULL if not wanted.  They are overwritten.  dgate may be asked for without
+ * a gate (that of a gate of 1), and so on. */
+typedef struct {
+  float *dgate, *dscale, *dshift;         /* [docs][channels]                */
+  float *dweight, *dbias, *dpost_weight;  /* [channels]                      */
+} pulse_norm_grads;
+
+/* Workspace bytes of a backward call of `tokens` rows. */
+pulse_status pulse_norm_sizes(const pulse_norm_desc* desc, int32_t tokens,
+                              size_t* backward_bytes);
+
+/* For every row t of document d, with Post and Pre the norms times their
+ * weights (and plus the bias, for Pre):
+ *   h = x + r gate[d] Post(y)                  rounded to stream_dtype,
+ *   u = Pre(h) (1 + scale[d]) + shift[d]       of h as rounded.
+ * Padding takes no part: h = x, u = 0, and nothing there reaches a result
+ * (x apart).  Statistics and sums are fp32.  h may be x itself and u may be y
+ * itself (same pointer and stride); otherwise outputs must not overlap
+ * inputs.  Without `branch` y and h are not used, without `pre` u is not
+ * (NULL).  0 <= tokens <= 2^23. */
+pulse_status pulse_norm_forward(const pulse_norm_desc* desc, int32_t tokens, const pulse_rows* x,
+                                const pulse_rows* y, const pulse_norm_params* params,
+                                const pulse_rows* h, const pulse_rows* u, void* stream);
+
+/* Gradients from du and dh (NULL: 0), those of u and of h as the next joint
+ * sees it, and from the forward's h and y.  With dN the gradient of the norm's
+ * n and dH = dh + (the norm's gradient): dx = dH, dy = Post'(r gate dH), and
+ * the parameters' sums over rows, in fp32 and in a fixed order.  Padding: dx =
+ * dh (0 without it), dy = 0, nothing to any sum.  Without `pre` there is no du
+ * (NULL) and h is not read (NULL).  dx may be dh, dy may be du or y; otherwise
+ * outputs must not overlap inputs.  dx may be NULL (it is then not wanted). */
+pulse_status pulse_norm_backward(const pulse_norm_desc* desc, int32_t tokens, const pulse_rows* du,
+                                 const pulse_rows* dh, const pulse_rows* h, const pulse_rows* y,
+                                 const pulse_norm_params* params, const pulse_rows* dx,
+                                 const pulse_rows* dy, const pulse_norm_grads* grads,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- activations kept in 8 bits --------------------------------------------- */
+
+typedef enum { PULSE_ACT_NONE = 0, PULSE_ACT_GELU = 1, PULSE_ACT_SILU = 2 } pulse_act;
+
+/* Kept rows of C channels.  Groups of 32 channels (the last may be shorter)
+ * share a power of two 2^e, -126 <= e <= 121, the least with which their largest
+ * value rounds to at most 127; a value is kept as q = round(x 2^-e), to
+ * nearest even, and stands for q 2^e, which bf16 holds exactly (at e = 121 q is
+ * cut to [-127, 127]).  A group that holds a NaN or an infinity stands for
+ * NaN.  Layout: [tokens][P] bytes q +
+ * 128, P = C rounded up to a multiple of 32 (channels past C hold 0), then, on
+ * the next multiple of 16 bytes, [tokens][P / 32] bytes e + 126, or 255 for
+ * NaN. */
+typedef struct {
+  int32_t channels; /* a multiple of 8, 8..65536                            */
+  int32_t act;      /* pulse_act                                            */
+  int32_t dtype;    /* of x, a, da and dx: PULSE_BF16 or PULSE_F32          */
+} pulse_keep_desc;
+
+/* Bytes of `tokens` kept rows, 0 <= tokens <= 2^23. */
+pulse_status pulse_keep_sizes(const pulse_keep_desc* desc, int32_t tokens, size_t* bytes);
+
+/* Keep x, and write a = act(x) of x itself (NULL: not wanted, as without an
+ * act; it may be x).  `kept` is 16-byte aligned. */
+pulse_status pulse_keep_save(const pulse_keep_desc* desc, int32_t tokens, const pulse_rows* x,
+                             const pulse_rows* a, void* kept, size_t kept_bytes, void* stream);
+
+/* x as kept. */
+pulse_status pulse_keep_load(const pulse_keep_desc* desc, int32_t tokens, const void* kept,
+                             size_t kept_bytes, const pulse_rows* x, void* stream);
+
+/* dx = da act'(x) and, where a_kept is not NULL, act(x) kept in 8 bits again,
+ * of x as kept.  dx may be da.  Needs an act. */
+pulse_status pulse_keep_backward(const pulse_keep_desc* desc, int32_t tokens, const pulse_rows* da,
+                                 const void* kept, size_t kept_bytes, const pulse_rows* dx,
+                                 void* a_kept, size_t a_kept_bytes, void* stream);
+
+/* Workspace bytes of a weight gradient. */
+pulse_status pulse_keep_wgrad_sizes(const pulse_keep_desc* desc, int32_t tokens, int32_t outputs,
+                                    size_t* workspace_bytes);
+
+/* The weight gradient of a linear layer y = W x + b whose input was kept:
+ *   dw[n][c] = sum_t dy[t][n] x[t][c],  db[n] = sum_t dy[t][n] (NULL: not
+ * wanted), added to what dw and db hold if `accumulate` is 1.  dy is bf16
+ * [tokens][outputs] (whatever desc->dtype; outputs a multiple of 8, 8..65536),
+ * dw fp32 [outputs][channels], contiguous, 16-byte aligned.  The products of
+ * bf16 dy and kept values are exact, sums are fp32 and in a fixed order.  desc->act is
+ * not applied.  No tokens: dw and db are 0 (or stay).  The workspace is
+ * 256-byte aligned. */
+pulse_status pulse_keep_wgrad(const pulse_keep_desc* desc, int32_t tokens, int32_t outputs,
+                              const pulse_rows* dy, const void* kept, size_t kept_bytes, float* dw,
+                              float* db, int32_t accumulate, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* ---- linear layers in 8-bit integers ------------------------------------------ */
+
+typedef struct {
+  int32_t inputs;  /* K, a multiple of 8, 8..65536                          */
+  int32_t outputs; /* N, a multiple of 8, 8..65536                          */
+  int32_t act;     /* pulse_act, of the output                              */
+  int32_t dtype;   /* of x and y: PULSE_BF16 only                           */
+} pulse_lin8_desc;
+
+/* Bytes of the laid-out weights, and of the workspace for `tokens` rows
+ * (either may be NULL). */
+pulse_status pulse_lin8_sizes(const pulse_lin8_desc* desc, int32_t tokens, size_t* weight_bytes,
+                              size_t* workspace_bytes);
+
+/* Lay out weights w [outputs][inputs] (w_dtype; contiguous, 16-byte aligned):
+ * with s[n] = m / 127, m the largest |w[n][k]| or 2^-100 where that is larger,
+ * q[n][k] = round(w[n][k] (127 / m)), to nearest even; both quotients and the
+ * product are rounded to fp32.  A row that holds a NaN or an infinity gives NaN.
+ * `weights` is 256-byte aligned. */
+pulse_status pulse_lin8_pack(const pulse_lin8_desc* desc, const void* w, int32_t w_dtype,
+                             void* weights, size_t weight_bytes, void* stream);
+
+/* y = act(s_x[t] s_w[n] sum_k q_x[t][k] q_w[n][k] + bias[n]), where every row
+ * of x is laid out as the rows of w are.  The sum is exact in integers, the rest
+ * fp32, rounded once.  bias is fp32 [outputs], 16-byte aligned, or NULL.  A row of x
+ * that holds a NaN or an infinity gives NaN, and reaches no other.  y must not
+ * overlap x.  The workspace is 256-byte aligned. */
+pulse_status pulse_lin8_forward(const pulse_lin8_desc* desc, int32_t tokens, const pulse_rows* x,
+                                const void* weights, size_t weight_bytes, const float* bias,
+                                const pulse_rows* y, void* workspace, size_t workspace_bytes,
+                                void* stream);
 
 /* ---- gradient norm and clipping ------------------------------------------- */
 

@@ -38,8 +38,9 @@ CFLAGS = [
 ]
 
 SOURCES = ["igemm2.hip", "norm.hip", "misc.hip", "probe.hip", "attn.hip",
-           "tnorm.hip", "mask.hip", "rope.hip", "mattn.hip", "clip.hip", "stage.cpp",
-           "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp"]
+           "tnorm.hip", "mask.hip", "rope.hip", "mattn.hip", "clip.hip", "bnorm.hip", "keep.hip",
+           "kgrad.hip", "lin8.hip", "stage.cpp",
+           "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp", "rowops.cpp"]
 
 # The stages' attention takes maxima of MFMA results: with the IEEE mode bit
 # off fmaxf needs no quieting copy of each operand, which halves the VALU work
@@ -54,7 +55,7 @@ SOURCE_FLAGS = {"attn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}
 # -fsanitize applies to the host pass alone; the kernels are not built with it.
 ASAN_BUILD = os.path.join(ROOT, "_build_asan")
 ASAN_LIB = os.path.join(ASAN_BUILD, "libpulse_stage_asan.so")
-HOST_SOURCES = ["stage.cpp", "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp"]
+HOST_SOURCES = ["stage.cpp", "tstage.cpp", "sched.cpp", "partition.cpp", "ops.cpp", "rowops.cpp"]
 ASAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
               "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-fno-sanitize-recover=all",
               "-g"]

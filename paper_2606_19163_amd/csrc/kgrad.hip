@@ -1,0 +1,403 @@
+// Weight gradient of a linear layer whose input is kept in 8 bits (gfx950):
+// dw[n][c] = sum_t dy[t][n] x[t][c] on bf16 MFMA.  A kept value is a whole
+// number of at most 7 bits times a power of two, which bf16 holds exactly, so
+// that products are exact and only the fp32 sums round.
+#include "keepvec.hpp"
+
+namespace pulse {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+// what lanes past the last token or output fetch
+__device__ __attribute__((aligned(16))) const uint32_t kgrad_zero[4] = {0, 0, 0, 0};
+
+constexpr int BK = 64;  // tokens per step
+
+// Tiles are token-major rows of P bytes, row r rotated by a (r & 3) + b ((r >>
+// 3) & 1) units of 32 bytes, so that each half-wave of a transpose read (rows
+// {0..3, 8..11} or {16..19, 24..27} of a 32-row slice, 32 bytes per row) hits
+// 8 distinct 32-byte bank groups of the 64-bank LDS.
+constexpr int rot_bad(int P, int a, int b) {
+  const int U = P / 32;
+  int bad = 0;
+  for (int hw = 0; hw < 2; ++hw)
+    for (int u = 0; u < U; ++u) {
+      int seen = 0;
+      for (int g = 2 * hw; g < 2 * hw + 2; ++g)
+        for (int q = 0; q < 4; ++q) {
+          const int r = 8 * g + q;
+          const int grp = (r * U + (u + a * (r & 3) + b * ((r >> 3) & 1)) % U) % 8;
+          if ((seen >> grp) & 1) ++bad;
+          seen |= 1 << grp;
+        }
+    }
+  return bad;
+}
+constexpr int best_rot(int P) {  // a + 256 b of the first pair with the fewest conflicts
+  const int U = P / 32;
+  int best = 0, least = 1 << 30;
+  for (int a = 0; a < U; ++a)
+    for (int b = 0; b < U; ++b) {
+      const int bad = rot_bad(P, a, b);
+      if (bad < least) {
+        best = a + 256 * b;
+        least = bad;
+      }
+    }
+  return best;
+}
+template <int P>
+__device__ __forceinline__ int rot_of(int r) {
+  constexpr int R = best_rot(P);
+  return 2 * ((R % 256) * (r & 3) + (R / 256) * ((r >> 3) & 1));
+}
+// slot of 16-byte chunk c of row r, and the chunk in slot s
+template <int P>
+__device__ __forceinline__ int slot_of(int c, int r) {
+  return (c + rot_of<P>(r)) % (P / 16);
+}
+template <int P>
+__device__ __forceinline__ int chunk_in(int s, int r) {
+  return (s + 4 * (P / 16) - rot_of<P>(r)) % (P / 16);
+}
+
+// BN outputs x BC channels per block, WN x WC per wave
+template <int BN_, int BC_, int WN_, int WC_>
+struct Tile {
+  static constexpr int BN = BN_, BC = BC_, WN = WN_, WC = WC_;
+  static constexpr int WAVES_N = BN / WN, WAVES_C = BC / WC, NW = WAVES_N * WAVES_C;
+  static constexpr int NT = NW * 64;
+  static constexpr int TN = WN / 16, TC = WC / 16;
+  static constexpr int PY = BN * 2, PX = BC * 2;  // row bytes
+  static constexpr int Y_BYTES = BK * PY, X_BYTES = BK * PX, STAGE = Y_BYTES + X_BYTES;
+  static constexpr int YU = Y_BYTES / (NT * 16);  // 16-byte loads per thread and step
+  static constexpr int XU = BK * BC / (NT * 16);
+  static constexpr int LDS = 2 * STAGE;
+  static_assert(YU * NT * 16 == Y_BYTES && XU * NT * 16 == BK * BC && XU >= 1, "loads");
+  static_assert(36 * PY < 65536 && Y_BYTES + 36 * PX < 65536 && LDS <= 160 * 1024, "LDS");
+  static_assert(4 * 3 * (BN / 16 + 4) < 4096, "rotations stay below 4 rows of chunks");
+};
+
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+
+// ds_read_b64_tr_b16 at addr + OFF: four tokens of a column.  Inline, since the
+// compiler would wait for the LDS-DMA before it; the caller waits (lgkm_wait).
+template <int OFF>
+__device__ __forceinline__ v4s ds_rdtr(uint32_t addr) {
+  v4s v;
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+__device__ __forceinline__ void lgkm_wait0() {
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+}
+__device__ __forceinline__ void vm_wait0() {
+  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));
+}
+// the MFMAs that use v stay below the waits before this
+__device__ __forceinline__ void tie(bf16x8_t& v) { asm volatile("" : "+v"(v)); }
+
+__device__ __forceinline__ int xcd_order(int b, int n) {
+  const int q = n >> 3, r = n & 7, x = b & 7;
+  return x * q + (x < r ? x : r) + (b >> 3);
+}
+
+struct Split {
+  int tilesC, tiles, chunk;  // chunk: tokens per split, a multiple of BK
+  int splits;
+  float *part, *bias;        // partial dw [split][N][C] (splits > 1), db [split tilesC][N]
+};
+
+template <class C, bool BIAS>
+__global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uint8_t* q,
+                                                 const uint8_t* e) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[C::LDS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wn = wave % C::WAVES_N, wc = wave / C::WAVES_N;
+  const int lb = xcd_order(blockIdx.x, gridDim.x);
+  const int z = lb / s.tiles, tile = lb - z * s.tiles;
+  const int tn = tile / s.tilesC, tc = tile - tn * s.tilesC;
+  const int n0 = tn * C::BN, c0 = tc * C::BC;
+  const long P = (a.C + 31) / 32 * 32;
+  const long tbeg = (long)z * s.chunk;
+  const int len = (int)min((long)s.chunk, a.tokens - tbeg);  // tokens of this split
+  const int KT = (len + BK - 1) / BK;
+
+  // dy goes straight to LDS: lane slot i of a load is chunk_in(i) of its row
+  const uint16_t* ysrc[C::YU];
+  int yrow[C::YU];
+#pragma unroll
+  for (int u = 0; u < C::YU; ++u) {
+    const int i = u * C::NT + tid;
+    const int r = i / (C::PY / 16);
+    const int n = n0 + 8 * chunk_in<C::PY>(i - r * (C::PY / 16), r);
+    yrow[u] = n < a.N ? r : 1 << 30;
+    ysrc[u] = static_cast<const uint16_t*>(a.dy) + (tbeg + r) * a.dyt + n;
+  }
+  // x goes through registers: 16 bytes of a row become 32
+  const uint8_t *xsrc[C::XU], *esrc[C::XU];
+  int xrow[C::XU];
+  uint32_t xdst[C::XU];
+#pragma unroll
+  for (int u = 0; u < C::XU; ++u) {
+    const int i = u * C::NT + tid;
+    const int r = i / (C::BC / 16), k = i - r * (C::BC / 16);
+    const int c = c0 + 16 * k;
+    xrow[u] = c < P ? r : 1 << 30;
+    xsrc[u] = q + (tbeg + r) * P + c;
+    esrc[u] = e + (tbeg + r) * (P >> 5) + (c >> 5);
+    xdst[u] = (uint32_t)(C::Y_BYTES + r * C::PX + 16 * slot_of<C::PX>(2 * k, r));
+  }
+  uint4 xq[C::XU];
+  uint32_t xe[C::XU];
+  auto fetch_x = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < C::XU; ++u) {
+      // 128 four times, and any exponent: 0
+      xq[u] = uint4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+      xe[u] = 0;
+      if (kt * BK + xrow[u] < len) {
+        xq[u] = *reinterpret_cast<const uint4*>(xsrc[u] + (long)kt * BK * P);
+        xe[u] = esrc[u][(long)kt * BK * (P >> 5)];
+      }
+    }
+  };
+  auto store_x = [&](int kt) __attribute__((always_inline)) {
+    char* base = smem + (kt & 1) * C::STAGE;
+#pragma unroll
+    for (int u = 0; u < C::XU; ++u) {
+      const float step = keep_step(xe[u]);
+      float v[16];
+      unkeep4(v, xq[u].x, step);
+      unkeep4(v + 4, xq[u].y, step);
+      unkeep4(v + 8, xq[u].z, step);
+      unkeep4(v + 12, xq[u].w, step);
+      uint4* d = reinterpret_cast<uint4*>(base + xdst[u]);
+      d[0] = uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+      d[1] = uint4{pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]),
+                   pack2(v[14], v[15])};
+    }
+  };
+  auto fetch_y = [&](int kt) __attribute__((always_inline)) {
+    char* base = smem + (kt & 1) * C::STAGE;
+#pragma unroll
+    for (int u = 0; u < C::YU; ++u) {
+      const void* g = kt * BK + yrow[u] < len
+                          ? static_cast<const void*>(ysrc[u] + (long)kt * BK * a.dyt)
+                          : static_cast<const void*>(kgrad_zero);
+      __builtin_amdgcn_global_load_lds(g, (lds_ptr_t)(base + (u * C::NT + wave * 64) * 16), 16, 0,
+                                       0);
+    }
+  };
+
+  // a lane's column and first token in the transpose reads
+  const int g16 = lane >> 4, j16 = lane & 15;
+  const int trow = 8 * g16 + (j16 >> 2), tcol = 4 * (j16 & 3);
+  uint32_t rx[C::TC], ry[C::TN];
+#pragma unroll
+  for (int i = 0; i < C::TC; ++i) {
+    const int col = wc * C::WC + i * 16 + tcol;
+    rx[i] = (uint32_t)(C::Y_BYTES + trow * C::PX + slot_of<C::PX>(col >> 3, trow) * 16 +
+                       (col & 7) * 2);
+  }
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int col = wn * C::WN + j * 16 + tcol;
+    ry[j] = (uint32_t)(trow * C::PY + slot_of<C::PY>(col >> 3, trow) * 16 + (col & 7) * 2);
+  }
+  f32x4_t acc[C::TC][C::TN], sum[C::TN];
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    sum[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8_t ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
+
+  const uint32_t sbase = lds_at(smem);
+  auto half = [&](uint32_t sb, bool bias, auto tag) __attribute__((always_inline)) {
+    constexpr int S = decltype(tag)::value;
+    bf16x8_t fx[C::TC], fy[C::TN];
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) {
+      const v4s lo = ds_rdtr<(S * 32 + 0) * C::PX>(sb + rx[i]);
+      const v4s hi = ds_rdtr<(S * 32 + 4) * C::PX>(sb + rx[i]);
+      fx[i] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const v4s lo = ds_rdtr<(S * 32 + 0) * C::PY>(sb + ry[j]);
+      const v4s hi = ds_rdtr<(S * 32 + 4) * C::PY>(sb + ry[j]);
+      fy[j] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    lgkm_wait0();
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) tie(fx[i]);
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) tie(fy[j]);
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], fy[j], acc[i][j], 0, 0, 0);
+    if (BIAS && bias)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+        sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fy[j], sum[j], 0, 0, 0);
+  };
+
+  if (KT > 0) {
+    fetch_x(0);
+    store_x(0);
+    fetch_y(0);
+    if (KT > 1) fetch_x(1);
+  }
+  for (int kt = 0; kt < KT; ++kt) {
+    // this step's tiles are there, and all waves are done with the other stage
+    vm_wait0();
+    lgkm_wait0();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < KT) {
+      store_x(kt + 1);
+      fetch_y(kt + 1);
+      if (kt + 2 < KT) fetch_x(kt + 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // the tiles along C share the steps of the columns' sums, their waves' halves
+    const bool mine = kt % s.tilesC == tc && wc == 0;
+    const uint32_t sb = sbase + (uint32_t)((kt & 1) * C::STAGE);
+    half(sb, mine, std::integral_constant<int, 0>());
+    half(sb, mine, std::integral_constant<int, 1>());
+  }
+
+  // lane: channels 4 g16 .. + 3 of output j16 of each 16 x 16
+  float* dst = s.splits > 1 ? s.part + (long)z * a.N * a.C : a.dw;
+  const bool add = s.splits == 1 && a.accumulate;
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = n0 + wn * C::WN + j * 16 + j16;
+    if (n >= a.N) continue;
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) {
+      const int c = c0 + wc * C::WC + i * 16 + 4 * g16;
+      if (c >= a.C) continue;
+      f32x4_t* p = reinterpret_cast<f32x4_t*>(dst + (long)n * a.C + c);
+      *p = add ? *p + acc[i][j] : acc[i][j];
+    }
+    if (BIAS && wc == 0 && g16 == 0) s.bias[((long)z * s.tilesC + tc) * a.N + n] = sum[j][0];
+  }
+#endif
+}
+
+// Blocks below `wblocks`: four values of dw each thread, summed over the
+// splits; the others: db, 64 outputs x 4 lanes of partial sums.
+__global__ __launch_bounds__(256) void k_kgrad_sum(KgradArgs a, Split s, int wblocks) {
+  if ((int)blockIdx.x < wblocks) {
+    const long at = 4 * ((long)blockIdx.x * 256 + threadIdx.x), total = (long)a.N * a.C;
+    if (at >= total) return;
+    float4 v = *reinterpret_cast<const float4*>(s.part + at);
+    for (int z = 1; z < s.splits; ++z) {
+      const float4 w = *reinterpret_cast<const float4*>(s.part + z * total + at);
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    float4* p = reinterpret_cast<float4*>(a.dw + at);
+    if (a.accumulate) {
+      const float4 w = *p;
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    *p = v;
+    return;
+  }
+  __shared__ float sm[4][64];
+  const int lane = threadIdx.x & 63, k = threadIdx.x >> 6;
+  const int n = (blockIdx.x - wblocks) * 64 + lane;
+  float v = 0.f;
+  if (n < a.N)
+    for (int r = k; r < s.splits * s.tilesC; r += 4) v += s.bias[(long)r * a.N + n];
+  sm[k][lane] = v;
+  __syncthreads();
+  if (k == 0 && n < a.N) {
+    v = (sm[0][lane] + sm[1][lane]) + (sm[2][lane] + sm[3][lane]);
+    a.db[n] = a.accumulate ? a.db[n] + v : v;
+  }
+}
+
+__global__ __launch_bounds__(256) void k_kgrad_clear(float* p, long n) {
+  const long i = 4 * ((long)blockIdx.x * 256 + threadIdx.x);  // n is a multiple of 8
+  if (i < n) *reinterpret_cast<float4*>(p + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+struct Plan {
+  bool large;
+  Split s;
+  size_t floats;
+};
+
+Plan plan_of(int tokens, int C, int N) {
+  Plan p{};
+  const long tl = (long)((N + 255) / 256) * ((C + 127) / 128);
+  p.large = tl * ((tokens + 1023) / 1024) >= 128;
+  const int bn = p.large ? 256 : 64, bc = p.large ? 128 : 64;
+  p.s.tilesC = (C + bc - 1) / bc;
+  p.s.tiles = (N + bn - 1) / bn * p.s.tilesC;
+  const int steps = (tokens + BK - 1) / BK;
+  const int room = p.large ? 256 : 512;
+  int splits = p.s.tiles >= room ? 1 : room / p.s.tiles;
+  if (splits > (steps + 3) / 4) splits = (steps + 3) / 4;
+  if (splits < 1) splits = 1;
+  p.s.chunk = (steps + splits - 1) / splits * BK;
+  p.s.splits = tokens ? (tokens + p.s.chunk - 1) / p.s.chunk : 1;
+  const size_t part = p.s.splits > 1 ? (size_t)p.s.splits * N * C : 0;
+  p.floats = part + (size_t)p.s.splits * p.s.tilesC * N;
+  return p;
+}
+
+template <class C>
+hipError_t run(const KgradArgs& a, const Split& s, hipStream_t st) {
+  const uint8_t* q = static_cast<const uint8_t*>(a.kept);
+  auto kern = a.db ? k_kgrad<C, true> : k_kgrad<C, false>;
+  hipLaunchKernelGGL(kern, dim3(s.tiles * s.splits), dim3(C::NT), 0, st, a, s, q,
+                     q + keep_exps_at(a.C, a.tokens));
+  return hipGetLastError();
+}
+
+hipError_t clear(float* p, long n, hipStream_t st) {
+  hipLaunchKernelGGL(k_kgrad_clear, dim3((n / 4 + 255) / 256), dim3(256), 0, st, p, n);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t kgrad_bytes(int tokens, int C, int N) { return plan_of(tokens, C, N).floats * 4; }
+
+hipError_t launch_kgrad(const KgradArgs& a, hipStream_t st) {
+  if (a.tokens == 0) {
+    if (a.accumulate) return hipSuccess;
+    const hipError_t e = clear(a.dw, (long)a.N * a.C, st);
+    return e != hipSuccess || !a.db ? e : clear(a.db, a.N, st);
+  }
+  Plan p = plan_of(a.tokens, a.C, a.N);
+  p.s.part = a.ws;
+  p.s.bias = a.ws + (p.s.splits > 1 ? (size_t)p.s.splits * a.N * a.C : 0);
+  hipError_t e = p.large ? run<Tile<256, 128, 64, 64>>(a, p.s, st)
+                         : run<Tile<64, 64, 32, 32>>(a, p.s, st);
+  if (e != hipSuccess) return e;
+  const int wblocks = p.s.splits > 1 ? (int)(((long)a.N * a.C / 4 + 255) / 256) : 0;
+  const int blocks = wblocks + (a.db ? (a.N + 63) / 64 : 0);
+  if (!blocks) return hipSuccess;
+  hipLaunchKernelGGL(k_kgrad_sum, dim3(blocks), dim3(256), 0, st, a, p.s, wblocks);
+  return hipGetLastError();
+}
+
+}  // namespace pulse

@@ -1,6 +1,7 @@
 // Internal launcher interface of the packed-sequence operators (mask.hip,
-// rope.hip, mattn.hip, clip.hip); not part of the public ABI.  Arguments have
-// been validated by ops.cpp.
+// rope.hip, mattn.hip, clip.hip, bnorm.hip, keep.hip, kgrad.hip, lin8.hip); not
+// part of the public ABI.  Arguments have been validated by ops.cpp and
+// rowops.cpp.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -57,6 +58,81 @@ size_t mattn_fwd_bytes(const pulse_attn_desc& d);
 size_t mattn_bwd_bytes(const pulse_attn_desc& d);
 hipError_t launch_mattn_fwd(const MattnArgs& a, hipStream_t st);
 hipError_t launch_mattn_bwd(const MattnArgs& a, hipStream_t st);
+
+// ---- norms of a block (bnorm.hip) --------------------------------------------
+
+// strides in elements; unused pointers are null
+struct NormArgs {
+  int tokens, C, docs, pre, post, branch, dtype, stream_dtype;
+  float eps, r;
+  const int32_t* off;
+  const float *gate, *scale, *shift;
+  long gate_t, scale_t, shift_t;
+  const float *weight, *bias, *post_weight;
+  const void *x, *y, *du, *dh;
+  void *h, *u, *dx, *dy;  // h is read by the backward pass
+  long xt, yt, ht, ut, dut, dht, dxt, dyt;
+};
+
+size_t norm_bwd_bytes(const pulse_norm_desc& d, int tokens);
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st);
+hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* ws,
+                           hipStream_t st);
+
+// ---- activations in 8 bits (keep.hip, kgrad.hip) -----------------------------
+
+constexpr int KEEP_GROUP = 32;
+inline int64_t keep_pitch(int channels) { return (channels + 31) / 32 * 32; }
+inline size_t keep_values(int channels, int tokens) { return (size_t)tokens * keep_pitch(channels); }
+inline size_t keep_exps_at(int channels, int tokens) {
+  return (keep_values(channels, tokens) + 15) / 16 * 16;
+}
+inline size_t keep_bytes(int channels, int tokens) {
+  return keep_exps_at(channels, tokens) + (size_t)tokens * (keep_pitch(channels) / 32);
+}
+
+// x (or da) read, y (a, the loaded rows, or dx) written; strides in elements
+struct KeepArgs {
+  int tokens, C, act, dtype;
+  const void* x;
+  void* y;
+  long xt, yt;
+  void* kept;    // values, then exponents
+  void* a_kept;  // or null
+};
+hipError_t launch_keep_save(const KeepArgs& a, hipStream_t st);
+hipError_t launch_keep_load(const KeepArgs& a, hipStream_t st);
+hipError_t launch_keep_back(const KeepArgs& a, hipStream_t st);
+
+struct KgradArgs {
+  int tokens, C, N;
+  const void* dy;
+  long dyt;
+  const void* kept;
+  float *dw, *db;
+  int accumulate;
+  float* ws;
+};
+size_t kgrad_bytes(int tokens, int C, int N);
+hipError_t launch_kgrad(const KgradArgs& a, hipStream_t st);
+
+// ---- linear layers in 8-bit integers (lin8.hip) --------------------------------
+
+struct Lin8Args {
+  int tokens, K, N, act;
+  const void* x;
+  long xt;
+  const void* weights;
+  const float* bias;
+  void* y;
+  long yt;
+  void* ws;
+};
+size_t lin8_weight_bytes(int K, int N);
+size_t lin8_ws_bytes(int tokens, int K, int N);
+hipError_t launch_lin8_pack(int K, int N, const void* w, int w_dtype, void* weights,
+                            hipStream_t st);
+hipError_t launch_lin8(const Lin8Args& a, hipStream_t st);
 
 // ---- gradient norm and clipping (clip.hip) -----------------------------------
 

@@ -1,43 +1,16 @@
 // C ABI of the packed-sequence operators (pulse_ops.h): checks of the host
 // arguments, then one launcher call each (okernels.hpp).
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <new>
 #include <vector>
 
-#include "error.hpp"
-#include "okernels.hpp"
+#include "ocheck.hpp"
 
 using namespace pulse;
 
 namespace {
 
-pulse_status ofail(pulse_status s, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  return set_last_error(s, buf);
-}
-
-#define OCHK(expr)                    \
-  do {                                \
-    pulse_status s_ = (expr);         \
-    if (s_ != PULSE_OK) return s_;    \
-  } while (0)
-
-pulse_status launched(hipError_t e, const char* what) {
-  return e == hipSuccess ? PULSE_OK
-                         : ofail(PULSE_E_HIP, "%s failed: %s", what, hipGetErrorString(e));
-}
-
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-constexpr int MAX_TOKENS = 1 << 24;
 constexpr int MAX_HEADS = 1024;
-constexpr int64_t MAX_EXTENT = INT64_C(1) << 47;
 
 // a [tokens][heads][dim] view; `out`: written, so its elements are distinct
 pulse_status check_heads(const pulse_heads* x, const char* name, int tokens, int heads, int dim,
@@ -122,15 +95,6 @@ pulse_status check_attn(const pulse_attn_desc* d) {
   if (!std::isfinite(d->scale)) return ofail(PULSE_E_INVALID_ARG, "scale must be finite");
   if (!(d->cap >= 0.f) || !std::isfinite(d->cap))
     return ofail(PULSE_E_INVALID_ARG, "cap must be finite and >= 0");
-  return PULSE_OK;
-}
-
-pulse_status check_ws(const void* ws, size_t have, size_t need) {
-  if (need == 0) return PULSE_OK;
-  if (!ws) return ofail(PULSE_E_INVALID_ARG, "workspace is NULL");
-  if (!aligned(ws, 256)) return ofail(PULSE_E_INVALID_ARG, "workspace is not 256-byte aligned");
-  if (have < need)
-    return ofail(PULSE_E_INVALID_ARG, "workspace has %zu bytes, needs %zu", have, need);
   return PULSE_OK;
 }
 

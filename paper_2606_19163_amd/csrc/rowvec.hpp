@@ -1,0 +1,117 @@
+// Device helpers of the row operators (bnorm.hip, keep.hip, lin8.hip): 8
+// channels as fp32, sums over the lanes that share a row, activations.
+#pragma once
+
+#include "common.hpp"
+#include "okernels.hpp"
+
+namespace pulse {
+
+// 8 channels in memory, and as fp32
+template <typename T>
+struct Vec8;
+template <>
+struct Vec8<uint16_t> {
+  uint4 w;
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    w = *reinterpret_cast<const uint4*>(p);
+  }
+  __device__ __forceinline__ void zero() { w = uint4{0, 0, 0, 0}; }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t x = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+    return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
+  }
+};
+template <>
+struct Vec8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ float get(int i) const {
+    const float4& x = i < 4 ? a : b;
+    return (i & 3) == 0 ? x.x : (i & 3) == 1 ? x.y : (i & 3) == 2 ? x.z : x.w;
+  }
+};
+
+__device__ __forceinline__ void put8(uint16_t* p, const float (&v)[8]) {
+  *reinterpret_cast<uint4*>(p) =
+      uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+}
+__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// v of lane ^ 1, 2 (quad permutes), of the mirrored lane of 8 and of 16
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+
+struct Add {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// op over the 16 (32, 64) lanes that hold a row, the same on each: vector
+// instructions alone, where a shuffle would go through LDS
+template <int L, class Op>
+__device__ __forceinline__ float lanes_op(float v, Op op) {
+  v = op(v, dpp<DPP_XOR1>(v));
+  v = op(v, dpp<DPP_XOR2>(v));
+  v = op(v, dpp<DPP_HALF_MIRROR>(v));
+  v = op(v, dpp<DPP_MIRROR>(v));
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                    false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                    false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  return v;
+}
+
+// sums of a and b over the L lanes of a row; L = 256 takes the whole block and
+// 8 floats of LDS, which alternate between two such sets
+template <int L>
+__device__ __forceinline__ void row_sums(float& a, float& b, float* sm, int& turn) {
+  a = lanes_op<L>(a, Add());
+  b = lanes_op<L>(b, Add());
+  if constexpr (L == 256) {
+    float* s = sm + 8 * turn;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+      s[threadIdx.x >> 6] = a;
+      s[4 + (threadIdx.x >> 6)] = b;
+    }
+    __syncthreads();
+    a = (s[0] + s[1]) + (s[2] + s[3]);
+    b = (s[4] + s[5]) + (s[6] + s[7]);
+  }
+}
+
+// act(z) and act'(z), `act` a pulse_act
+template <int ACT>
+__device__ __forceinline__ float act_f(float z) {
+  if constexpr (ACT == PULSE_ACT_GELU) return gelu_f(z);
+  if constexpr (ACT == PULSE_ACT_SILU) return silu_f(z);
+  return z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_d(float z) {
+  if constexpr (ACT == PULSE_ACT_GELU) return gelu_d(z);
+  if constexpr (ACT == PULSE_ACT_SILU) return dsilu_f(z);
+  return 1.f;
+}
+
+}  // namespace pulse

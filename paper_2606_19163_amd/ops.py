@@ -4,12 +4,17 @@ Images and clips of several resolutions lie one after another in one sequence,
 a document each.  :class:`Mask` says which keys every query row attends,
 :class:`Rope` turns query and key heads by their positions, :class:`Attn` is
 attention under such a mask, forward and backward, and :class:`GradClip` the
-global gradient norm with clipping.
+global gradient norm with clipping.  Around the attention, :class:`Norm` is the
+joint between two halves of a block (gate, residual, norms, the documents'
+scales and shifts), :class:`Checkpoint` keeps activations in 8 bits until the
+backward pass and computes gradients from them, and :class:`Linear8` is a linear
+layer in 8-bit integers for sampling.
 
 Argument marshalling only: every step runs in the library's HIP kernels, and
 loading fails loudly when the library has not been built.  Tensors are
 ``[tokens, heads, head_dim]`` with the last axis contiguous; the other two may
-be strided (the heads inside a projection's output, or head-major storage).
+be strided (the heads inside a projection's output, or head-major storage), or
+``[tokens, channels]`` with strided rows.
 Gradients come from the ``backward`` methods; autograd sees none of this, so a
 call refuses inputs that require a gradient where torch records one.  Work is
 enqueued on ``stream`` (default: torch's current one), and what a call allocates
@@ -27,13 +32,16 @@ import torch
 
 from .stage import BF16, F32, E_INVALID_ARG, PulseError, _check, lib as _lib
 
-__all__ = ["Rope", "Mask", "Attn", "Saved", "GradClip", "rope_freqs", "grid_positions", "MaskRow"]
+__all__ = ["Rope", "Mask", "Attn", "Saved", "GradClip", "Norm", "Checkpoint", "Kept", "Linear8",
+           "rope_freqs", "grid_positions", "MaskRow"]
 
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
 _vp = ctypes.c_void_p
 _szp = ctypes.POINTER(ctypes.c_size_t)
 _PAIRS = {"adjacent": 0, "halves": 1}
+_NORMS = {None: 0, "layer": 1, "rms": 2}
+_ACTS = {None: 0, "gelu": 1, "silu": 2}
 
 
 class Heads(ctypes.Structure):
@@ -61,6 +69,35 @@ class AttnDesc(ctypes.Structure):
 
 class ClipTensor(ctypes.Structure):
     _fields_ = [("grad", _vp), ("out", _vp), ("n", _i64), ("dtype", ctypes.c_int)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("ptr", _vp), ("token_stride", _i64)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("channels", _i32), ("docs", _i32), ("pre", _i32), ("post", _i32),
+                ("branch", _i32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("dtype", _i32), ("stream_dtype", _i32)]
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [("offsets", _vp), ("gate", _vp), ("scale", _vp), ("shift", _vp),
+                ("gate_stride", _i64), ("scale_stride", _i64), ("shift_stride", _i64),
+                ("weight", _vp), ("bias", _vp), ("post_weight", _vp)]
+
+
+class NormGrads(ctypes.Structure):
+    _fields_ = [("dgate", _vp), ("dscale", _vp), ("dshift", _vp), ("dweight", _vp),
+                ("dbias", _vp), ("dpost_weight", _vp)]
+
+
+class KeepDesc(ctypes.Structure):
+    _fields_ = [("channels", _i32), ("act", _i32), ("dtype", _i32)]
+
+
+class Lin8Desc(ctypes.Structure):
+    _fields_ = [("inputs", _i32), ("outputs", _i32), ("act", _i32), ("dtype", _i32)]
 
 
 # torch.cuda.current_stream() builds an object that only its handle is read from
@@ -103,6 +140,24 @@ def lib():
         L.pulse_clip_bind.restype = st
         L.pulse_clip_run.argtypes = [_vp, f, f, _vp, _vp]
         L.pulse_clip_run.restype = st
+        rp, sz, nd = ctypes.POINTER(Rows), ctypes.c_size_t, ctypes.POINTER(NormDesc)
+        pp, gp = ctypes.POINTER(NormParams), ctypes.POINTER(NormGrads)
+        kd, ld = ctypes.POINTER(KeepDesc), ctypes.POINTER(Lin8Desc)
+        for name, args in (
+                ("norm_sizes", [nd, _i32, _szp]),
+                ("norm_forward", [nd, _i32, rp, rp, pp, rp, rp, _vp]),
+                ("norm_backward", [nd, _i32, rp, rp, rp, rp, pp, rp, rp, gp, _vp, sz, _vp]),
+                ("keep_sizes", [kd, _i32, _szp]),
+                ("keep_save", [kd, _i32, rp, rp, _vp, sz, _vp]),
+                ("keep_load", [kd, _i32, _vp, sz, rp, _vp]),
+                ("keep_backward", [kd, _i32, rp, _vp, sz, rp, _vp, sz, _vp]),
+                ("keep_wgrad_sizes", [kd, _i32, _i32, _szp]),
+                ("keep_wgrad", [kd, _i32, _i32, rp, _vp, sz, _vp, _vp, _i32, _vp, sz, _vp]),
+                ("lin8_sizes", [ld, _i32, _szp, _szp]),
+                ("lin8_pack", [ld, _vp, _i32, _vp, sz, _vp]),
+                ("lin8_forward", [ld, _i32, rp, _vp, sz, _vp, rp, _vp, sz, _vp])):
+            fn = getattr(L, "pulse_" + name)
+            fn.argtypes, fn.restype = args, st
         _bound = L
     return _bound
 
@@ -130,6 +185,18 @@ def _heads(t, name, shape, dtype, dev):
         _bad(f"{name} is on {t.device}, not on the current GPU")
     # the stride of an axis of one element is never used
     return Heads(t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0)
+
+
+def _rows(t, name, shape, dtype, dev):
+    """The view [tokens, channels] `t` of GPU `dev`, where the call runs."""
+    if t.dtype is not dtype or t.shape != shape:
+        _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
+    s0, s1 = t.stride()
+    if s1 != 1:
+        _bad(f"{name}: the channels of a row must be contiguous")
+    if t.get_device() != dev:
+        _bad(f"{name} is on {t.device}, not on the current GPU")
+    return Rows(t.data_ptr(), s0 if shape[0] > 1 else 0)
 
 
 def _flat(t, name, n, dtype, dev):
@@ -512,3 +579,376 @@ class GradClip:
         _check(lib().pulse_clip_run(self.h, max_norm, eps,
                                     _flat(norm, "norm", 1, torch.float32, dev), s))
         return norm
+
+
+def _choice(v, among, name):
+    if v not in among:
+        _bad(f"{name} must be one of {sorted(map(str, among))}, not {v!r}")
+    return among[v]
+
+
+def _bytes_at(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class Norm:
+    """The joint between two halves of a transformer block:
+
+        h = x + residual_scale * gate[doc] * Post(y)
+        u = Pre(h) * (1 + scale[doc]) + shift[doc]
+
+    with the residual stream x and h (``stream_dtype``), the last half's output y
+    and the next half's input u (``dtype``).  ``pre`` and ``post`` are "layer",
+    "rms" or None: the norm before the next half (None: the joint only adds, and
+    there is no u) and after the last one (None: y itself).  Without ``branch``
+    there is no y, and h is x.  Documents are rows [offsets[d], offsets[d + 1]) of
+    int32 ``offsets`` [docs + 1]; rows from the last offset on are padding, where h
+    = x and u = 0 and which no sum sees.  Without offsets all rows are the one
+    document's.  ``gate``, ``scale`` and ``shift`` are fp32 [docs, channels] (rows
+    may be strided), ``weight``, ``bias`` and ``post_weight`` fp32 [channels];
+    each may be left out."""
+
+    def __init__(self, channels, docs=1, pre="layer", post=None, branch=True, eps=1e-6,
+                 residual_scale=1.0, dtype=None, stream_dtype=None):
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        self.stream_dtype = self.dtype if stream_dtype is None else stream_dtype
+        self.channels, self.docs, self.branch = channels, docs, bool(branch)
+        self.pre, self.post = pre, post
+        self.desc = NormDesc(channels, docs, _choice(pre, _NORMS, "pre"),
+                             _choice(post, _NORMS, "post"), 1 if branch else 0, eps,
+                             residual_scale, _dtype(self.dtype), _dtype(self.stream_dtype))
+        n = ctypes.c_size_t()
+        _check(lib().pulse_norm_sizes(self.desc, 0, n))
+        self.sizes = {0: n.value}
+
+    def _cond(self, t, name, dev):
+        if t is None:
+            return None, 0
+        if t.dtype is not torch.float32 or t.shape != (self.docs, self.channels) or \
+                t.stride(1) != 1:
+            _bad(f"{name} must be fp32 [{self.docs}, {self.channels}] with contiguous rows, not "
+                 f"{t.dtype} {tuple(t.shape)}")
+        if t.get_device() != dev:
+            _bad(f"{name} is on {t.device}, not on the current GPU")
+        return t.data_ptr(), t.stride(0)
+
+    def _params(self, offsets, gate, scale, shift, weight, bias, post_weight, dev):
+        (g, gs), (s, ss), (f, fs) = (self._cond(gate, "gate", dev), self._cond(scale, "scale", dev),
+                                     self._cond(shift, "shift", dev))
+        c, f32 = self.channels, torch.float32
+        return NormParams(_flat(offsets, "offsets", self.docs + 1, torch.int32, dev), g, s, f, gs,
+                          ss, fs, _flat(weight, "weight", c, f32, dev),
+                          _flat(bias, "bias", c, f32, dev),
+                          _flat(post_weight, "post_weight", c, f32, dev))
+
+    def _branch(self, y):
+        if (y is not None) != self.branch:
+            _bad("y is missing" if self.branch else "y is given, and the joint has no branch")
+
+    def forward(self, x, y=None, offsets=None, gate=None, scale=None, shift=None, weight=None,
+                bias=None, post_weight=None, out=None, stream=None):
+        """(h, u), written into the tensors of ``out`` if given (h may be x's own
+        memory, u may be y's).  h is x without a branch, u is None without
+        ``pre``."""
+        if _grad_on():
+            _by_hand(("x", x), ("y", y), ("gate", gate), ("scale", scale), ("shift", shift),
+                     ("weight", weight), ("bias", bias), ("post_weight", post_weight))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward(x, y, offsets, gate, scale, shift, weight, bias, post_weight,
+                                    out)
+        self._branch(y)
+        dev, s = _here()
+        shape = (x.shape[0], self.channels)
+        h, u = (None, None) if out is None else out
+        if not self.branch:
+            h = x
+        elif h is None:
+            h = torch.empty(shape, dtype=self.stream_dtype, device=x.device)
+        if self.pre is None:
+            u = None
+        elif u is None:
+            u = torch.empty(shape, dtype=self.dtype, device=x.device)
+        _check(lib().pulse_norm_forward(
+            self.desc, shape[0], _rows(x, "x", shape, self.stream_dtype, dev),
+            _rows(y, "y", shape, self.dtype, dev) if self.branch else None,
+            self._params(offsets, gate, scale, shift, weight, bias, post_weight, dev),
+            _rows(h, "h", shape, self.stream_dtype, dev) if self.branch else None,
+            None if u is None else _rows(u, "u", shape, self.dtype, dev), s))
+        return h, u
+
+    def backward(self, du, h, dh=None, y=None, offsets=None, gate=None, scale=None, shift=None,
+                 weight=None, bias=None, post_weight=None, out=None, stream=None):
+        """Gradients as a dict: dx, dy (with a branch), and of each parameter that
+        is given (dgate, dscale, dshift, dweight, dbias, dpost_weight; fp32).  du is
+        the gradient of u, dh that of h as the next joint sees it (None: 0), h the
+        forward's (x without a branch).  ``out``: a dict of tensors to write into; dx
+        may be dh's own memory, dy may be du's or y's.  Without ``pre`` du and h are
+        None."""
+        if _grad_on():
+            _by_hand(("du", du), ("dh", dh), ("h", h), ("y", y))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(du, h, dh, y, offsets, gate, scale, shift, weight, bias,
+                                     post_weight, out)
+        self._branch(y)
+        if self.pre is not None and (du is None or h is None):
+            _bad("du or h is missing")
+        if self.pre is None and (du is not None or h is not None):
+            _bad("du or h is given, and the joint has no norm before the next half")
+        at = next((t for t in (du, dh, y) if t is not None), None)
+        if at is None:
+            _bad("no gradient is given")
+        dev, s = _here()
+        n, c, f32 = at.shape[0], self.channels, torch.float32
+        shape, device = (n, c), at.device
+        res = {} if out is None else dict(out)
+        wanted = [("dx", shape, self.stream_dtype)]
+        if self.branch:
+            wanted.append(("dy", shape, self.dtype))
+        for name, t in (("dgate", gate), ("dscale", scale), ("dshift", shift)):
+            if t is not None:
+                wanted.append((name, (self.docs, c), f32))
+        for name, t in (("dweight", weight), ("dbias", bias), ("dpost_weight", post_weight)):
+            if t is not None:
+                wanted.append((name, (c,), f32))
+        names = [w[0] for w in wanted]
+        for k in res:
+            if k not in names:
+                _bad(f"out has {k}, which this call does not compute")
+        for name, size, dt in wanted:
+            if res.get(name) is None:
+                res[name] = torch.empty(size, dtype=dt, device=device)
+        grads = NormGrads(*[_flat(res.get(k), k, (self.docs * c if k in ("dgate", "dscale", "dshift")
+                                                  else c), f32, dev)
+                            for k, _ in NormGrads._fields_])
+        need = self.sizes.get(n)
+        if need is None:
+            b = ctypes.c_size_t()
+            _check(lib().pulse_norm_sizes(self.desc, n, b))
+            need = self.sizes[n] = b.value
+        ws = _bytes_at(need, device)
+        st, dt = self.stream_dtype, self.dtype
+        _check(lib().pulse_norm_backward(
+            self.desc, n, None if du is None else _rows(du, "du", shape, dt, dev),
+            None if dh is None else _rows(dh, "dh", shape, st, dev),
+            None if h is None else _rows(h, "h", shape, st, dev),
+            _rows(y, "y", shape, dt, dev) if self.branch else None,
+            self._params(offsets, gate, scale, shift, weight, bias, post_weight, dev),
+            _rows(res["dx"], "dx", shape, st, dev),
+            _rows(res["dy"], "dy", shape, dt, dev) if self.branch else None, grads,
+            ws.data_ptr(), need, s))
+        return {k: res[k] for k in names}
+
+
+class Kept:
+    """Rows of ``channels`` channels in 8 bits: what :class:`Checkpoint` keeps."""
+
+    __slots__ = ("tokens", "channels", "bytes", "buffer", "ptr", "home", "full")
+
+    def __init__(self, tokens, channels, device="cuda"):
+        n = ctypes.c_size_t()
+        _check(lib().pulse_keep_sizes(KeepDesc(channels, 0, BF16), tokens, n))
+        self.tokens, self.channels, self.bytes = tokens, channels, n.value
+        self.buffer = _bytes_at(max(n.value, 16), device)
+        self.ptr, self.home, self.full = self.buffer.data_ptr(), _home(self.buffer), False
+
+
+class Checkpoint:
+    """Activations of ``channels`` channels kept in 8 bits until the backward
+    pass.  Groups of 32 channels share a power of two; a kept value is a whole
+    number of at most 127 times it, which bf16 holds exactly.  ``act`` ("gelu" or
+    "silu"): the activation function that follows x, for :meth:`forward` and
+    :meth:`backward`; x and its function's value and gradient are ``dtype``."""
+
+    def __init__(self, channels, act=None, dtype=None):
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        self.channels, self.act = channels, act
+        self.desc = KeepDesc(channels, _choice(act, _ACTS, "act"), _dtype(self.dtype))
+        self.sizes = {}
+        _check(lib().pulse_keep_sizes(self.desc, 0, ctypes.c_size_t()))
+
+    def buffer(self, tokens, device="cuda"):
+        """Room for the kept rows of ``tokens`` tokens."""
+        return Kept(tokens, self.channels, device)
+
+    def _kept(self, kept, name, tokens, dev, s, read):
+        if kept.channels != self.channels or tokens is not None and kept.tokens != tokens:
+            _bad(f"{name} is of {kept.tokens} tokens and {kept.channels} channels")
+        if read and not kept.full:
+            _bad(f"{name} holds nothing yet")
+        if kept.buffer.get_device() != dev:
+            _bad(f"{name} is on {kept.buffer.device}, not on the current GPU")
+        if s != kept.home:
+            _used_on(kept.buffer, dev)
+        return kept.ptr, kept.bytes
+
+    def save(self, x, out=None, kept=None, stream=None):
+        """Keep x (into ``kept`` of an earlier call, if given), and write act(x)
+        into ``out``, if given (it may be x); returns what is kept."""
+        if _grad_on():
+            _by_hand(("x", x))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.save(x, out, kept)
+        dev, s = _here()
+        n = x.shape[0]
+        shape = (n, self.channels)
+        if kept is None:
+            kept = Kept(n, self.channels, x.device)
+        _check(lib().pulse_keep_save(
+            self.desc, n, _rows(x, "x", shape, self.dtype, dev),
+            None if out is None else _rows(out, "out", shape, self.dtype, dev),
+            *self._kept(kept, "kept", n, dev, s, False), s))
+        kept.full = True
+        return kept
+
+    def forward(self, x, out=None, kept=None, stream=None):
+        """(act(x), kept)."""
+        if self.act is None:
+            _bad("there is no act: use save")
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward(x, out, kept)
+        if out is None:
+            out = torch.empty((x.shape[0], self.channels), dtype=self.dtype, device=x.device)
+        return out, self.save(x, out, kept)
+
+    def load(self, kept, out=None, stream=None):
+        """x as kept."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.load(kept, out)
+        dev, s = _here()
+        shape = (kept.tokens, self.channels)
+        at = self._kept(kept, "kept", None, dev, s, True)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=kept.buffer.device)
+        _check(lib().pulse_keep_load(self.desc, kept.tokens, *at,
+                                     _rows(out, "out", shape, self.dtype, dev), s))
+        return out
+
+    def backward(self, da, kept, out=None, again=None, stream=None):
+        """The gradient of x from that of act(x), at x as kept (``out`` may be
+        da).  ``again``: receives act(x) of x as kept, in 8 bits, for the next
+        layer's weight gradient."""
+        if _grad_on():
+            _by_hand(("da", da))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(da, kept, out, again)
+        dev, s = _here()
+        n = da.shape[0]
+        shape = (n, self.channels)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=da.device)
+        _check(lib().pulse_keep_backward(
+            self.desc, n, _rows(da, "da", shape, self.dtype, dev),
+            *self._kept(kept, "kept", n, dev, s, True),
+            _rows(out, "out", shape, self.dtype, dev),
+            *((None, 0) if again is None else self._kept(again, "again", n, dev, s, False)), s))
+        if again is not None:
+            again.full = True
+        return out
+
+    def weight_grad(self, dy, kept, out=None, bias_out=None, accumulate=False, stream=None):
+        """dw [outputs, channels] = dy^T x of x as kept (no act is applied), fp32,
+        for a linear layer whose output's gradient is dy (bf16 [tokens, outputs]);
+        ``bias_out`` receives dy's sums over tokens.  ``accumulate``: add to what
+        ``out`` and ``bias_out`` hold."""
+        if _grad_on():
+            _by_hand(("dy", dy))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.weight_grad(dy, kept, out, bias_out, accumulate)
+        dev, s = _here()
+        n, m = dy.shape
+        f32 = torch.float32
+        if out is None:
+            if accumulate:
+                _bad("there is nothing to add to: out is None")
+            out = torch.empty((m, self.channels), dtype=f32, device=dy.device)
+        if out.shape != (m, self.channels):
+            _bad(f"out is {tuple(out.shape)}, expected {(m, self.channels)}")
+        need = self.sizes.get((n, m))
+        if need is None:
+            b = ctypes.c_size_t()
+            _check(lib().pulse_keep_wgrad_sizes(self.desc, n, m, b))
+            need = self.sizes[n, m] = b.value
+        ws = _bytes_at(need, dy.device)
+        _check(lib().pulse_keep_wgrad(
+            self.desc, n, m, _rows(dy, "dy", (n, m), torch.bfloat16, dev),
+            *self._kept(kept, "kept", n, dev, s, True),
+            _flat(out, "out", m * self.channels, f32, dev),
+            _flat(bias_out, "bias_out", m, f32, dev), 1 if accumulate else 0, ws.data_ptr(), need,
+            s))
+        return out
+
+
+class Linear8:
+    """y = act(x W^T + bias) in 8-bit integers, for sampling: W (fp32 or bf16
+    [outputs, inputs]) is laid out once, with a scale for each output channel; a
+    call lays out x (bf16 [tokens, inputs]) with a scale for each token, and
+    integer sums are exact.  ``bias``: fp32 [outputs].  After the weights change,
+    call :meth:`update`."""
+
+    def __init__(self, weight, bias=None, act=None):
+        if weight.dim() != 2:
+            _bad(f"weight is {tuple(weight.shape)}, expected [outputs, inputs]")
+        self.outputs, self.inputs = weight.shape
+        self.desc = Lin8Desc(self.inputs, self.outputs, _choice(act, _ACTS, "act"), BF16)
+        n = ctypes.c_size_t()
+        _check(lib().pulse_lin8_sizes(self.desc, 0, n, None))
+        self.bytes, self.sizes = n.value, {}
+        self.weights = _bytes_at(n.value, weight.device)
+        self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
+        self.update(weight, bias)
+
+    def update(self, weight, bias=None, stream=None):
+        """Lay out other weights of the same shape."""
+        if _grad_on():
+            _by_hand(("weight", weight), ("bias", bias))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.update(weight, bias)
+        dev, s = _here()
+        if tuple(weight.shape) != (self.outputs, self.inputs):
+            _bad(f"weight is {tuple(weight.shape)}, expected {(self.outputs, self.inputs)}")
+        at = _flat(weight, "weight", self.outputs * self.inputs, weight.dtype, dev)
+        self.bias_ptr = _flat(bias, "bias", self.outputs, torch.float32, dev)
+        _check(lib().pulse_lin8_pack(self.desc, at, _dtype(weight.dtype), self._weights(dev, s),
+                                     self.bytes, s))
+        self.bias = bias
+
+    def _weights(self, dev, s):
+        if self.weights.get_device() != dev:
+            _bad(f"the weights are on {self.weights.device}, not on the current GPU")
+        if s != self.home:
+            _used_on(self.weights, dev)
+            if getattr(self, "bias", None) is not None:
+                _used_on(self.bias, dev)
+        return self.ptr
+
+    def forward(self, x, out=None, stream=None):
+        """y (bf16 [tokens, outputs])."""
+        bf = torch.bfloat16
+        if x.requires_grad and _grad_on():
+            _by_hand(("x", x))
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward(x, out)
+        dev, s = _here()
+        n = x.shape[0]
+        if out is None:
+            out = torch.empty((n, self.outputs), dtype=bf, device=x.device)
+        need = self.sizes.get(n)
+        if need is None:
+            b = ctypes.c_size_t()
+            _check(lib().pulse_lin8_sizes(self.desc, n, None, b))
+            need = self.sizes[n] = b.value
+        ws = _bytes_at(need, x.device)
+        _check(lib().pulse_lin8_forward(
+            self.desc, n, _rows(x, "x", (n, self.inputs), bf, dev), self._weights(dev, s),
+            self.bytes, self.bias_ptr, _rows(out, "out", (n, self.outputs), bf, dev),
+            ws.data_ptr(), need, s))
+        return out

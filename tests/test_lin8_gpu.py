@@ -1,0 +1,178 @@
+"""Linear layers in 8-bit integers against the definition: the same rows of
+whole numbers and scales (fp32 quotients and products, as defined), the rest in
+float64.
+
+Tolerance per value: half a step of bf16 (2^-8), and fp32's roundings of the
+sum's conversion, two products and the bias, 4 * 2^-24 of the sizes that are
+added; through an activation (slope at most 1.13) 1.13 times as much, and its own
+error of 3e-7 (1 + |z|)."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2606_19163_amd import ops
+
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _randn(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=F32)
+
+
+def _rows(x):
+    """(whole numbers, scales) of the rows, in fp32 as defined."""
+    x = x.float()
+    top = x.abs().amax(1, keepdim=True)
+    bad = ~torch.isfinite(top)
+    top = torch.where(bad, torch.ones_like(top), top).clamp(min=2.0 ** -100)
+    q = torch.round(x * (torch.tensor(127.0) / top))
+    nan = torch.full_like(top, float("nan"))
+    return torch.where(bad, torch.zeros_like(q), q), torch.where(bad, nan, top / 127.0)
+
+
+def _check(y, x, w, bias, act):
+    (qx, sx), (qw, sw) = _rows(x), _rows(w)
+    z = (qx.double().cuda() @ qw.double().cuda().t().contiguous()).cpu()
+    z = z * sx.double() * sw.double().t()
+    b = torch.zeros(w.shape[0], dtype=torch.float64) if bias is None else bias.double()
+    size = z.abs() + b.abs()
+    z = z + b
+    ref, slack = z, 4 * 2.0 ** -24 * size
+    if act:
+        ref = 0.5 * z * torch.erfc(-z / math.sqrt(2.0)) if act == "gelu" else z * torch.sigmoid(z)
+        slack = 1.13 * slack + 3e-7 * (1 + z.abs())
+    y = y.cpu().double()
+    assert y.shape == ref.shape
+    assert torch.equal(torch.isnan(y), torch.isnan(ref))
+    off = (y - ref).abs().nan_to_num(0.0)
+    bound = (2.0 ** -8 * ref.abs() * 1.0001 + slack).nan_to_num(0.0)
+    assert bool((off <= bound).all()), float((off / bound.clamp(min=1e-30)).max())
+
+
+def _case(tokens, inputs, outputs, bias=True, act=None, wtype=BF, seed=0):
+    x = (_randn(seed + 1, tokens, inputs) * torch.exp(_randn(seed + 2, inputs))).to(BF)
+    w = (_randn(seed + 3, outputs, inputs) * torch.exp(0.5 * _randn(seed + 4, outputs, 1))
+         / math.sqrt(inputs)).to(wtype)
+    b = _randn(seed + 5, outputs) if bias else None
+    layer = ops.Linear8(w.cuda(), bias=None if b is None else b.cuda(), act=act)
+    _check(layer.forward(x.cuda()), x, w, b, act)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 33, 64, 65, 129, 300])
+@pytest.mark.parametrize("inputs,outputs", [(8, 8), (24, 136), (64, 64), (72, 24), (320, 520),
+                                            (1408, 264), (2000, 16)])
+def test_sizes(tokens, inputs, outputs):
+    log(f"case lin8 {tokens}x{inputs}->{outputs}")
+    _case(tokens, inputs, outputs)
+
+
+@pytest.mark.parametrize("tokens,inputs,outputs", [(2048, 200, 4096), (8192, 328, 1544),
+                                                   (2100, 64, 6000), (1100, 768, 2304)])
+@pytest.mark.parametrize("act", [None, "gelu", "silu"])
+def test_many(tokens, inputs, outputs, act):
+    log(f"case lin8 {tokens}x{inputs}->{outputs} {act}")
+    _case(tokens, inputs, outputs, act=act)
+
+
+@pytest.mark.parametrize("tokens", [3, 40, 200])
+@pytest.mark.parametrize("bias,act,wtype", [(False, None, F32), (False, "gelu", BF),
+                                            (True, "silu", F32)])
+def test_kinds(tokens, bias, act, wtype):
+    _case(tokens, 136, 264, bias, act, wtype)
+
+
+@pytest.mark.parametrize("tokens", [1, 16, 70, 600])
+def test_long_sums_are_exact(tokens):
+    """The largest sum there is: 65536 products of 127 * 127 are below 2^31."""
+    x = torch.ones(tokens, 65536, dtype=BF)
+    x[:, ::3] = -1
+    w = x[:1].repeat(8, 1)
+    layer = ops.Linear8(w.cuda())
+    y = layer.forward(x.cuda())
+    # s_x s_w 65536 127^2, where s is 1 / 127 in fp32: within a step of bf16
+    assert bool(((y.double() - 65536).abs() <= 2.0 ** -8 * 65536).all())
+
+
+@pytest.mark.parametrize("tokens", [5, 70, 2048])
+def test_values(tokens):
+    """Rows of zeros, of tiny and huge values, NaN and infinities: each in its
+    own row or column."""
+    outputs = 4096 if tokens > 1000 else 24
+    x, w = _randn(1, tokens, 72).to(BF), _randn(2, outputs, 72).to(BF)
+    x[0] = 0
+    x[1] *= 1e-35
+    x[2, 3] = float("nan")
+    x[3, 5] = -float("inf")
+    x[4] *= 1e30
+    w[0] = 0
+    w[1, 7] = float("inf")
+    w[2] *= 1e-36
+    b = _randn(3, outputs)
+    layer = ops.Linear8(w.cuda(), bias=b.cuda())
+    y = layer.forward(x.cuda())
+    _check(y, x, w, b, None)
+    nan = torch.isnan(y).cpu()
+    assert bool(nan[2].all() and nan[3].all() and nan[:, 1].all())
+    nan[2] = nan[3] = False
+    nan[:, 1] = False
+    assert not bool(nan.any())
+    # one row of a value at the end of the range
+    big = torch.full((1, 72), torch.finfo(BF).max, dtype=BF)
+    one = torch.zeros(8, 72, dtype=BF)
+    one[:, 0] = 0.5
+    _check(ops.Linear8(one.cuda()).forward(big.cuda()), big, one, None, None)
+
+
+def test_rows_do_not_depend_on_the_batch():
+    """A token gives the same bits alone and in any batch."""
+    x, w = _randn(1, 2300, 328).to(BF).cuda(), _randn(2, 4096, 328).to(BF).cuda()
+    layer = ops.Linear8(w, bias=_randn(3, 4096).cuda(), act="gelu")
+    whole = layer.forward(x)
+    for a, b in ((0, 1), (7, 12), (100, 164), (2000, 2300)):
+        assert torch.equal(layer.forward(x[a:b]), whole[a:b])
+
+
+def test_strides_update_and_no_tokens():
+    t, k, n = 50, 136, 72
+    box = torch.full((t, k + n + 16), 5.0, dtype=BF, device="cuda")
+    x, y = box[:, :k], box[:, k + 8:k + 8 + n]
+    x.copy_(_randn(1, t, k))
+    w = _randn(2, n, k).cuda()
+    layer = ops.Linear8(w)
+    layer.forward(x, out=y)
+    assert torch.equal(y, layer.forward(x.contiguous()))
+    assert bool((box[:, k:k + 8] == 5).all()) and bool((box[:, k + 8 + n:] == 5).all())
+    assert layer.forward(x[:0]).shape == (0, n)
+    layer.update(2 * w, bias=torch.ones(n, device="cuda"))
+    _check(layer.forward(x), x.cpu(), 2 * w.cpu(), torch.ones(n), None)
+    far = 1200000000 // 8 * 8  # offsets above 2^31 elements
+    big = torch.empty(2 * far + k, dtype=BF, device="cuda").as_strided((3, k), (far, 1))
+    big.copy_(x[:3])
+    assert torch.equal(layer.forward(big), layer.forward(x[:3].contiguous()))
+
+
+@pytest.mark.parametrize("tokens", [1, 40, 300])
+def test_streams_and_graph(tokens):
+    x = _randn(1, tokens, 320).to(BF).cuda()
+    layer = ops.Linear8(_randn(2, 520, 320).cuda(), act="silu")
+    want = layer.forward(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = layer.forward(x, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = layer.forward(x)
+    for i in range(3):
+        if i:
+            x.mul_(-1.5).add_(0.125)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, layer.forward(x)), i
