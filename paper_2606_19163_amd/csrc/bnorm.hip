@@ -7,64 +7,72 @@
 namespace pulse {
 namespace {
 
-// 1 / standard deviation, and the rows' values turned to n
-template <int L, int NV>
-__device__ __forceinline__ float norm_row(float (&v)[NV][8], int nv, int lr, int kind, float inv_c,
-                                          float eps, float* sm, int& turn) {
+// floats of LDS that the sums over a row take
+template <int L>
+constexpr int ROW_LDS = L > 64 ? L / 16 : 1;
+
+// 1 / standard deviation, and the row's values turned to n.  Lanes past the
+// row (`in` false) hold 0 and stay at 0.
+template <int L>
+__device__ __forceinline__ float norm_row(float (&v)[8], bool in, int kind, float inv_c, float eps,
+                                          float* sm, int& turn) {
   float s = 0.f, q = 0.f;
   if (kind == PULSE_NORM_LAYER) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[j][i];
+    for (int i = 0; i < 8; ++i) s += v[i];
     row_sums<L>(s, q, sm, turn);
-    const float mean = s * inv_c;
-    // lanes past the row hold 0 and stay at 0
+    const float mean = in ? s * inv_c : 0.f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = lr + L * j < nv ? v[j][i] - mean : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] -= mean;
   }
   s = q = 0.f;
   // shares of the mean, which overflow only where it does
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(v[j][i] * inv_c, v[j][i], s);
+  for (int i = 0; i < 8; ++i) s = fmaf(v[i] * inv_c, v[i], s);
   row_sums<L>(s, q, sm, turn);
   const float r = rsqrtf(s + eps);
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] *= r;
+  for (int i = 0; i < 8; ++i) v[i] *= r;
   return r;
 }
 
 // the gradient g of n turned to that of the values: r (g - mean g - n mean(g n))
-template <int L, int NV>
-__device__ __forceinline__ void norm_back(float (&g)[NV][8], const float (&n)[NV][8], float r,
-                                          int kind, float inv_c, float* sm, int& turn) {
+template <int L>
+__device__ __forceinline__ void norm_back(float (&g)[8], const float (&n)[8], float r, int kind,
+                                          float inv_c, float* sm, int& turn) {
   float a = 0.f, b = 0.f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      a += g[j][i];
-      b = fmaf(g[j][i], n[j][i], b);
-    }
+  for (int i = 0; i < 8; ++i) {
+    a += g[i];
+    b = fmaf(g[i], n[i], b);
+  }
   row_sums<L>(a, b, sm, turn);
   a = kind == PULSE_NORM_LAYER ? a * inv_c : 0.f;
   b *= inv_c;
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[j][i] = r * (g[j][i] - a - n[j][i] * b);
+  for (int i = 0; i < 8; ++i) g[i] = r * (g[i] - a - n[i] * b);
 }
 
-// document of row t: docs or -1 for none
+// Document of row t: docs or -1 for none.  A wave whose lanes ask for one row
+// looks at 64 offsets at a time; bisection where they ask for several.
+template <bool WAVE>
 __device__ __forceinline__ int doc_of(const int32_t* off, int docs, int t) {
   if (!off) return 0;
-  int a = 0, b = docs + 1;
+  int a = 0, n = docs + 1;  // the first offset above t is in [a, a + n]
+  if (WAVE) {
+    const int lane = threadIdx.x & 63;
+    while (n > 64) {
+      const int step = (n + 63) >> 6;
+      const int i = a + lane * step;
+      const uint64_t m = __ballot(i < a + n && off[min(i, docs)] <= t);
+      if (!m) return a - 1;
+      const int first = a + (__popcll(m) - 1) * step;
+      n = min(step, a + n - first);
+      a = first;
+    }
+    return a + __popcll(__ballot(lane < n && off[min(a + lane, docs)] <= t)) - 1;
+  }
+  int b = n;
   while (a < b) {
     const int m = (a + b) >> 1;
     if (off[m] <= t)
@@ -75,13 +83,6 @@ __device__ __forceinline__ int doc_of(const int32_t* off, int docs, int t) {
   return a - 1;
 }
 
-template <int L, int NV, class F>
-__device__ __forceinline__ void each(int nv, int lr, F f) {
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-    if (lr + L * j < nv) f(j, 8 * (lr + L * j));
-}
-
 __device__ __forceinline__ void ldf8(float (&v)[8], const float* p) {
   Vec8<float> x;
   x.load(p);
@@ -89,79 +90,88 @@ __device__ __forceinline__ void ldf8(float (&v)[8], const float* p) {
   for (int i = 0; i < 8; ++i) v[i] = x.get(i);
 }
 
-// L lanes per row, NV vectors of 8 channels per lane, `rows` rows in order
-template <typename TS, typename TB, int L, int NV>
-__global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int rows) {
-  __shared__ float sm[16];
-  int turn = 0;
-  const int lr = threadIdx.x % L, nv = a.C >> 3;
-  const long t0 = ((long)blockIdx.x * (256 / L) + threadIdx.x / L) * rows;
-  const float inv_c = 1.f / a.C;
-  float A[NV][8], B[NV][8], G[NV][8];  // of the norm, its shift, of the branch
-  int cur = -2;
-  for (long t = t0; t < t0 + rows && t < a.tokens; ++t) {
-    const TS* px = static_cast<const TS*>(a.x) + t * a.xt;
-    Vec8<TS> x[NV];
-    Vec8<TB> y[NV];
-    each<L, NV>(nv, lr, [&](int j, int c) {
-      x[j].load(px + c);
-      if (a.branch) y[j].load(static_cast<const TB*>(a.y) + t * a.yt + c);
-    });
-    const int d = doc_of(a.off, a.docs, (int)t);
-    const bool inside = d >= 0 && d < a.docs;
-    if (d != cur && inside) {
-      cur = d;
-      each<L, NV>(nv, lr, [&](int j, int c) {
-        float w[8], s[8], b[8], f[8], g[8], p[8];
+// What a document's rows share, for a lane's channels: the norm's factor A and
+// shift B, the branch's factor G.
+struct Cond {
+  float A[8], B[8], G[8];
+  __device__ __forceinline__ void load(const NormArgs& a, int d, int c) {
+    float w[8], s[8], b[8], f[8], g[8], p[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = g[i] = p[i] = 1.f, s[i] = b[i] = f[i] = 0.f;
-        if (a.weight) ldf8(w, a.weight + c);
-        if (a.bias) ldf8(b, a.bias + c);
-        if (a.scale) ldf8(s, a.scale + (long)d * a.scale_t + c);
-        if (a.shift) ldf8(f, a.shift + (long)d * a.shift_t + c);
-        if (a.gate) ldf8(g, a.gate + (long)d * a.gate_t + c);
-        if (a.post_weight) ldf8(p, a.post_weight + c);
+    for (int i = 0; i < 8; ++i) w[i] = g[i] = p[i] = 1.f, s[i] = b[i] = f[i] = 0.f;
+    if (a.weight) ldf8(w, a.weight + c);
+    if (a.bias) ldf8(b, a.bias + c);
+    if (a.scale) ldf8(s, a.scale + (long)d * a.scale_t + c);
+    if (a.shift) ldf8(f, a.shift + (long)d * a.shift_t + c);
+    if (a.gate) ldf8(g, a.gate + (long)d * a.gate_t + c);
+    if (a.post_weight) ldf8(p, a.post_weight + c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          A[j][i] = w[i] * (1.f + s[i]);
-          B[j][i] = fmaf(b[i], 1.f + s[i], f[i]);
-          G[j][i] = a.r * g[i] * p[i];
-        }
-      });
+    for (int i = 0; i < 8; ++i) {
+      A[i] = w[i] * (1.f + s[i]);
+      B[i] = fmaf(b[i], 1.f + s[i], f[i]);
+      G[i] = a.r * g[i] * p[i];
     }
-    float h[NV][8];
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void get8(float (&v)[8], const Vec8<T>& x, bool in) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] = lr + L * j < nv ? x[j].get(i) : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] = in ? x.get(i) : 0.f;
+}
+
+// L lanes per row, 8 channels per lane; `rows` rows in order, the next one on
+// its way while one is worked on
+template <typename TS, typename TB, int L>
+__global__ __launch_bounds__(ROW_THREADS<L>) void k_norm_fwd(NormArgs a, int rows) {
+  __shared__ float sm[ROW_LDS<L>];
+  int turn = 0;
+  const int c = 8 * (threadIdx.x % L);
+  const bool in = c < a.C;
+  const float inv_c = 1.f / a.C;
+  const long t0 = ((long)blockIdx.x * (ROW_THREADS<L> / L) + threadIdx.x / L) * rows;
+  const long t1 = min(t0 + rows, (long)a.tokens);
+  Vec8<TS> x;
+  Vec8<TB> y;
+  x.zero();
+  y.zero();
+  auto fetch = [&](long t) __attribute__((always_inline)) {
+    if (in && t < t1) {
+      x.load(static_cast<const TS*>(a.x) + t * a.xt + c);
+      if (a.branch) y.load(static_cast<const TB*>(a.y) + t * a.yt + c);
+    }
+  };
+  fetch(t0);
+  Cond k;
+  bool inside = false;
+  long stop = t0;  // the first row past this document
+  for (long t = t0; t < t1; ++t) {
+    float h[8], v[8];
+    if (t >= stop) {
+      const int d = doc_of<(L >= 64)>(a.off, a.docs, (int)t);
+      inside = d >= 0 && d < a.docs;
+      stop = a.off && d < a.docs ? a.off[d + 1] : a.tokens;
+      if (inside && in) k.load(a, d, c);
+    }
+    get8(h, x, in);
+    get8(v, y, in);
+    fetch(t + 1);
     if (a.branch) {
       if (inside) {
-        float v[NV][8];
+        if (a.post) norm_row<L>(v, in, a.post, inv_c, a.eps, sm, turn);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[j][i] = lr + L * j < nv ? y[j].get(i) : 0.f;
-        if (a.post) norm_row<L, NV>(v, nv, lr, a.post, inv_c, a.eps, sm, turn);
-        each<L, NV>(nv, lr, [&](int j, int) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            h[j][i] = fmaf(G[j][i], v[j][i], h[j][i]);
-            // the norm is that of the stream as it is stored
-            if (sizeof(TS) == 2) h[j][i] = bf2f(f2bf(h[j][i]));
-          }
-        });
+        for (int i = 0; i < 8; ++i) {
+          h[i] = in ? fmaf(k.G[i], v[i], h[i]) : 0.f;
+          // the norm is that of the stream as it is stored
+          if (sizeof(TS) == 2) h[i] = bf2f(f2bf(h[i]));
+        }
       }
-      TS* ph = static_cast<TS*>(a.h) + t * a.ht;
-      each<L, NV>(nv, lr, [&](int j, int c) { put8(ph + c, h[j]); });
+      if (in) put8(static_cast<TS*>(a.h) + t * a.ht + c, h);
     }
     if (a.pre) {
-      TB* pu = static_cast<TB*>(a.u) + t * a.ut;
-      if (inside) norm_row<L, NV>(h, nv, lr, a.pre, inv_c, a.eps, sm, turn);
-      each<L, NV>(nv, lr, [&](int j, int c) {
+      if (inside) norm_row<L>(h, in, a.pre, inv_c, a.eps, sm, turn);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[j][i] = inside ? fmaf(h[j][i], A[j][i], B[j][i]) : 0.f;
-        put8(pu + c, h[j]);
-      });
+      for (int i = 0; i < 8; ++i) h[i] = inside ? fmaf(h[i], k.A[i], k.B[i]) : 0.f;
+      if (in) put8(static_cast<TB*>(a.u) + t * a.ut + c, h);
     }
   }
 }
@@ -170,133 +180,95 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int rows) {
 // the sums over its rows of document d, of du, du n and dH ny, in slot b + d:
 // from one pair (b, d) with rows to the next one of the two grows and neither
 // sinks, so that no two pairs share a slot.
-template <typename TS, typename TB, int L, int NV>
-__global__ __launch_bounds__(256, 2) void k_norm_bwd(NormArgs a, int R, float* part) {
-  extern __shared__ float comb[];  // [256 / L][C]
-  __shared__ float sm[16];
+template <typename TS, typename TB, int L>
+__global__ __launch_bounds__(ROW_THREADS<L>) void k_norm_bwd(NormArgs a, int R, float* part) {
+  constexpr int GR = ROW_THREADS<L> / L;
+  __shared__ float sm[ROW_LDS<L>];
+  __shared__ __attribute__((aligned(16))) float comb[GR > 1 ? GR * 8 * L : 4];
   int turn = 0;
-  constexpr int GR = 256 / L;
-  const int lr = threadIdx.x % L, gr = threadIdx.x / L, nv = a.C >> 3;
+  const int gr = threadIdx.x / L, c = 8 * (threadIdx.x % L);
+  const bool in = c < a.C;
   const float inv_c = 1.f / a.C;
   const long end = min((long)(blockIdx.x + 1) * R, (long)a.tokens);
   for (long seg = (long)blockIdx.x * R; seg < end;) {
-    const int d = doc_of(a.off, a.docs, (int)seg);
+    const int d = doc_of<true>(a.off, a.docs, (int)seg);
     const bool inside = d >= 0 && d < a.docs;
     long stop = end;
     if (a.off && d < a.docs) stop = max(seg + 1, min(end, (long)a.off[d + 1]));
-    float A[NV][8], G[NV][8];
-    float P1[NV][8], P2[NV][8], P3[NV][8];
+    Vec8<TS> dh, h;
+    Vec8<TB> du, y;
+    dh.zero(), h.zero(), du.zero(), y.zero();
+    auto fetch = [&](long t) __attribute__((always_inline)) {
+      if (!in || t >= stop) return;
+      if (a.dh) dh.load(static_cast<const TS*>(a.dh) + t * a.dht + c);
+      if (inside && a.pre) {
+        h.load(static_cast<const TS*>(a.h) + t * a.ht + c);
+        du.load(static_cast<const TB*>(a.du) + t * a.dut + c);
+      }
+      if (inside && a.branch) y.load(static_cast<const TB*>(a.y) + t * a.yt + c);
+    };
+    fetch(seg + gr);
+    Cond k;
+    if (inside && in) k.load(a, d, c);
+    float P1[8], P2[8], P3[8];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int i = 0; i < 8; ++i) P1[i] = P2[i] = P3[i] = 0.f;
+    for (long t = seg + gr; t < stop; t += GR) {
+      float g[8], n[8], u[8], ny[8], e[8];
+      get8(e, dh, in);
+      get8(n, h, in);
+      get8(u, du, in);
+      get8(ny, y, in);
+      fetch(t + GR);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) P1[j][i] = P2[j][i] = P3[j][i] = 0.f;
-    if (inside)
-      each<L, NV>(nv, lr, [&](int j, int c) {
-        float w[8], s[8], g[8], p[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = g[i] = p[i] = 1.f, s[i] = 0.f;
-        if (a.weight) ldf8(w, a.weight + c);
-        if (a.scale) ldf8(s, a.scale + (long)d * a.scale_t + c);
-        if (a.gate) ldf8(g, a.gate + (long)d * a.gate_t + c);
-        if (a.post_weight) ldf8(p, a.post_weight + c);
+      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+      if (inside && a.pre) {
+        const float r = norm_row<L>(n, in, a.pre, inv_c, a.eps, sm, turn);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          A[j][i] = w[i] * (1.f + s[i]);
-          G[j][i] = a.r * g[i] * p[i];
+          P1[i] += u[i];
+          P2[i] = fmaf(u[i], n[i], P2[i]);
+          g[i] = in ? u[i] * k.A[i] : 0.f;
         }
-      });
-    for (long t = seg + gr; t < stop; t += GR) {
-      Vec8<TS> dh[NV], h[NV];
-      Vec8<TB> du[NV], y[NV];
-      each<L, NV>(nv, lr, [&](int j, int c) {
-        if (a.dh) dh[j].load(static_cast<const TS*>(a.dh) + t * a.dht + c);
-        else dh[j].zero();
-        if (inside && a.pre) {
-          h[j].load(static_cast<const TS*>(a.h) + t * a.ht + c);
-          du[j].load(static_cast<const TB*>(a.du) + t * a.dut + c);
-        }
-        if (inside && a.branch) y[j].load(static_cast<const TB*>(a.y) + t * a.yt + c);
-      });
-      float g[NV][8], n[NV][8];
-      if (inside && a.pre) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const bool in = lr + L * j < nv;
-            n[j][i] = in ? h[j].get(i) : 0.f;
-          }
-        const float r = norm_row<L, NV>(n, nv, lr, a.pre, inv_c, a.eps, sm, turn);
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const bool in = lr + L * j < nv;
-            const float u = in ? du[j].get(i) : 0.f;
-            P1[j][i] += u;
-            P2[j][i] = fmaf(u, n[j][i], P2[j][i]);
-            g[j][i] = in ? u * A[j][i] : 0.f;
-          }
-        norm_back<L, NV>(g, n, r, a.pre, inv_c, sm, turn);
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) g[j][i] = lr + L * j < nv ? g[j][i] + dh[j].get(i) : 0.f;
-      } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) g[j][i] = lr + L * j < nv ? dh[j].get(i) : 0.f;
+        norm_back<L>(g, n, r, a.pre, inv_c, sm, turn);
       }
-      if (a.dx) {
-        TS* pd = static_cast<TS*>(a.dx) + t * a.dxt;
-        each<L, NV>(nv, lr, [&](int j, int c) { put8(pd + c, g[j]); });
-      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = in ? g[i] + e[i] : 0.f;
+      if (a.dx && in) put8(static_cast<TS*>(a.dx) + t * a.dxt + c, g);
       if (a.branch) {
         if (inside) {
           float r = 0.f;
+          if (a.post) r = norm_row<L>(ny, in, a.post, inv_c, a.eps, sm, turn);
 #pragma unroll
-          for (int j = 0; j < NV; ++j)
+          for (int i = 0; i < 8; ++i) {
+            P3[i] = fmaf(g[i], ny[i], P3[i]);
+            g[i] = in ? g[i] * k.G[i] : 0.f;
+          }
+          if (a.post) norm_back<L>(g, ny, r, a.post, inv_c, sm, turn);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) n[j][i] = lr + L * j < nv ? y[j].get(i) : 0.f;
-          if (a.post) r = norm_row<L, NV>(n, nv, lr, a.post, inv_c, a.eps, sm, turn);
-#pragma unroll
-          for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              P3[j][i] = fmaf(g[j][i], n[j][i], P3[j][i]);
-              g[j][i] = lr + L * j < nv ? g[j][i] * G[j][i] : 0.f;
-            }
-          if (a.post) norm_back<L, NV>(g, n, r, a.post, inv_c, sm, turn);
+          for (int i = 0; i < 8; ++i) g[i] = 0.f;
         }
-        TB* pd = static_cast<TB*>(a.dy) + t * a.dyt;
-        each<L, NV>(nv, lr, [&](int j, int c) {
-          if (!inside)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g[j][i] = 0.f;
-          put8(pd + c, g[j]);
-        });
+        if (in) put8(static_cast<TB*>(a.dy) + t * a.dyt + c, g);
       }
     }
     if (inside && part) {
-      float* dst = part + ((long)blockIdx.x + d) * 3 * a.C;
-      auto join = [&](float (&P)[NV][8], int k) __attribute__((always_inline)) {
-        if constexpr (GR == 1) {
-          each<L, NV>(nv, lr, [&](int j, int c) { put8(dst + (long)k * a.C + c, P[j]); });
-        } else {
+      float* dst = part + ((long)blockIdx.x + d) * 3 * a.C + c;
+      auto join = [&](float (&P)[8], int w) __attribute__((always_inline)) {
+        if constexpr (GR > 1) {
           __syncthreads();  // the last sums were read
-          each<L, NV>(nv, lr, [&](int j, int c) { put8(comb + gr * a.C + c, P[j]); });
+          put8(comb + gr * 8 * L + c, P);
           __syncthreads();
-          for (int c = 4 * threadIdx.x; c < a.C; c += 1024) {
-            float4 s = *reinterpret_cast<const float4*>(comb + c);
+          if (gr == 0)
 #pragma unroll
-            for (int w = 1; w < GR; ++w) {
-              const float4 v = *reinterpret_cast<const float4*>(comb + w * a.C + c);
-              s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            for (int i = 1; i < GR; ++i) {
+              float v[8];
+              ldf8(v, comb + i * 8 * L + c);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) P[j] += v[j];
             }
-            *reinterpret_cast<float4*>(dst + (long)k * a.C + c) = s;
-          }
         }
+        if (gr == 0 && in) put8(dst + (long)w * a.C, P);
       };
       if (a.pre) {
         join(P1, 0);
@@ -308,118 +280,124 @@ __global__ __launch_bounds__(256, 2) void k_norm_bwd(NormArgs a, int R, float* p
   }
 }
 
-// Sums over a document's slots: 64 channels x 4 lanes of slots, which meet in
-// a fixed order.  `docsum` [docs][3][C] receives what the weights' gradients
-// sum over documents.
-__global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads o, int R, int nb,
+// A block of the sums over slots and documents: 64 channels, four each of 16
+// lanes, times 16 lanes of what is summed, which meet in a fixed order.
+constexpr int SUM_C = 64, SUM_K = 16;
+using Sums = float[3][SUM_K][SUM_C];
+
+__device__ __forceinline__ void add4(float4& s, const float* p) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+}
+
+// thread t < 192: the total of sum t / 64, channel t % 64
+__device__ __forceinline__ float meet(Sums& sm, const float4 (&p)[3]) {
+  const int k = threadIdx.x >> 4, c = 4 * (threadIdx.x & 15);
+  __syncthreads();  // the last totals were read
+#pragma unroll
+  for (int i = 0; i < 3; ++i) *reinterpret_cast<float4*>(&sm[i][k][c]) = p[i];
+  __syncthreads();
+  float s = 0.f;
+  if (threadIdx.x < 3 * SUM_C)
+#pragma unroll
+    for (int j = 0; j < SUM_K; ++j) s += sm[threadIdx.x >> 6][j][threadIdx.x & 63];
+  return s;
+}
+
+// Sums over a document's slots.  `docsum` [docs][3][C] receives what the
+// weights' gradients sum over documents.
+__global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads o, int R,
                                                    const float* part, float* docsum) {
-  __shared__ float sm[3][4][64];
-  const int lane = threadIdx.x & 63, k = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane;
+  __shared__ __attribute__((aligned(16))) Sums sm;
+  __shared__ float tot[3][SUM_C];
+  const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
   for (int d = blockIdx.y; d < a.docs; d += gridDim.y) {
     const int r0 = a.off ? max(a.off[d], 0) : 0;
     const int r1 = a.off ? min(a.off[d + 1], a.tokens) : a.tokens;
-    float p[3] = {0.f, 0.f, 0.f};
-    if (r1 > r0 && c < a.C)
-      for (int b = r0 / R + k; b <= (r1 - 1) / R; b += 4) {
-        const float* src = part + ((long)b + d) * 3 * a.C + c;
+    float4 p[3];
+    p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r1 > r0 && c4 < a.C) {
+      const int last = (r1 - 1) / R;
+#pragma unroll 4
+      for (int b = r0 / R + k; b <= last; b += SUM_K) {
+        const float* src = part + ((long)b + d) * 3 * a.C + c4;
         if (a.pre) {
-          p[0] += src[0];
-          p[1] += src[a.C];
+          add4(p[0], src);
+          add4(p[1], src + a.C);
         }
-        if (a.branch) p[2] += src[2 * a.C];
+        if (a.branch) add4(p[2], src + 2 * a.C);
       }
-#pragma unroll
-    for (int i = 0; i < 3; ++i) sm[i][k][lane] = p[i];
+    }
+    const float total = meet(sm, p);
+    if (threadIdx.x < 3 * SUM_C) tot[threadIdx.x >> 6][threadIdx.x & 63] = total;
     __syncthreads();
-    if (k == 0 && c < a.C) {
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-        p[i] = (sm[i][0][lane] + sm[i][1][lane]) + (sm[i][2][lane] + sm[i][3][lane]);
+    const int c = blockIdx.x * SUM_C + threadIdx.x;
+    if (threadIdx.x < SUM_C && c < a.C) {
+      const float p0 = tot[0][threadIdx.x], p1 = tot[1][threadIdx.x], p2 = tot[2][threadIdx.x];
       const float w = a.weight ? a.weight[c] : 1.f, b = a.bias ? a.bias[c] : 0.f;
       const float s = 1.f + (a.scale ? a.scale[(long)d * a.scale_t + c] : 0.f);
       const float g = a.r * (a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
       const float wp = a.post_weight ? a.post_weight[c] : 1.f;
       const long at = (long)d * a.C + c;
-      if (o.dshift) o.dshift[at] = p[0];
-      if (o.dscale) o.dscale[at] = w * p[1] + b * p[0];
-      if (o.dgate) o.dgate[at] = a.r * wp * p[2];
+      if (o.dshift) o.dshift[at] = p0;
+      if (o.dscale) o.dscale[at] = w * p1 + b * p0;
+      if (o.dgate) o.dgate[at] = a.r * wp * p2;
       if (docsum) {
-        docsum[(long)d * 3 * a.C + c] = s * p[1];
-        docsum[(long)d * 3 * a.C + a.C + c] = s * p[0];
-        docsum[(long)d * 3 * a.C + 2 * a.C + c] = g * p[2];
+        docsum[(long)d * 3 * a.C + c] = s * p1;
+        docsum[(long)d * 3 * a.C + a.C + c] = s * p0;
+        docsum[(long)d * 3 * a.C + 2 * a.C + c] = g * p2;
       }
     }
-    __syncthreads();
   }
 }
 
-__global__ __launch_bounds__(1024) void k_norm_weights(NormArgs a, pulse_norm_grads o,
-                                                       const float* docsum) {
-  __shared__ float sm[3][16][64];
-  const int lane = threadIdx.x & 63, k = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane;
-  float p[3] = {0.f, 0.f, 0.f};
-  if (c < a.C)
-    for (int d = k; d < a.docs; d += 16) {
-      const float* src = docsum + (long)d * 3 * a.C + c;
+__global__ __launch_bounds__(256) void k_norm_weights(NormArgs a, pulse_norm_grads o,
+                                                      const float* docsum) {
+  __shared__ __attribute__((aligned(16))) Sums sm;
+  const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
+  float4 p[3];
+  p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c4 < a.C)
+#pragma unroll 4
+    for (int d = k; d < a.docs; d += SUM_K) {
+      const float* src = docsum + (long)d * 3 * a.C + c4;
 #pragma unroll
-      for (int i = 0; i < 3; ++i) p[i] += src[(long)i * a.C];
+      for (int i = 0; i < 3; ++i) add4(p[i], src + (long)i * a.C);
     }
-#pragma unroll
-  for (int i = 0; i < 3; ++i) sm[i][k][lane] = p[i];
-  __syncthreads();
-  if (k < 3 && c < a.C) {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += sm[k][i][lane];
-    float* dst = k == 0 ? o.dweight : k == 1 ? o.dbias : o.dpost_weight;
-    if (dst) dst[c] = s;
-  }
+  const float total = meet(sm, p);
+  const int i = threadIdx.x >> 6, c = blockIdx.x * SUM_C + (threadIdx.x & 63);
+  float* dst = i == 0 ? o.dweight : i == 1 ? o.dbias : i == 2 ? o.dpost_weight : nullptr;
+  if (dst && c < a.C) dst[c] = total;
 }
 
-// Rows per block of the backward pass: whole rounds of two blocks per CU,
-// and at least one row per group of lanes.
-int back_rows(int tokens, int groups) {
-  int r = (tokens + 511) / 512;
-  r = (r + groups - 1) / groups * groups;
-  return r < groups ? groups : r;
-}
-
-int groups_of(int C) { return C <= 256 ? 16 : C <= 2048 ? 4 : 1; }
-
-template <typename TS, typename TB, int L, int NV>
+template <typename TS, typename TB, int L>
 hipError_t fwd(const NormArgs& a, hipStream_t st) {
-  const int rows = 1;
-  const int per = 256 / L * rows;
-  hipLaunchKernelGGL((k_norm_fwd<TS, TB, L, NV>), dim3((a.tokens + per - 1) / per), dim3(256), 0,
-                     st, a, rows);
+  // rows in order share the loads of their document's vectors; a block per
+  // row while there are few
+  const int rows = a.tokens >= 8192 ? 4 : a.tokens >= 4096 ? 2 : 1;
+  const int per = ROW_THREADS<L> / L * rows;
+  hipLaunchKernelGGL((k_norm_fwd<TS, TB, L>), dim3((a.tokens + per - 1) / per),
+                     dim3(ROW_THREADS<L>), 0, st, a, rows);
   return hipGetLastError();
 }
 
-template <typename TS, typename TB, int L, int NV>
+template <typename TS, typename TB, int L>
 hipError_t bwd(const NormArgs& a, int R, int nb, float* part, hipStream_t st) {
-  constexpr int GR = 256 / L;
-  const size_t shared = GR > 1 ? (size_t)GR * a.C * 4 : 0;
-  hipLaunchKernelGGL((k_norm_bwd<TS, TB, L, NV>), dim3(nb), dim3(256), shared, st, a, R, part);
+  hipLaunchKernelGGL((k_norm_bwd<TS, TB, L>), dim3(nb), dim3(ROW_THREADS<L>), 0, st, a, R, part);
   return hipGetLastError();
 }
 
-// f(L, NV) for a row of C channels
+// Lanes of a row: f(L).
 template <class F>
-hipError_t by_size(int C, F f) {
-  const int v = C / 8;
+auto by_size(int C, F f) {
   using std::integral_constant;
-#define PULSE_ROW(L, NV) f(integral_constant<int, L>(), integral_constant<int, NV>())
-  if (v <= 16) return PULSE_ROW(16, 1);
-  if (v <= 32) return PULSE_ROW(16, 2);
-  if (v <= 64) return PULSE_ROW(64, 1);
-  if (v <= 128) return PULSE_ROW(64, 2);
-  if (v <= 192) return PULSE_ROW(64, 3);
-  if (v <= 256) return PULSE_ROW(64, 4);
-  if (v <= 512) return PULSE_ROW(256, 2);
-  return PULSE_ROW(256, 4);
-#undef PULSE_ROW
+  if (C <= 128) return f(integral_constant<int, 16>());
+  if (C <= 512) return f(integral_constant<int, 64>());
+  if (C <= 1024) return f(integral_constant<int, 128>());
+  if (C <= 1536) return f(integral_constant<int, 192>());
+  if (C <= 2048) return f(integral_constant<int, 256>());
+  if (C <= 4096) return f(integral_constant<int, 512>());
+  return f(integral_constant<int, 1024>());
 }
 
 template <class F>
@@ -429,6 +407,8 @@ hipError_t by_type(const NormArgs& a, F f) {
   return f(uint16_t(), uint16_t());
 }
 
+constexpr int BACK_BLOCKS = 768;
+
 struct BackPlan {
   int R, nb;
   size_t slots;  // floats of the slots, then of the documents' sums
@@ -436,7 +416,14 @@ struct BackPlan {
 };
 BackPlan back_plan(int C, int docs, int tokens) {
   BackPlan p;
-  p.R = back_rows(tokens, groups_of(C));
+  const int groups = by_size(C, [](auto l) {
+    constexpr int L = decltype(l)::value;
+    return ROW_THREADS<L> / L;
+  });
+  // rows per block: the blocks fill the GPU, and every group of lanes has one
+  p.R = (tokens + BACK_BLOCKS - 1) / BACK_BLOCKS;
+  p.R = (p.R + groups - 1) / groups * groups;
+  if (p.R < groups) p.R = groups;
   p.nb = (tokens + p.R - 1) / p.R;
   p.slots = ((size_t)p.nb + docs) * 3 * C;
   p.floats = p.slots + (size_t)docs * 3 * C;
@@ -452,8 +439,8 @@ size_t norm_bwd_bytes(const pulse_norm_desc& d, int tokens) {
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
   return by_type(a, [&](auto ts, auto tb) {
-    return by_size(a.C, [&](auto l, auto nv) {
-      return fwd<decltype(ts), decltype(tb), decltype(l)::value, decltype(nv)::value>(a, st);
+    return by_size(a.C, [&](auto l) {
+      return fwd<decltype(ts), decltype(tb), decltype(l)::value>(a, st);
     });
   });
 }
@@ -466,9 +453,8 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
   float* part = conds || weights ? ws : nullptr;
   if (a.tokens) {
     const hipError_t e = by_type(a, [&](auto ts, auto tb) {
-      return by_size(a.C, [&](auto l, auto nv) {
-        return bwd<decltype(ts), decltype(tb), decltype(l)::value, decltype(nv)::value>(
-            a, p.R, p.nb, part, st);
+      return by_size(a.C, [&](auto l) {
+        return bwd<decltype(ts), decltype(tb), decltype(l)::value>(a, p.R, p.nb, part, st);
       });
     });
     if (e != hipSuccess) return e;
@@ -476,10 +462,10 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
   if (!part) return hipSuccess;
   float* docsum = weights ? ws + p.slots : nullptr;
   hipLaunchKernelGGL(k_norm_docs, dim3((a.C + 63) / 64, a.docs < 32768 ? a.docs : 32768),
-                     dim3(256), 0, st, a, o, p.R, p.nb, part, docsum);
+                     dim3(256), 0, st, a, o, p.R, part, docsum);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !weights) return e;
-  hipLaunchKernelGGL(k_norm_weights, dim3((a.C + 63) / 64), dim3(1024), 0, st, a, o, docsum);
+  hipLaunchKernelGGL(k_norm_weights, dim3((a.C + 63) / 64), dim3(256), 0, st, a, o, docsum);
   return hipGetLastError();
 }
 

@@ -81,22 +81,30 @@ __device__ __forceinline__ float lanes_op(float v, Op op) {
   return v;
 }
 
-// sums of a and b over the L lanes of a row; L = 256 takes the whole block and
-// 8 floats of LDS, which alternate between two such sets
+// Threads of a block whose rows take L lanes each: rows of up to a wave share
+// a block of four waves, longer ones have a block of their own.
+template <int L>
+constexpr int ROW_THREADS = L > 64 ? L : 256;
+
+// sums of a and b over the L lanes of a row.  L > 64 takes the whole block and
+// L / 32 floats of LDS, which alternate between two such sets.
 template <int L>
 __device__ __forceinline__ void row_sums(float& a, float& b, float* sm, int& turn) {
-  a = lanes_op<L>(a, Add());
-  b = lanes_op<L>(b, Add());
-  if constexpr (L == 256) {
-    float* s = sm + 8 * turn;
+  a = lanes_op<(L > 64 ? 64 : L)>(a, Add());
+  b = lanes_op<(L > 64 ? 64 : L)>(b, Add());
+  if constexpr (L > 64) {
+    constexpr int W = L / 64;
+    float2* s = reinterpret_cast<float2*>(sm) + W * turn;
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
-      s[threadIdx.x >> 6] = a;
-      s[4 + (threadIdx.x >> 6)] = b;
-    }
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = make_float2(a, b);
     __syncthreads();
-    a = (s[0] + s[1]) + (s[2] + s[3]);
-    b = (s[4] + s[5]) + (s[6] + s[7]);
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float2 v = s[w];
+      a += v.x;
+      b += v.y;
+    }
   }
 }
 
