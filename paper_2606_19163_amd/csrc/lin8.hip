@@ -81,25 +81,30 @@ __global__ __launch_bounds__(256) void k_rows8(int rows, int K, const T* x, long
   }
 }
 
-template <int ACT>
-__device__ __forceinline__ void put_y(const Lin8Args& a, long t, int n, i32x4_t acc, Scale sx,
-                                      const Scale* sw) {
-  const int4* pw = reinterpret_cast<const int4*>(sw + n);
-  const int4 w0 = pw[0], w1 = pw[1];
-  float v[4] = {
-      ldexpf((float)acc[0] * sx.m * __int_as_float(w0.x), sx.e + w0.y),
-      ldexpf((float)acc[1] * sx.m * __int_as_float(w0.z), sx.e + w0.w),
-      ldexpf((float)acc[2] * sx.m * __int_as_float(w1.x), sx.e + w1.y),
-      ldexpf((float)acc[3] * sx.m * __int_as_float(w1.z), sx.e + w1.w),
-  };
-  if (a.bias) {
-    const float4 b = *reinterpret_cast<const float4*>(a.bias + n);
-    v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
+// What four outputs share: their scales and biases.
+struct Outs {
+  float m[4], b[4];
+  int e[4];
+  __device__ __forceinline__ void load(const Lin8Args& a, const Scale* sw, int n) {
+    const int4* pw = reinterpret_cast<const int4*>(sw + n);
+    const int4 w0 = pw[0], w1 = pw[1];
+    m[0] = __int_as_float(w0.x), m[1] = __int_as_float(w0.z);
+    m[2] = __int_as_float(w1.x), m[3] = __int_as_float(w1.z);
+    e[0] = w0.y, e[1] = w0.w, e[2] = w1.y, e[3] = w1.w;
+    const float4 v = a.bias ? *reinterpret_cast<const float4*>(a.bias + n)
+                            : make_float4(0.f, 0.f, 0.f, 0.f);
+    b[0] = v.x, b[1] = v.y, b[2] = v.z, b[3] = v.w;
   }
+};
+
+// four outputs of a row
+template <int ACT>
+__device__ __forceinline__ uint2 out4(i32x4_t acc, Scale sx, const Outs& o) {
+  float v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = act_f<ACT>(v[i]);
-  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.yt + n) =
-      uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+  for (int i = 0; i < 4; ++i)
+    v[i] = act_f<ACT>(ldexpf((float)acc[i] * sx.m * o.m[i], sx.e + o.e[i]) + o.b[i]);
+  return uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
 // Few rows: a block of 4 waves takes 16 outputs and TT x 16 rows, its waves a
@@ -132,7 +137,12 @@ __global__ __launch_bounds__(256) void k_lin8_few(Lin8Args a, Laid x, Laid w) {
     const i32x4_t s = part[0][i][lane] + part[1][i][lane] + part[2][i][lane] + part[3][i][lane];
     const long t = (tt + i) * 16 + (lane & 15);
     const int n = tn * 16 + 4 * (lane >> 4);
-    if (t < a.tokens && n < a.N) put_y<ACT>(a, t, n, s, x.scale[t], w.scale);
+    if (t < a.tokens && n < a.N) {
+      Outs o;
+      o.load(a, w.scale, n);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.yt + n) =
+          out4<ACT>(s, x.scale[t], o);
+    }
   }
 }
 
@@ -145,7 +155,11 @@ struct Tile {
   static constexpr int FT = BT / 16, FN = BN / 16, STAGE = (FT + FN) * FRAG;
   static constexpr int NU = (FT + FN) / NW;  // fragments per wave and step
   static constexpr int LDS = STAGES * STAGE;
+  // outputs on their way out: WT rows of each wave, which start 16 bytes apart
+  // modulo the banks
+  static constexpr int PY = WN * 2 + 16, OUT = WT * PY, CPR = WN / 8;
   static_assert(NU * NW == FT + FN && FT % NW == 0, "loads");
+  static_assert(NW * OUT <= LDS, "outputs");
   static_assert(LDS <= 160 * 1024 && (STAGES - 2) * NU < 64, "LDS, vmcnt");
 };
 
@@ -181,7 +195,7 @@ __device__ __forceinline__ int xcd_order(int b, int n) {
 }
 
 template <class C, int ACT>
-__global__ __launch_bounds__(C::NT) void k_lin8(Lin8Args a, Laid x, Laid w, int tilesN) {
+__global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, int tilesN) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -243,17 +257,34 @@ __global__ __launch_bounds__(C::NT) void k_lin8(Lin8Args a, Laid x, Laid w, int 
     __builtin_amdgcn_sched_barrier(0);
     stage = stage + 1 == C::STAGES ? 0 : stage + 1;
   }
-  // lane: outputs 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16
+  // lane: outputs 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16.  They
+  // go through LDS, so that whole rows of a wave's outputs leave together: 8
+  // bytes a lane straight to memory took 90 us more at 8192 x 1408 x 5632.
+  __syncthreads();  // all waves are done with the stages
+  char* out = smem + wave * C::OUT;
+  const long t0 = (long)tt * C::BT + wt * C::WT;
+  const int n0 = tn * C::BN + wn * C::WN;
+  Scale sx[C::TT];
 #pragma unroll
-  for (int i = 0; i < C::TT; ++i) {
-    const long t = (long)tt * C::BT + wt * C::WT + i * 16 + (lane & 15);
-    if (t >= a.tokens) continue;
-    const Scale sx = x.scale[t];
+  for (int i = 0; i < C::TT; ++i) sx[i] = x.scale[t0 + i * 16 + (lane & 15)];
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) {
-      const int n = tn * C::BN + wn * C::WN + j * 16 + 4 * (lane >> 4);
-      if (n < a.N) put_y<ACT>(a, t, n, acc[j][i], sx, w.scale);
-    }
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = j * 16 + 4 * (lane >> 4);
+    if (n0 + n >= a.N) continue;
+    Outs o;
+    o.load(a, w.scale, n0 + n);
+#pragma unroll
+    for (int i = 0; i < C::TT; ++i)
+      *reinterpret_cast<uint2*>(out + (i * 16 + (lane & 15)) * C::PY + n * 2) =
+          out4<ACT>(acc[j][i], sx[i], o);
+  }
+  lgkm_wait0();
+#pragma unroll 4
+  for (int e = lane; e < C::WT * C::CPR; e += 64) {
+    const int r = e / C::CPR, c = e % C::CPR;
+    if (t0 + r < a.tokens && n0 + 8 * c < a.N)
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + (t0 + r) * a.yt + n0 + 8 * c) =
+          *reinterpret_cast<const uint4*>(out + r * C::PY + 16 * c);
   }
 #endif
 }
