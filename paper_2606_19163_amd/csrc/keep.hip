@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void k_keep_save(KeepArgs a, int rows, uint32_
     if (in) x.load(static_cast<const T*>(a.x) + t * a.xt + 8 * k);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = x.get(i);
-    keep8(v, q + (t * V + k) * 8, e + t * (V >> 2) + (k >> 2), (k & 3) == 0);
+    keep8(v, q + (t * V + k) * 8, e + t * keep_exp_pitch(a.C) + (k >> 2), (k & 3) == 0);
     if (PUT && in) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = act_f<ACT>(v[i]);
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void k_keep_load(KeepArgs a, int rows, uint32_
   walk(a.tokens, rows, V, M, [&](long t, int k) {
     if (8 * k >= a.C) return;
     float v[8];
-    load8(v, q + (t * V + k) * 8, e[t * (V >> 2) + (k >> 2)]);
+    load8(v, q + (t * V + k) * 8, e[t * keep_exp_pitch(a.C) + (k >> 2)]);
     put8(static_cast<T*>(a.y) + t * a.yt + 8 * k, v);
   });
 }
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void k_keep_back(KeepArgs a, int rows, uint32_
   walk(a.tokens, rows, V, M, [&](long t, int k) {
     const bool in = 8 * k < a.C;
     float z[8], v[8];
-    load8(z, q + (t * V + k) * 8, e[t * (V >> 2) + (k >> 2)]);
+    load8(z, q + (t * V + k) * 8, e[t * keep_exp_pitch(a.C) + (k >> 2)]);
     if (in) {
       Vec8<T> g;
       g.load(static_cast<const T*>(a.x) + t * a.xt + 8 * k);
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void k_keep_back(KeepArgs a, int rows, uint32_
     if (PUT) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[i] = in ? act_f<ACT>(z[i]) : 0.f;
-      keep8(z, q2 + (t * V + k) * 8, e2 + t * (V >> 2) + (k >> 2), (k & 3) == 0);
+      keep8(z, q2 + (t * V + k) * 8, e2 + t * keep_exp_pitch(a.C) + (k >> 2), (k & 3) == 0);
     }
   });
 }

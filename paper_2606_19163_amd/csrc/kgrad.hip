@@ -12,8 +12,11 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
-// what lanes past the last token or output fetch
-__device__ __attribute__((aligned(16))) const uint32_t kgrad_zero[4] = {0, 0, 0, 0};
+// What lanes past the last token, output or channel fetch: zeros of dy, and of x
+// with their exponent.
+__device__ __attribute__((aligned(16))) const uint32_t kgrad_zero[12] = {
+    0,           0,           0,           0, 0x80808080u, 0x80808080u,
+    0x80808080u, 0x80808080u, 0,           0, 0,           0};
 
 constexpr int BK = 64;  // tokens per step
 
@@ -76,7 +79,8 @@ struct Tile {
   static constexpr int Y_BYTES = BK * PY, X_BYTES = BK * PX, STAGE = Y_BYTES + X_BYTES;
   static constexpr int YU = Y_BYTES / (NT * 16);  // 16-byte loads per thread and step
   static constexpr int XU = BK * BC / (NT * 16);
-  static constexpr int LDS = 2 * STAGE;
+  static constexpr int STAGES = 3, LDS = STAGES * STAGE;
+  static constexpr int LOADS = YU + 2 * XU;  // per thread and step
   static_assert(YU * NT * 16 == Y_BYTES && XU * NT * 16 == BK * BC && XU >= 1, "loads");
   static_assert(36 * PY < 65536 && Y_BYTES + 36 * PX < 65536 && LDS <= 160 * 1024, "LDS");
   static_assert(4 * 3 * (BN / 16 + 4) < 4096, "rotations stay below 4 rows of chunks");
@@ -94,14 +98,39 @@ __device__ __forceinline__ v4s ds_rdtr(uint32_t addr) {
   asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
   return v;
 }
+// ds_write_b128 at addr + OFF, inline for the same reason
+template <int OFF>
+__device__ __forceinline__ void ds_wr128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c,
+                                         uint32_t d) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 v = {a, b, c, d};
+  asm volatile("ds_write_b128 %0, %1 offset:%2" ::"v"(addr), "v"(v), "i"(OFF));
+}
 __device__ __forceinline__ void lgkm_wait0() {
   __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
 }
-__device__ __forceinline__ void vm_wait0() {
-  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 // the MFMAs that use v stay below the waits before this
 __device__ __forceinline__ void tie(bf16x8_t& v) { asm volatile("" : "+v"(v)); }
+
+// One load instruction, whatever the compiler knows of the address: the waits
+// count them.
+template <typename T>
+__device__ __forceinline__ T ld_once(const void* p) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  uint64_t at = reinterpret_cast<uint64_t>(p);
+  asm volatile("" : "+v"(at));
+  if constexpr (sizeof(T) == 16) {
+    const u32x4 v = *(const __attribute__((address_space(1))) u32x4*)at;
+    return uint4{v.x, v.y, v.z, v.w};
+  } else {
+    return *(const __attribute__((address_space(1))) T*)at;
+  }
+}
 
 __device__ __forceinline__ int xcd_order(int b, int n) {
   const int q = n >> 3, r = n & 7, x = b & 7;
@@ -126,10 +155,12 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
   const int z = lb / s.tiles, tile = lb - z * s.tiles;
   const int tn = tile / s.tilesC, tc = tile - tn * s.tilesC;
   const int n0 = tn * C::BN, c0 = tc * C::BC;
-  const long P = (a.C + 31) / 32 * 32;
+  const long P = (a.C + 31) / 32 * 32, E = keep_exp_pitch(a.C);
   const long tbeg = (long)z * s.chunk;
   const int len = (int)min((long)s.chunk, a.tokens - tbeg);  // tokens of this split
   const int KT = (len + BK - 1) / BK;
+
+  const uint32_t sbase = lds_at(smem);
 
   // dy goes straight to LDS: lane slot i of a load is chunk_in(i) of its row
   const uint16_t* ysrc[C::YU];
@@ -145,7 +176,7 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
   // x goes through registers: 16 bytes of a row become 32
   const uint8_t *xsrc[C::XU], *esrc[C::XU];
   int xrow[C::XU];
-  uint32_t xdst[C::XU];
+  uint32_t xdst[C::XU], eshift[C::XU];
 #pragma unroll
   for (int u = 0; u < C::XU; ++u) {
     const int i = u * C::NT + tid;
@@ -153,46 +184,49 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
     const int c = c0 + 16 * k;
     xrow[u] = c < P ? r : 1 << 30;
     xsrc[u] = q + (tbeg + r) * P + c;
-    esrc[u] = e + (tbeg + r) * (P >> 5) + (c >> 5);
+    esrc[u] = e + (tbeg + r) * E + (c >> 7) * 4;
+    eshift[u] = (c >> 5 & 3) * 8;
     xdst[u] = (uint32_t)(C::Y_BYTES + r * C::PX + 16 * slot_of<C::PX>(2 * k, r));
   }
-  uint4 xq[C::XU];
-  uint32_t xe[C::XU];
-  auto fetch_x = [&](int kt) __attribute__((always_inline)) {
+  // two steps' worth of x on its way, in two sets of registers
+  struct X {
+    uint4 q[C::XU];
+    uint32_t e[C::XU];
+  };
+  const uint8_t* const pad = reinterpret_cast<const uint8_t*>(kgrad_zero) + 16;
+  // steps are fetched in order
+  auto fetch_x = [&](int kt, X& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < C::XU; ++u) {
-      // 128 four times, and any exponent: 0
-      xq[u] = uint4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-      xe[u] = 0;
-      if (kt * BK + xrow[u] < len) {
-        xq[u] = *reinterpret_cast<const uint4*>(xsrc[u] + (long)kt * BK * P);
-        xe[u] = esrc[u][(long)kt * BK * (P >> 5)];
-      }
+      const bool ok = kt * BK + xrow[u] < len;
+      x.q[u] = ld_once<uint4>(ok ? xsrc[u] : pad);
+      x.e[u] = ld_once<uint32_t>(ok ? esrc[u] : pad + 16);
+      xsrc[u] += BK * P;
+      esrc[u] += BK * E;
     }
   };
-  auto store_x = [&](int kt) __attribute__((always_inline)) {
-    char* base = smem + (kt & 1) * C::STAGE;
+  auto store_x = [&](int stage, const X& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < C::XU; ++u) {
-      const float step = keep_step(xe[u]);
+      const float step = keep_step(x.e[u] >> eshift[u] & 255u);
       float v[16];
-      unkeep4(v, xq[u].x, step);
-      unkeep4(v + 4, xq[u].y, step);
-      unkeep4(v + 8, xq[u].z, step);
-      unkeep4(v + 12, xq[u].w, step);
-      uint4* d = reinterpret_cast<uint4*>(base + xdst[u]);
-      d[0] = uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
-      d[1] = uint4{pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]),
-                   pack2(v[14], v[15])};
+      unkeep4(v, x.q[u].x, step);
+      unkeep4(v + 4, x.q[u].y, step);
+      unkeep4(v + 8, x.q[u].z, step);
+      unkeep4(v + 12, x.q[u].w, step);
+      const uint32_t d = sbase + (uint32_t)(stage * C::STAGE) + xdst[u];
+      ds_wr128<0>(d, pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+      ds_wr128<16>(d, pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]),
+                   pack2(v[14], v[15]));
     }
   };
-  auto fetch_y = [&](int kt) __attribute__((always_inline)) {
-    char* base = smem + (kt & 1) * C::STAGE;
+  auto fetch_y = [&](int kt, int stage) __attribute__((always_inline)) {
+    char* base = smem + stage * C::STAGE;
 #pragma unroll
     for (int u = 0; u < C::YU; ++u) {
-      const void* g = kt * BK + yrow[u] < len
-                          ? static_cast<const void*>(ysrc[u] + (long)kt * BK * a.dyt)
-                          : static_cast<const void*>(kgrad_zero);
+      const void* g = kt * BK + yrow[u] < len ? static_cast<const void*>(ysrc[u])
+                                              : static_cast<const void*>(kgrad_zero);
+      ysrc[u] += BK * a.dyt;
       __builtin_amdgcn_global_load_lds(g, (lds_ptr_t)(base + (u * C::NT + wave * 64) * 16), 16, 0,
                                        0);
     }
@@ -224,62 +258,112 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
 
-  const uint32_t sbase = lds_at(smem);
-  auto half = [&](uint32_t sb, bool bias, auto tag) __attribute__((always_inline)) {
+  bf16x8_t fx[2][C::TC], fy[2][C::TN];
+  auto read = [&](uint32_t sb, auto tag) __attribute__((always_inline)) {
     constexpr int S = decltype(tag)::value;
-    bf16x8_t fx[C::TC], fy[C::TN];
 #pragma unroll
     for (int i = 0; i < C::TC; ++i) {
       const v4s lo = ds_rdtr<(S * 32 + 0) * C::PX>(sb + rx[i]);
       const v4s hi = ds_rdtr<(S * 32 + 4) * C::PX>(sb + rx[i]);
-      fx[i] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      fx[S][i] =
+          __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       const v4s lo = ds_rdtr<(S * 32 + 0) * C::PY>(sb + ry[j]);
       const v4s hi = ds_rdtr<(S * 32 + 4) * C::PY>(sb + ry[j]);
-      fy[j] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      fy[S][j] =
+          __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+  };
+  auto wait_read = [&](int S) __attribute__((always_inline)) {
     lgkm_wait0();
 #pragma unroll
-    for (int i = 0; i < C::TC; ++i) tie(fx[i]);
+    for (int i = 0; i < C::TC; ++i) tie(fx[S][i]);
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) tie(fy[j]);
+    for (int j = 0; j < C::TN; ++j) tie(fy[S][j]);
+  };
+  auto mma = [&](int S) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < C::TC; ++i)
 #pragma unroll
       for (int j = 0; j < C::TN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], fy[j], acc[i][j], 0, 0, 0);
-    if (BIAS && bias)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[S][i], fy[S][j], acc[i][j], 0, 0, 0);
+  };
+  auto add_bias = [&](int S) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < C::TN; ++j)
-        sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fy[j], sum[j], 0, 0, 0);
+    for (int j = 0; j < C::TN; ++j)
+      sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fy[S][j], sum[j], 0, 0, 0);
   };
 
-  if (KT > 0) {
-    fetch_x(0);
-    store_x(0);
-    fetch_y(0);
-    if (KT > 1) fetch_x(1);
-  }
-  for (int kt = 0; kt < KT; ++kt) {
-    // this step's tiles are there, and all waves are done with the other stage
-    vm_wait0();
-    lgkm_wait0();
-    __builtin_amdgcn_s_barrier();
+  // Step kt computes from stage kt % 3.  While the MFMAs of its first half run,
+  // the second half is read and x of kt + 1 is turned into its stage; between the
+  // halves all waves meet: then the first half of kt + 1 is read behind the second
+  // half's MFMAs, and dy of kt + 3 may take this stage's place.  A load has two
+  // steps to arrive; past the last step they fetch zeros.
+  X xs[2];
+  int cur = 0;   // kt % 3
+  int turn = 0;  // kt % tilesC: the tiles along C share the steps of db
+  auto step = [&](int kt, X& x) __attribute__((always_inline)) {
+    const int next = cur == 2 ? 0 : cur + 1;
+    read(sbase + (uint32_t)(cur * C::STAGE), std::integral_constant<int, 1>());
+    vm_wait<2 * C::YU + 2 * C::XU>();  // x of kt + 1
     __builtin_amdgcn_sched_barrier(0);
-    if (kt + 1 < KT) {
-      store_x(kt + 1);
-      fetch_y(kt + 1);
-      if (kt + 2 < KT) fetch_x(kt + 2);
+    store_x(next, x);
+    fetch_x(kt + 3, x);
+    mma(0);
+    // a matrix instruction takes as long as four vector ones beside it
+#pragma unroll
+    for (int i = 0; i < C::TC * C::TN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    // the tiles along C share the steps of the columns' sums, their waves' halves
-    const bool mine = kt % s.tilesC == tc && wc == 0;
-    const uint32_t sb = sbase + (uint32_t)((kt & 1) * C::STAGE);
-    half(sb, mine, std::integral_constant<int, 0>());
-    half(sb, mine, std::integral_constant<int, 1>());
+    wait_read(1);
+    if (BIAS) {
+      if (turn == tc && wc == 0) {
+        add_bias(0);
+        add_bias(1);
+      }
+      turn = turn + 1 == s.tilesC ? 0 : turn + 1;
+    }
+    vm_wait<C::YU + 4 * C::XU>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    read(sbase + (uint32_t)(next * C::STAGE), std::integral_constant<int, 0>());
+    fetch_y(kt + 3, cur);
+    mma(1);
+    __builtin_amdgcn_sched_barrier(0);
+    // here, not at the next step: no register may move while a read is on its
+    // way to it, and the compiler does not know that it is
+    wait_read(0);
+    cur = next;
+  };
+  // the waits count loads, so that these keep their order
+  fetch_x(0, xs[0]);
+  store_x(0, xs[0]);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_y(0, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_x(1, xs[1]);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_y(1, 1);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_x(2, xs[0]);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_y(2, 2);
+  __builtin_amdgcn_sched_barrier(0);
+  vm_wait<2 * C::YU + 4 * C::XU>();
+  lgkm_wait0();
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  read(sbase, std::integral_constant<int, 0>());
+  wait_read(0);
+  for (int kt = 0; kt < KT; kt += 2) {  // a step past an odd last one adds zeros
+    step(kt, xs[1]);
+    step(kt + 1, xs[0]);
   }
+  vm_wait<0>();
 
   // lane: channels 4 g16 .. + 3 of output j16 of each 16 x 16
   float* dst = s.splits > 1 ? s.part + (long)z * a.N * a.C : a.dw;

@@ -81,14 +81,15 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
 
 // ---- activations in 8 bits (keep.hip, kgrad.hip) -----------------------------
 
-constexpr int KEEP_GROUP = 32;
 inline int64_t keep_pitch(int channels) { return (channels + 31) / 32 * 32; }
+// bytes of a row's exponents: whole words, so that four are one load
+__host__ __device__ inline int64_t keep_exp_pitch(int channels) { return (channels + 127) / 128 * 4; }
 inline size_t keep_values(int channels, int tokens) { return (size_t)tokens * keep_pitch(channels); }
 inline size_t keep_exps_at(int channels, int tokens) {
   return (keep_values(channels, tokens) + 15) / 16 * 16;
 }
 inline size_t keep_bytes(int channels, int tokens) {
-  return keep_exps_at(channels, tokens) + (size_t)tokens * (keep_pitch(channels) / 32);
+  return keep_exps_at(channels, tokens) + (size_t)tokens * keep_exp_pitch(channels);
 }
 
 // x (or da) read, y (a, the loaded rows, or dx) written; strides in elements

@@ -134,7 +134,7 @@ def _keep_size(channels, tokens):
 def test_keep_sizes():
     for c, t in ((8, 1), (32, 3), (40, 7), (1408, 8192), (65536, 1 << 23), (64, 0)):
         p = -(-c // 32) * 32
-        assert _keep_size(c, t) == (S.OK, -(-t * p // 16) * 16 + t * p // 32)
+        assert _keep_size(c, t) == (S.OK, -(-t * p // 16) * 16 + t * -(-p // 128) * 4)
     for c, t in ((0, 1), (12, 1), (65544, 1), (64, -1), (64, (1 << 23) + 1)):
         _refused(_keep_size(c, t)[0], S.E_SHAPE)
     _refused(ops.lib().pulse_keep_sizes(None, 1, ctypes.c_size_t()), S.E_INVALID_ARG)
