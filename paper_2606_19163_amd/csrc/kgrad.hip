@@ -384,6 +384,275 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
 #endif
 }
 
+// Fragments of x in bf16 for many outputs: [c / 16][t / 32] of 1 KB, lane l
+// holding channel l % 16 of tokens 8 (l / 16) to + 7, zeros past the last
+// token and channel.  A block turns 64 tokens of 128 channels.
+constexpr int WIDE_C = 128;
+__global__ __launch_bounds__(256) void k_kgrad_turn(KgradArgs a, const uint8_t* q,
+                                                    const uint8_t* e, char* frags) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int PX = WIDE_C * 2;
+  __shared__ __attribute__((aligned(1024))) char smem[BK * PX];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const long P = (a.C + 31) / 32 * 32, E = keep_exp_pitch(a.C);
+  const int c0 = blockIdx.y * WIDE_C;
+  const long t0 = (long)blockIdx.x * BK;
+  const long blocks32 = (long)gridDim.x * 2;
+  const uint32_t sbase = lds_at(smem);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = u * 256 + tid, r = i >> 3, k = i & 7, c = c0 + 16 * k;
+    uint4 w = uint4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+    float step = 0.f;
+    if (t0 + r < a.tokens && c < P) {
+      w = *reinterpret_cast<const uint4*>(q + (t0 + r) * P + c);
+      step = keep_step(e[(t0 + r) * E + (c >> 5)]);
+    }
+    float v[16];
+    unkeep4(v, w.x, step);
+    unkeep4(v + 4, w.y, step);
+    unkeep4(v + 8, w.z, step);
+    unkeep4(v + 12, w.w, step);
+    const uint32_t d = sbase + (uint32_t)(r * PX + 16 * slot_of<PX>(2 * k, r));
+    ds_wr128<0>(d, pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+    ds_wr128<16>(d, pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]),
+                 pack2(v[14], v[15]));
+  }
+  lgkm_wait0();
+  __syncthreads();
+  const int trow = 8 * (lane >> 4) + ((lane & 15) >> 2), tcol = 4 * (lane & 3);
+  bf16x8_t f[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int col = (2 * wave + i) * 16 + tcol;
+    const uint32_t rx =
+        sbase + (uint32_t)(trow * PX + slot_of<PX>(col >> 3, trow) * 16 + (col & 7) * 2);
+    const v4s l0 = ds_rdtr<0>(rx), h0 = ds_rdtr<4 * PX>(rx);
+    const v4s l1 = ds_rdtr<32 * PX>(rx), h1 = ds_rdtr<36 * PX>(rx);
+    f[i][0] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l0, h0, 0, 1, 2, 3, 4, 5, 6, 7));
+    f[i][1] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l1, h1, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  lgkm_wait0();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    tie(f[i][0]);
+    tie(f[i][1]);
+    char* dst = frags + ((c0 / 16 + 2 * wave + i) * blocks32 + 2 * blockIdx.x) * 1024 + lane * 16;
+    *reinterpret_cast<bf16x8_t*>(dst) = f[i][0];
+    *reinterpret_cast<bf16x8_t*>(dst + 1024) = f[i][1];
+  }
+#endif
+}
+
+// The gradient from such fragments: 256 outputs x 128 channels per block, eight
+// waves of 64 x 64.
+template <int BN_, int STAGES_>
+struct Wide {
+  static constexpr int BN = BN_, BC = WIDE_C, NW = BN / 32, NT = NW * 64, TN = 4, TC = 4;
+  static constexpr int WAVES_N = NW / 2;
+  static constexpr int PY = BN * 2, Y_BYTES = BK * PY, X_BYTES = BK * BC * 2;
+  static constexpr int STAGE = Y_BYTES + X_BYTES, STAGES = STAGES_;
+  static constexpr int YU = Y_BYTES / (NT * 16), XU = X_BYTES / (NT * 16), LOADS = YU + XU;
+};
+
+template <int OFF>
+__device__ __forceinline__ bf16x8_t ds_rd128(uint32_t addr) {
+  bf16x8_t v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+
+template <class C, bool BIAS>
+__global__ __launch_bounds__(C::NT, 2) void k_kgrad_wide(KgradArgs a, Split s,
+                                                         const char* frags) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[C::STAGES * C::STAGE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wn = wave % C::WAVES_N, wc = wave / C::WAVES_N;
+  const int lb = xcd_order(blockIdx.x, gridDim.x);
+  const int z = lb / s.tiles, tile = lb - z * s.tiles;
+  const int tn = tile / s.tilesC, tc = tile - tn * s.tilesC;
+  const int n0 = tn * C::BN, c0 = tc * C::BC;
+  const long tbeg = (long)z * s.chunk;
+  const int len = (int)min((long)s.chunk, a.tokens - tbeg);
+  const int KT = (len + BK - 1) / BK;
+  const long blocks32 = (long)((a.tokens + BK - 1) / BK) * 2;
+
+  // lane slot i of a load is chunk_in(i) of its row; outputs past the last read
+  // the first ones', and are not stored
+  const uint16_t* ysrc[C::YU];
+  int yrow[C::YU];
+#pragma unroll
+  for (int u = 0; u < C::YU; ++u) {
+    const int i = u * C::NT + tid;
+    const int r = i / (C::PY / 16);
+    const int n = n0 + 8 * chunk_in<C::PY>(i - r * (C::PY / 16), r);
+    yrow[u] = r;
+    ysrc[u] = static_cast<const uint16_t*>(a.dy) + (tbeg + r) * a.dyt + (n < a.N ? n : 0);
+  }
+  // fragment f of a stage: channels f / 2, half f % 2
+  const char* xsrc[C::XU];
+#pragma unroll
+  for (int u = 0; u < C::XU; ++u) {
+    const int f = u * C::NW + wave;
+    xsrc[u] = frags + ((c0 / 16 + f / 2) * blocks32 + tbeg / 32 + f % 2) * 1024 + lane * 16;
+  }
+  auto fetch = [&](int kt, int stage) __attribute__((always_inline)) {
+    char* base = smem + stage * C::STAGE;
+    if ((kt + 1) * BK <= len) {
+#pragma unroll
+      for (int u = 0; u < C::YU; ++u)
+        __builtin_amdgcn_global_load_lds(
+            ysrc[u], (lds_ptr_t)(base + (u * C::NT + wave * 64) * 16), 16, 0, 0);
+    } else {
+#pragma unroll
+      for (int u = 0; u < C::YU; ++u) {
+        const void* g = kt * BK + yrow[u] < len ? static_cast<const void*>(ysrc[u])
+                                                : static_cast<const void*>(kgrad_zero);
+        __builtin_amdgcn_global_load_lds(g, (lds_ptr_t)(base + (u * C::NT + wave * 64) * 16), 16,
+                                         0, 0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < C::YU; ++u) ysrc[u] += BK * a.dyt;
+#pragma unroll
+    for (int u = 0; u < C::XU; ++u) {
+      __builtin_amdgcn_global_load_lds(
+          xsrc[u], (lds_ptr_t)(base + C::Y_BYTES + (u * C::NW + wave) * 1024), 16, 0, 0);
+      xsrc[u] += 2 * 1024;
+    }
+  };
+
+  const int g16 = lane >> 4, j16 = lane & 15;
+  const int trow = 8 * g16 + (j16 >> 2), tcol = 4 * (j16 & 3);
+  const uint32_t sbase = lds_at(smem);
+  const uint32_t rx = sbase + (uint32_t)(C::Y_BYTES + wc * C::TC * 2048 + lane * 16);
+  uint32_t ry[C::TN];
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int col = (wn * C::TN + j) * 16 + tcol;
+    ry[j] = sbase +
+            (uint32_t)(trow * C::PY + slot_of<C::PY>(col >> 3, trow) * 16 + (col & 7) * 2);
+  }
+  f32x4_t acc[C::TC][C::TN], sum[C::TN];
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    sum[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8_t ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
+
+  bf16x8_t fx[2][C::TC], fy[2][C::TN];
+  auto read = [&](uint32_t off, auto tag) __attribute__((always_inline)) {
+    constexpr int S = decltype(tag)::value;
+    fx[S][0] = ds_rd128<S * 1024>(rx + off);
+    fx[S][1] = ds_rd128<S * 1024 + 2048>(rx + off);
+    fx[S][2] = ds_rd128<S * 1024 + 4096>(rx + off);
+    fx[S][3] = ds_rd128<S * 1024 + 6144>(rx + off);
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const v4s lo = ds_rdtr<(S * 32 + 0) * C::PY>(ry[j] + off);
+      const v4s hi = ds_rdtr<(S * 32 + 4) * C::PY>(ry[j] + off);
+      fy[S][j] =
+          __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
+  auto wait_read = [&](int S) __attribute__((always_inline)) {
+    lgkm_wait0();
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) tie(fx[S][i]);
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) tie(fy[S][j]);
+  };
+  auto mma = [&](int S) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[S][i], fy[S][j], acc[i][j], 0, 0, 0);
+  };
+  auto add_bias = [&](int S) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j)
+      sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fy[S][j], sum[j], 0, 0, 0);
+  };
+  const std::integral_constant<int, 0> first{};
+  const std::integral_constant<int, 1> second{};
+
+  // Step kt computes from stage kt % STAGES: its second half is read while the first
+  // half's MFMAs run; then all waves meet, and the first half of kt + 1 is read
+  // behind the second half's MFMAs, while kt + STAGES takes this stage's place.
+  // Reads end before the step does: no register may move while a read is on its
+  // way to it, and the compiler does not know that it is.
+#pragma unroll
+  for (int i = 0; i < C::STAGES; ++i)
+    if (i < KT) fetch(i, i);
+  // stage kt is there: at most the later ones are on their way
+  auto wait_stage = [&](int kt, int later) __attribute__((always_inline)) {
+    if (later > 1 && kt + 2 < KT)
+      vm_wait<2 * C::LOADS>();
+    else if (later > 0 && kt + 1 < KT)
+      vm_wait<C::LOADS>();
+    else
+      vm_wait<0>();
+  };
+  wait_stage(0, C::STAGES - 1);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  read(0, first);
+  wait_read(0);
+  int cur = 0;   // kt % STAGES
+  int turn = 0;  // kt % tilesC: the tiles along C share the steps of db
+  for (int kt = 0; kt < KT; ++kt) {
+    const int next = cur + 1 == C::STAGES ? 0 : cur + 1;
+    read((uint32_t)(cur * C::STAGE), second);
+    __builtin_amdgcn_sched_barrier(0);
+    mma(0);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_read(1);
+    if (BIAS) {
+      if (turn == tc && wc == 0) {
+        add_bias(0);
+        add_bias(1);
+      }
+      turn = turn + 1 == s.tilesC ? 0 : turn + 1;
+    }
+    wait_stage(kt + 1, C::STAGES - 2);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + C::STAGES < KT) fetch(kt + C::STAGES, cur);
+    __builtin_amdgcn_sched_barrier(0);
+    read((uint32_t)(next * C::STAGE), first);
+    __builtin_amdgcn_sched_barrier(0);
+    mma(1);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_read(0);
+    cur = next;
+  }
+
+  float* dst = s.splits > 1 ? s.part + (long)z * a.N * a.C : a.dw;
+  const bool add = s.splits == 1 && a.accumulate;
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = n0 + (wn * C::TN + j) * 16 + j16;
+    if (n >= a.N) continue;
+#pragma unroll
+    for (int i = 0; i < C::TC; ++i) {
+      const int c = c0 + wc * 64 + i * 16 + 4 * g16;
+      if (c >= a.C) continue;
+      f32x4_t* p = reinterpret_cast<f32x4_t*>(dst + (long)n * a.C + c);
+      *p = add ? *p + acc[i][j] : acc[i][j];
+    }
+    if (BIAS && wc == 0 && g16 == 0) s.bias[((long)z * s.tilesC + tc) * a.N + n] = sum[j][0];
+  }
+#endif
+}
+
 // Blocks below `wblocks`: four values of dw each thread, summed over the
 // splits; the others: db, 64 outputs x 4 lanes of partial sums.
 __global__ __launch_bounds__(256) void k_kgrad_sum(KgradArgs a, Split s, int wblocks) {
@@ -425,34 +694,49 @@ __global__ __launch_bounds__(256) void k_kgrad_clear(float* p, long n) {
 struct Plan {
   bool large;
   Split s;
-  size_t floats;
+  size_t sums;   // bytes of the partial sums
+  size_t bytes;  // with the fragments of x
 };
 
 Plan plan_of(int tokens, int C, int N) {
   Plan p{};
-  const long tl = (long)((N + 255) / 256) * ((C + 127) / 128);
-  p.large = tl * ((tokens + 1023) / 1024) >= 128;
-  const int bn = p.large ? 256 : 64, bc = p.large ? 128 : 64;
+  // The launch that turns x first pays from 7 GFLOP on: 16.5 against 12.7 us at
+  // 512 x 768 x 2304, 28.4 against 28.3 at 2048 x 768 x 2304, 31.3 against 36.7 at
+  // 8192 x 768 x 768, 23.5 against 30.2 at 512 x 1408 x 5632.
+  p.large = (double)tokens * N * C >= 3.5e9;
+    const int bn = p.large ? 128 : 64, bc = p.large ? 128 : 64;
   p.s.tilesC = (C + bc - 1) / bc;
   p.s.tiles = (N + bn - 1) / bn * p.s.tilesC;
   const int steps = (tokens + BK - 1) / BK;
-  const int room = p.large ? 256 : 512;
+  const int room = 512;
   int splits = p.s.tiles >= room ? 1 : room / p.s.tiles;
-  if (splits > (steps + 3) / 4) splits = (steps + 3) / 4;
+  if (splits > (steps + 7) / 8) splits = (steps + 7) / 8;
   if (splits < 1) splits = 1;
   p.s.chunk = (steps + splits - 1) / splits * BK;
   p.s.splits = tokens ? (tokens + p.s.chunk - 1) / p.s.chunk : 1;
   const size_t part = p.s.splits > 1 ? (size_t)p.s.splits * N * C : 0;
-  p.floats = part + (size_t)p.s.splits * p.s.tilesC * N;
+  p.sums = ((part + (size_t)p.s.splits * p.s.tilesC * N) * 4 + 1023) / 1024 * 1024;
+  p.bytes = p.sums + (p.large ? (size_t)steps * BK * p.s.tilesC * WIDE_C * 2 : 0);
   return p;
 }
 
-template <class C>
-hipError_t run(const KgradArgs& a, const Split& s, hipStream_t st) {
+hipError_t run(const KgradArgs& a, const Plan& p, hipStream_t st) {
+  using Small = Tile<64, 64, 32, 32>;
+  using W = Wide<128, 2>;
   const uint8_t* q = static_cast<const uint8_t*>(a.kept);
-  auto kern = a.db ? k_kgrad<C, true> : k_kgrad<C, false>;
-  hipLaunchKernelGGL(kern, dim3(s.tiles * s.splits), dim3(C::NT), 0, st, a, s, q,
-                     q + keep_exps_at(a.C, a.tokens));
+  const uint8_t* e = q + keep_exps_at(a.C, a.tokens);
+  if (!p.large) {
+    auto kern = a.db ? k_kgrad<Small, true> : k_kgrad<Small, false>;
+    hipLaunchKernelGGL(kern, dim3(p.s.tiles * p.s.splits), dim3(Small::NT), 0, st, a, p.s, q, e);
+    return hipGetLastError();
+  }
+  char* frags = reinterpret_cast<char*>(a.ws) + p.sums;
+  hipLaunchKernelGGL(k_kgrad_turn, dim3((a.tokens + BK - 1) / BK, p.s.tilesC), dim3(256), 0, st, a,
+                     q, e, frags);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  auto kern = a.db ? k_kgrad_wide<W, true> : k_kgrad_wide<W, false>;
+  hipLaunchKernelGGL(kern, dim3(p.s.tiles * p.s.splits), dim3(W::NT), 0, st, a, p.s, frags);
   return hipGetLastError();
 }
 
@@ -463,7 +747,7 @@ hipError_t clear(float* p, long n, hipStream_t st) {
 
 }  // namespace
 
-size_t kgrad_bytes(int tokens, int C, int N) { return plan_of(tokens, C, N).floats * 4; }
+size_t kgrad_bytes(int tokens, int C, int N) { return plan_of(tokens, C, N).bytes; }
 
 hipError_t launch_kgrad(const KgradArgs& a, hipStream_t st) {
   if (a.tokens == 0) {
@@ -474,8 +758,7 @@ hipError_t launch_kgrad(const KgradArgs& a, hipStream_t st) {
   Plan p = plan_of(a.tokens, a.C, a.N);
   p.s.part = a.ws;
   p.s.bias = a.ws + (p.s.splits > 1 ? (size_t)p.s.splits * a.N * a.C : 0);
-  hipError_t e = p.large ? run<Tile<256, 128, 64, 64>>(a, p.s, st)
-                         : run<Tile<64, 64, 32, 32>>(a, p.s, st);
+  hipError_t e = run(a, p, st);
   if (e != hipSuccess) return e;
   const int wblocks = p.s.splits > 1 ? (int)(((long)a.N * a.C / 4 + 255) / 256) : 0;
   const int blocks = wblocks + (a.db ? (a.N + 63) / 64 : 0);

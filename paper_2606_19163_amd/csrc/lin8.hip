@@ -15,6 +15,9 @@ constexpr int FRAG = 1024;
 constexpr int ROWS = 256;  // rows of both operands are padded to whole tiles
 
 __host__ __device__ inline long pad_to(long v, long m) { return (v + m - 1) / m * m; }
+// fragments along K: steps of the kernels take one or two, so there are whole
+// pairs
+__host__ __device__ inline int k_frags(int K) { return (int)(pad_to(K, 128) / 64); }
 
 // A scale m 2^e, 0.5 <= m < 1: a sum times two of them passes fp32's range only
 // where the result does.
@@ -33,51 +36,97 @@ __host__ __device__ inline Laid laid(const void* p, int rows) {
   return Laid{reinterpret_cast<const Scale*>(c), c + pad_to(rows, ROWS) * sizeof(Scale)};
 }
 size_t laid_bytes(int rows, int K) {
-  return (size_t)pad_to(rows, ROWS) * sizeof(Scale) + (size_t)pad_to(rows, ROWS) * pad_to(K, 64);
+  return (size_t)pad_to(rows, ROWS) * sizeof(Scale) + (size_t)pad_to(rows, ROWS) * k_frags(K) * 64;
 }
 
-// One wave per row: its largest value, then its bytes.  Rows of zeros fill the
-// last 16.
-template <typename T>
-__global__ __launch_bounds__(256) void k_rows8(int rows, int K, const T* x, long xt, Scale* scale,
-                                               char* frag) {
-#pragma clang fp contract(off)
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= (int)pad_to(rows, 16)) return;
-  const int KS = (int)pad_to(K, 64) / 64;
-  const T* px = x + (long)row * xt;
-  uint32_t m = 0;
-  if (row < rows)
-    for (int k = 8 * lane; k < K; k += 512) {
-      Vec8<T> v;
-      v.load(px + k);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v.get(i)) & 0x7fffffffu);
-    }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+// What a row's largest value gives: the factor of its values, and its scale.
+struct Turn {
+  float r;
+  Scale s;
+};
+__device__ __forceinline__ Turn turn_of(uint32_t m) {
   const float top = fmaxf(__uint_as_float(m), 0x1p-100f);
   const bool bad = m >= 0x7f800000u;
-  const float r = bad ? 0.f : 127.f / top;
-  if (lane == 0) {
-    const float s = top / 127.f;  // at least 2^-107: never denormal
-    scale[row] = Scale{bad ? __uint_as_float(0x7fc00000u) : __builtin_amdgcn_frexp_mantf(s),
-                       bad ? 0 : __builtin_amdgcn_frexp_expf(s)};
-  }
-  char* pf = frag + (long)(row >> 4) * KS * FRAG + (row & 15) * 16;
-  for (int k = 8 * lane; k < KS * 64; k += 512) {
-    uint32_t b[8];
-    Vec8<T> v;
-    v.zero();
-    if (row < rows && k < K && !bad) v.load(px + k);
+  const float s = top / 127.f;  // at least 2^-107: never denormal
+  return Turn{bad ? 0.f : 127.f / top,
+              Scale{bad ? __uint_as_float(0x7fc00000u) : __builtin_amdgcn_frexp_mantf(s),
+                    bad ? 0 : __builtin_amdgcn_frexp_expf(s)}};
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t bits_max(uint32_t m, const Vec8<T>& v) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = v.get(i) * r;
-      b[i] = __float_as_uint(t + 12582912.f) & 255u;  // to nearest even, as an integer
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v.get(i)) & 0x7fffffffu);
+  return m;
+}
+struct MaxBits {
+  __device__ __forceinline__ float operator()(float a, float b) const {
+    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+  }
+};
+// over a wave's lanes; NaN is above infinity
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+  return __float_as_uint(lanes_op<64>(__uint_as_float(m), MaxBits()));
+}
+
+// eight values as bytes: the product is rounded, then its sum with 1.5 2^23,
+// to a whole number, to nearest even, whose low byte is at the bottom
+template <typename T>
+__device__ __forceinline__ uint2 bytes8(const Vec8<T>& v, float r) {
+#pragma clang fp contract(off)
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = r == 0.f ? 0.f : v.get(i) * r;
+    b[i] = __float_as_uint(t + 12582912.f);
+  }
+  const auto four = [](const uint32_t* b) __attribute__((always_inline)) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+  };
+  return uint2{four(b), four(b + 4)};
+}
+
+// A wave per row, the 16 rows of a fragment per block, so that whole lines
+// meet in one L2.  Rows of up to 512 NV values stay in registers between the
+// search for the largest and the bytes.
+template <typename T, int NV>
+__global__ __launch_bounds__(1024) void k_rows8(int rows, int K, const T* x, long xt, Scale* scale,
+                                                char* frag) {
+  const int row = blockIdx.x * 16 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int KS = k_frags(K);
+  const bool in = row < rows;
+  const T* px = x + (long)row * xt;
+  Vec8<T> v[NV];
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    v[j].zero();
+    if (in && 8 * lane + 512 * j < K) v[j].load(px + 8 * lane + 512 * j);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) m = bits_max(m, v[j]);
+  if (in)
+    for (int k = 8 * lane + 512 * NV; k < K; k += 512) {
+      Vec8<T> w;
+      w.load(px + k);
+      m = bits_max(m, w);
     }
+  const Turn t = turn_of(wave_max(m));
+  if (lane == 0) scale[row] = t.s;
+  char* pf = frag + (long)blockIdx.x * KS * FRAG + (row & 15) * 16;
+  const auto put = [&](int k, const Vec8<T>& w) __attribute__((always_inline)) {
     *reinterpret_cast<uint2*>(pf + (long)(k >> 6) * FRAG + ((k >> 4) & 3) * 256 + (k & 8)) =
-        uint2{b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24,
-              b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24};
+        bytes8(w, t.r);
+  };
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (8 * lane + 512 * j < KS * 64) put(8 * lane + 512 * j, v[j]);
+  for (int k = 8 * lane + 512 * NV; k < KS * 64; k += 512) {
+    Vec8<T> w;
+    w.zero();
+    if (in && k < K) w.load(px + k);
+    put(k, w);
   }
 }
 
@@ -108,26 +157,71 @@ __device__ __forceinline__ uint2 out4(i32x4_t acc, Scale sx, const Outs& o) {
 }
 
 // Few rows: a block of 4 waves takes 16 outputs and TT x 16 rows, its waves a
-// quarter of K each, straight from memory; their sums meet in LDS.
-template <int ACT, int TT>
+// quarter of K each, the weights straight from memory; their sums meet in LDS.
+// FUSED: up to 16 rows, which every block lays out for itself, in LDS, while its
+// first weights are on their way: one launch, where the rows are few enough.
+template <int ACT, int TT, bool FUSED>
 __global__ __launch_bounds__(256) void k_lin8_few(Lin8Args a, Laid x, Laid w) {
+  extern __shared__ __attribute__((aligned(16))) char rows[];  // FUSED: [tokens][pitch]
   __shared__ i32x4_t part[4][TT][64];
+  __shared__ Scale scales[16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int KS = (int)pad_to(a.K, 64) / 64;
+  const int KS = k_frags(a.K);
   const int tn = blockIdx.x, tt = blockIdx.y * TT;
-  const char* pw = w.frag + (long)tn * KS * FRAG + lane * 16;
-  const char* px = x.frag + (long)tt * KS * FRAG + lane * 16;
+  const char* pw = w.frag + ((long)tn * KS + wave) * FRAG + lane * 16;
+  constexpr int AHEAD = 8;
+  i32x4_t fw[AHEAD];
+  const auto fetch = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (k0 + 4 * i + wave < KS)
+        fw[i] = *reinterpret_cast<const i32x4_t*>(pw + (long)(k0 + 4 * i) * FRAG);
+  };
+  fetch(0);
+  const int pitch = FUSED ? KS * 64 + 16 : 0;
+  const char* px[TT];
+  if constexpr (FUSED) {
+    for (int t = wave; t < a.tokens; t += 4) {
+      const uint16_t* src = static_cast<const uint16_t*>(a.x) + t * a.xt;
+      uint32_t m = 0;
+      for (int k = 8 * lane; k < a.K; k += 512) {
+        Vec8<uint16_t> v;
+        v.load(src + k);
+        m = bits_max(m, v);
+      }
+      const Turn q = turn_of(wave_max(m));
+      if (lane == 0) scales[t] = q.s;
+      for (int k = 8 * lane; k < KS * 64; k += 512) {
+        Vec8<uint16_t> v;
+        v.zero();
+        if (k < a.K) v.load(src + k);
+        *reinterpret_cast<uint2*>(rows + t * pitch + k) = bytes8(v, q.r);
+      }
+    }
+    __syncthreads();
+    // rows past the last give sums that are not stored
+    px[0] = rows + min(lane & 15, a.tokens - 1) * pitch + (lane >> 4) * 16 + wave * 64;
+  } else {
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+      px[i] = x.frag + ((long)(tt + i) * KS + wave) * FRAG + lane * 16;
+  }
   i32x4_t acc[TT];
 #pragma unroll
   for (int i = 0; i < TT; ++i) acc[i] = i32x4_t{0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = wave; k < KS; k += 4) {
-    const i32x4_t fw = *reinterpret_cast<const i32x4_t*>(pw + (long)k * FRAG);
+  for (int k0 = 0; k0 < KS; k0 += 4 * AHEAD) {
+    if (k0) fetch(k0);
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-      const i32x4_t fx = *reinterpret_cast<const i32x4_t*>(px + ((long)i * KS + k) * FRAG);
-      acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc[i], 0, 0, 0);
+    for (int j = 0; j < AHEAD; ++j) {
+      const int k = k0 + 4 * j;
+      if (k + wave < KS)
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+          const i32x4_t fx =
+              *reinterpret_cast<const i32x4_t*>(px[i] + (long)k * (FUSED ? 64 : FRAG));
+          acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j], fx, acc[i], 0, 0, 0);
+        }
     }
   }
 #pragma unroll
@@ -141,24 +235,25 @@ __global__ __launch_bounds__(256) void k_lin8_few(Lin8Args a, Laid x, Laid w) {
       Outs o;
       o.load(a, w.scale, n);
       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.yt + n) =
-          out4<ACT>(s, x.scale[t], o);
+          out4<ACT>(s, FUSED ? scales[t] : x.scale[t], o);
     }
   }
 }
 
 // BT rows x BN outputs per block, WT x WN per wave
-template <int BT_, int BN_, int WT_, int WN_, int STAGES_>
+template <int BT_, int BN_, int WT_, int WN_, int STAGES_, int KB_>
 struct Tile {
+  static constexpr int KB = KB_;  // fragments along K per step
   static constexpr int BT = BT_, BN = BN_, WT = WT_, WN = WN_, STAGES = STAGES_;
   static constexpr int WAVES_T = BT / WT, NW = WAVES_T * (BN / WN), NT = NW * 64;
   static constexpr int TT = WT / 16, TN = WN / 16;
-  static constexpr int FT = BT / 16, FN = BN / 16, STAGE = (FT + FN) * FRAG;
-  static constexpr int NU = (FT + FN) / NW;  // fragments per wave and step
+  static constexpr int FT = BT / 16, FN = BN / 16, STAGE = (FT + FN) * KB * FRAG;
+  static constexpr int NU = (FT + FN) * KB / NW;  // fragments per wave and step
   static constexpr int LDS = STAGES * STAGE;
   // outputs on their way out: WT rows of each wave, which start 16 bytes apart
   // modulo the banks
   static constexpr int PY = WN * 2 + 16, OUT = WT * PY, CPR = WN / 8;
-  static_assert(NU * NW == FT + FN && FT % NW == 0, "loads");
+  static_assert(NU * NW == (FT + FN) * KB && (KB == 1 || KB == 2), "loads");
   static_assert(NW * OUT <= LDS, "outputs");
   static_assert(LDS <= 160 * 1024 && (STAGES - 2) * NU < 64, "LDS, vmcnt");
 };
@@ -178,11 +273,12 @@ __device__ __forceinline__ i32x4_t ds_rd128(uint32_t addr) {
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
   return v;
 }
-template <int N>
+// N fragments, STEP apart
+template <int N, int STEP>
 __device__ __forceinline__ void ds_rd_n(i32x4_t* f, uint32_t addr) {
   if constexpr (N > 0) {
-    ds_rd_n<N - 1>(f, addr);
-    f[N - 1] = ds_rd128<(N - 1) * FRAG>(addr);
+    ds_rd_n<N - 1, STEP>(f, addr);
+    f[N - 1] = ds_rd128<(N - 1) * STEP * FRAG>(addr);
   }
 }
 __device__ __forceinline__ void tie(i32x4_t& v) { asm volatile("" : "+v"(v)); }
@@ -203,21 +299,22 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
   const int wt = wave % C::WAVES_T, wn = wave / C::WAVES_T;
   const int lb = xcd_order(blockIdx.x, gridDim.x);
   const int tt = lb / tilesN, tn = lb - tt * tilesN;
-  const int KT = (int)pad_to(a.K, 64) / 64;
-  // rows are padded to whole tiles: every fragment of a tile exists
+  const int KS = k_frags(a.K), KT = KS / C::KB;
+  // fragment f of a stage: part f % KB along K of rows f / KB.  Rows are padded
+  // to whole tiles: every fragment of a tile exists.
   const char* src[C::NU];
 #pragma unroll
   for (int u = 0; u < C::NU; ++u) {
-    const int f = u * C::NW + wave;
-    src[u] = (f < C::FT ? x.frag + ((long)tt * C::FT + f) * KT * FRAG
-                        : w.frag + ((long)tn * C::FN + f - C::FT) * KT * FRAG) +
-             lane * 16;
+    const int f = u * C::NW + wave, r = f / C::KB;
+    src[u] = (r < C::FT ? x.frag + ((long)tt * C::FT + r) * KS * FRAG
+                        : w.frag + ((long)tn * C::FN + r - C::FT) * KS * FRAG) +
+             f % C::KB * FRAG + lane * 16;
   }
   auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < C::NU; ++u)
       __builtin_amdgcn_global_load_lds(
-          src[u] + (long)kt * FRAG,
+          src[u] + (long)kt * C::KB * FRAG,
           (lds_ptr_t)(smem + stage * C::STAGE + (u * C::NW + wave) * FRAG), 16, 0, 0);
   };
   i32x4_t acc[C::TN][C::TT];
@@ -226,6 +323,26 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
 #pragma unroll
     for (int i = 0; i < C::TT; ++i) acc[j][i] = i32x4_t{0, 0, 0, 0};
   const uint32_t base = lds_at(smem) + lane * 16;
+  i32x4_t fx[C::KB][C::TT], fw[C::KB][C::TN];
+  auto read = [&](uint32_t sb, auto tag) __attribute__((always_inline)) {
+    constexpr int P = decltype(tag)::value;
+    ds_rd_n<C::TT, C::KB>(fx[P], sb + (wt * C::TT * C::KB + P) * FRAG);
+    ds_rd_n<C::TN, C::KB>(fw[P], sb + ((C::FT + wn * C::TN) * C::KB + P) * FRAG);
+  };
+  auto arrive = [&](int P) __attribute__((always_inline)) {
+    lgkm_wait0();
+#pragma unroll
+    for (int i = 0; i < C::TT; ++i) tie(fx[P][i]);
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) tie(fw[P][j]);
+  };
+  auto mul = [&](int P) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+      for (int i = 0; i < C::TT; ++i)
+        acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[P][j], fx[P][i], acc[j][i], 0, 0, 0);
+  };
 #pragma unroll
   for (int i = 0; i < C::STAGES - 1; ++i)
     if (i < KT) issue(i, i);
@@ -241,19 +358,15 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
     if (kt + C::STAGES - 1 < KT)
       issue(kt + C::STAGES - 1, stage == 0 ? C::STAGES - 1 : stage - 1);
     const uint32_t sb = base + stage * C::STAGE;
-    i32x4_t fx[C::TT], fw[C::TN];
-    ds_rd_n<C::TT>(fx, sb + wt * C::TT * FRAG);
-    ds_rd_n<C::TN>(fw, sb + (C::FT + wn * C::TN) * FRAG);
-    lgkm_wait0();
-#pragma unroll
-    for (int i = 0; i < C::TT; ++i) tie(fx[i]);
-#pragma unroll
-    for (int j = 0; j < C::TN; ++j) tie(fw[j]);
-#pragma unroll
-    for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-      for (int i = 0; i < C::TT; ++i)
-        acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j], fx[i], acc[j][i], 0, 0, 0);
+    read(sb, std::integral_constant<int, 0>());
+    arrive(0);
+    if constexpr (C::KB == 2) {
+      read(sb, std::integral_constant<int, 1>());
+      mul(0);
+      __builtin_amdgcn_sched_barrier(0);
+      arrive(1);
+    }
+    mul(C::KB - 1);
     __builtin_amdgcn_sched_barrier(0);
     stage = stage + 1 == C::STAGES ? 0 : stage + 1;
   }
@@ -296,34 +409,56 @@ hipError_t tiles(const Lin8Args& a, Laid x, Laid w, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int ACT>
-hipError_t run(const Lin8Args& a, Laid x, Laid w, hipStream_t st) {
-  if (a.tokens <= 64) {
-    const int tn = (a.N + 15) / 16;
-    if (a.tokens <= 16)
-      hipLaunchKernelGGL((k_lin8_few<ACT, 1>), dim3(tn, 1), dim3(256), 0, st, a, x, w);
-    else
-      hipLaunchKernelGGL((k_lin8_few<ACT, 2>), dim3(tn, (a.tokens + 31) / 32), dim3(256), 0, st, a,
-                         x, w);
-    return hipGetLastError();
-  }
-  const long big = (long)((a.tokens + 127) / 128) * ((a.N + 255) / 256);
-  return big >= 256 ? tiles<Tile<128, 256, 64, 128, 3>, ACT>(a, x, w, st)
-                    : tiles<Tile<64, 128, 32, 64, 3>, ACT>(a, x, w, st);
-}
-
 template <typename T>
 hipError_t rows8(int rows, int K, const void* x, long xt, Laid to, hipStream_t st) {
-  hipLaunchKernelGGL(k_rows8<T>, dim3((pad_to(rows, 16) + 3) / 4), dim3(256), 0, st, rows, K,
+  auto kern = K <= 512    ? k_rows8<T, 1>
+              : K <= 1024 ? k_rows8<T, 2>
+              : K <= 1536 ? k_rows8<T, 3>
+              : K <= 2048 ? k_rows8<T, 4>
+                          : k_rows8<T, 6>;
+  hipLaunchKernelGGL(kern, dim3(pad_to(rows, 16) / 16), dim3(1024), 0, st, rows, K,
                      static_cast<const T*>(x), xt, const_cast<Scale*>(to.scale),
                      const_cast<char*>(to.frag));
   return hipGetLastError();
 }
 
+// Bytes of LDS that up to 16 rows take, if every block is to lay them out.
+bool fused(int tokens, int K) { return tokens <= 16 && tokens * (k_frags(K) * 64 + 16) <= 32768; }
+
+template <int ACT>
+hipError_t run(const Lin8Args& a, Laid x, Laid w, hipStream_t st) {
+  const int tn = (a.N + 15) / 16;
+  if (fused(a.tokens, a.K)) {
+    hipLaunchKernelGGL((k_lin8_few<ACT, 1, true>), dim3(tn, 1), dim3(256),
+                       a.tokens * (k_frags(a.K) * 64 + 16), st, a, x, w);
+    return hipGetLastError();
+  }
+  const hipError_t e = rows8<uint16_t>(a.tokens, a.K, a.x, a.xt, x, st);
+  if (e != hipSuccess) return e;
+  if (a.tokens <= 64) {
+    if (a.tokens <= 16)
+      hipLaunchKernelGGL((k_lin8_few<ACT, 1, false>), dim3(tn, 1), dim3(256), 0, st, a, x, w);
+    else
+      hipLaunchKernelGGL((k_lin8_few<ACT, 2, false>), dim3(tn, (a.tokens + 31) / 32), dim3(256), 0,
+                         st, a, x, w);
+    return hipGetLastError();
+  }
+  const auto count = [&](int bt, int bn) {
+    return (long)((a.tokens + bt - 1) / bt) * ((a.N + bn - 1) / bn);
+  };
+  if (count(128, 256) >= 256) return tiles<Tile<128, 256, 64, 128, 3, 1>, ACT>(a, x, w, st);
+  // 64 x 64 while all of them run at once, three on a CU: 512 x 5632 x 1408 24 us
+  // against 33 with 64 x 128, 512 x 1408 x 5632 18.0 against 19.7; past that 64 x
+  // 128: 1232 x 1408 x 2816 16 against 19.6.  Two fragments along K per step: one
+  // takes 28 us instead of 24 for K of 5632, the same for K of 768 and 1408.
+  return count(64, 64) <= 768 ? tiles<Tile<64, 64, 32, 32, 3, 2>, ACT>(a, x, w, st)
+                              : tiles<Tile<64, 128, 32, 64, 3, 2>, ACT>(a, x, w, st);
+}
+
 }  // namespace
 
 size_t lin8_weight_bytes(int K, int N) { return laid_bytes(N, K); }
-size_t lin8_ws_bytes(int tokens, int K, int) { return tokens ? laid_bytes(tokens, K) : 0; }
+size_t lin8_ws_bytes(int tokens, int K, int) { return fused(tokens, K) ? 0 : laid_bytes(tokens, K); }
 
 hipError_t launch_lin8_pack(int K, int N, const void* w, int w_dtype, void* weights,
                             hipStream_t st) {
@@ -335,8 +470,6 @@ hipError_t launch_lin8_pack(int K, int N, const void* w, int w_dtype, void* weig
 hipError_t launch_lin8(const Lin8Args& a, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
   const Laid x = laid(a.ws, a.tokens), w = laid(a.weights, a.N);
-  const hipError_t e = rows8<uint16_t>(a.tokens, a.K, a.x, a.xt, x, st);
-  if (e != hipSuccess) return e;
   switch (a.act) {
     case PULSE_ACT_GELU: return run<PULSE_ACT_GELU>(a, x, w, st);
     case PULSE_ACT_SILU: return run<PULSE_ACT_SILU>(a, x, w, st);

@@ -27,6 +27,7 @@ from __future__ import annotations
 import bisect
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -143,6 +144,8 @@ def lib():
         rp, sz, nd = ctypes.POINTER(Rows), ctypes.c_size_t, ctypes.POINTER(NormDesc)
         pp, gp = ctypes.POINTER(NormParams), ctypes.POINTER(NormGrads)
         kd, ld = ctypes.POINTER(KeepDesc), ctypes.POINTER(Lin8Desc)
+        global _fast
+        _fast = {}
         for name, args in (
                 ("norm_sizes", [nd, _i32, _szp]),
                 ("norm_forward", [nd, _i32, rp, rp, pp, rp, rp, _vp]),
@@ -158,8 +161,20 @@ def lib():
                 ("lin8_forward", [ld, _i32, rp, _vp, sz, _vp, rp, _vp, sz, _vp])):
             fn = getattr(L, "pulse_" + name)
             fn.argtypes, fn.restype = args, st
+            # the same entry for structures that come as bytes or addresses: packing
+            # takes a third of the time of building one
+            fn = L["pulse_" + name]
+            fn.argtypes = [a if a in (_i32, sz, _szp) else _vp for a in args]
+            fn.restype = st
+            _fast[name] = fn
         _bound = L
     return _bound
+
+
+_fast = {}
+_pack_rows = struct.Struct("=qq").pack
+_pack_params = struct.Struct("=qqqqqqqqqq").pack
+_pack_grads = struct.Struct("=qqqqqq").pack
 
 
 def _bad(msg):
@@ -188,7 +203,8 @@ def _heads(t, name, shape, dtype, dev):
 
 
 def _rows(t, name, shape, dtype, dev):
-    """The view [tokens, channels] `t` of GPU `dev`, where the call runs."""
+    """The view [tokens, channels] `t` of GPU `dev`, where the call runs, as the
+    bytes of a Rows."""
     if t.dtype is not dtype or t.shape != shape:
         _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
     s0, s1 = t.stride()
@@ -196,7 +212,7 @@ def _rows(t, name, shape, dtype, dev):
         _bad(f"{name}: the channels of a row must be contiguous")
     if t.get_device() != dev:
         _bad(f"{name} is on {t.device}, not on the current GPU")
-    return Rows(t.data_ptr(), s0 if shape[0] > 1 else 0)
+    return _pack_rows(t.data_ptr(), s0 if shape[0] > 1 else 0)
 
 
 def _flat(t, name, n, dtype, dev):
@@ -223,11 +239,14 @@ def _by_hand(*inputs):
 _grad_on = torch.is_grad_enabled
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _here():
     """The current GPU and the handle of its current stream.  A call given a
     `stream` makes it current and calls itself, so that what it allocates
     belongs to the stream it runs on."""
-    dev = torch.cuda.current_device()
+    dev = _device()
     return dev, _raw_stream(dev)
 
 
@@ -619,27 +638,30 @@ class Norm:
                              residual_scale, _dtype(self.dtype), _dtype(self.stream_dtype))
         n = ctypes.c_size_t()
         _check(lib().pulse_norm_sizes(self.desc, 0, n))
-        self.sizes = {0: n.value}
+        self.at, self.sizes = ctypes.addressof(self.desc), {0: n.value}
+        self.cond_shape = (docs, channels)
 
     def _cond(self, t, name, dev):
         if t is None:
-            return None, 0
-        if t.dtype is not torch.float32 or t.shape != (self.docs, self.channels) or \
-                t.stride(1) != 1:
-            _bad(f"{name} must be fp32 [{self.docs}, {self.channels}] with contiguous rows, not "
+            return 0, 0
+        s0, s1 = t.stride() if t.dim() == 2 else (0, 0)
+        if t.dtype is not torch.float32 or t.shape != self.cond_shape or s1 != 1:
+            _bad(f"{name} must be fp32 {list(self.cond_shape)} with contiguous rows, not "
                  f"{t.dtype} {tuple(t.shape)}")
         if t.get_device() != dev:
             _bad(f"{name} is on {t.device}, not on the current GPU")
-        return t.data_ptr(), t.stride(0)
+        return t.data_ptr(), s0
 
     def _params(self, offsets, gate, scale, shift, weight, bias, post_weight, dev):
+        """The bytes of a NormParams."""
         (g, gs), (s, ss), (f, fs) = (self._cond(gate, "gate", dev), self._cond(scale, "scale", dev),
                                      self._cond(shift, "shift", dev))
         c, f32 = self.channels, torch.float32
-        return NormParams(_flat(offsets, "offsets", self.docs + 1, torch.int32, dev), g, s, f, gs,
-                          ss, fs, _flat(weight, "weight", c, f32, dev),
-                          _flat(bias, "bias", c, f32, dev),
-                          _flat(post_weight, "post_weight", c, f32, dev))
+        return _pack_params(
+            _flat(offsets, "offsets", self.docs + 1, torch.int32, dev) or 0, g, s, f, gs, ss, fs,
+            0 if weight is None else _flat(weight, "weight", c, f32, dev),
+            0 if bias is None else _flat(bias, "bias", c, f32, dev),
+            0 if post_weight is None else _flat(post_weight, "post_weight", c, f32, dev))
 
     def _branch(self, y):
         if (y is not None) != self.branch:
@@ -650,7 +672,8 @@ class Norm:
         """(h, u), written into the tensors of ``out`` if given (h may be x's own
         memory, u may be y's).  h is x without a branch, u is None without
         ``pre``."""
-        if _grad_on():
+        if _grad_on() and any(t is not None and t.requires_grad for t in
+                              (x, y, gate, scale, shift, weight, bias, post_weight)):
             _by_hand(("x", x), ("y", y), ("gate", gate), ("scale", scale), ("shift", shift),
                      ("weight", weight), ("bias", bias), ("post_weight", post_weight))
         if stream is not None:
@@ -669,8 +692,8 @@ class Norm:
             u = None
         elif u is None:
             u = torch.empty(shape, dtype=self.dtype, device=x.device)
-        _check(lib().pulse_norm_forward(
-            self.desc, shape[0], _rows(x, "x", shape, self.stream_dtype, dev),
+        _check(_fast["norm_forward"](
+            self.at, shape[0], _rows(x, "x", shape, self.stream_dtype, dev),
             _rows(y, "y", shape, self.dtype, dev) if self.branch else None,
             self._params(offsets, gate, scale, shift, weight, bias, post_weight, dev),
             _rows(h, "h", shape, self.stream_dtype, dev) if self.branch else None,
@@ -719,9 +742,10 @@ class Norm:
         for name, size, dt in wanted:
             if res.get(name) is None:
                 res[name] = torch.empty(size, dtype=dt, device=device)
-        grads = NormGrads(*[_flat(res.get(k), k, (self.docs * c if k in ("dgate", "dscale", "dshift")
-                                                  else c), f32, dev)
-                            for k, _ in NormGrads._fields_])
+        grads = _pack_grads(*[
+            0 if res.get(k) is None else
+            _flat(res[k], k, self.docs * c if k in ("dgate", "dscale", "dshift") else c, f32, dev)
+            for k, _ in NormGrads._fields_])
         need = self.sizes.get(n)
         if need is None:
             b = ctypes.c_size_t()
@@ -729,8 +753,8 @@ class Norm:
             need = self.sizes[n] = b.value
         ws = _bytes_at(need, device)
         st, dt = self.stream_dtype, self.dtype
-        _check(lib().pulse_norm_backward(
-            self.desc, n, None if du is None else _rows(du, "du", shape, dt, dev),
+        _check(_fast["norm_backward"](
+            self.at, n, None if du is None else _rows(du, "du", shape, dt, dev),
             None if dh is None else _rows(dh, "dh", shape, st, dev),
             None if h is None else _rows(h, "h", shape, st, dev),
             _rows(y, "y", shape, dt, dev) if self.branch else None,
@@ -765,7 +789,7 @@ class Checkpoint:
         self.dtype = torch.bfloat16 if dtype is None else dtype
         self.channels, self.act = channels, act
         self.desc = KeepDesc(channels, _choice(act, _ACTS, "act"), _dtype(self.dtype))
-        self.sizes = {}
+        self.at, self.sizes = ctypes.addressof(self.desc), {}
         _check(lib().pulse_keep_sizes(self.desc, 0, ctypes.c_size_t()))
 
     def buffer(self, tokens, device="cuda"):
@@ -786,7 +810,7 @@ class Checkpoint:
     def save(self, x, out=None, kept=None, stream=None):
         """Keep x (into ``kept`` of an earlier call, if given), and write act(x)
         into ``out``, if given (it may be x); returns what is kept."""
-        if _grad_on():
+        if x.requires_grad and _grad_on():
             _by_hand(("x", x))
         if stream is not None:
             with torch.cuda.stream(stream):
@@ -796,8 +820,8 @@ class Checkpoint:
         shape = (n, self.channels)
         if kept is None:
             kept = Kept(n, self.channels, x.device)
-        _check(lib().pulse_keep_save(
-            self.desc, n, _rows(x, "x", shape, self.dtype, dev),
+        _check(_fast["keep_save"](
+            self.at, n, _rows(x, "x", shape, self.dtype, dev),
             None if out is None else _rows(out, "out", shape, self.dtype, dev),
             *self._kept(kept, "kept", n, dev, s, False), s))
         kept.full = True
@@ -824,15 +848,15 @@ class Checkpoint:
         at = self._kept(kept, "kept", None, dev, s, True)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=kept.buffer.device)
-        _check(lib().pulse_keep_load(self.desc, kept.tokens, *at,
-                                     _rows(out, "out", shape, self.dtype, dev), s))
+        _check(_fast["keep_load"](self.at, kept.tokens, *at,
+                                  _rows(out, "out", shape, self.dtype, dev), s))
         return out
 
     def backward(self, da, kept, out=None, again=None, stream=None):
         """The gradient of x from that of act(x), at x as kept (``out`` may be
         da).  ``again``: receives act(x) of x as kept, in 8 bits, for the next
         layer's weight gradient."""
-        if _grad_on():
+        if da.requires_grad and _grad_on():
             _by_hand(("da", da))
         if stream is not None:
             with torch.cuda.stream(stream):
@@ -842,8 +866,8 @@ class Checkpoint:
         shape = (n, self.channels)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=da.device)
-        _check(lib().pulse_keep_backward(
-            self.desc, n, _rows(da, "da", shape, self.dtype, dev),
+        _check(_fast["keep_backward"](
+            self.at, n, _rows(da, "da", shape, self.dtype, dev),
             *self._kept(kept, "kept", n, dev, s, True),
             _rows(out, "out", shape, self.dtype, dev),
             *((None, 0) if again is None else self._kept(again, "again", n, dev, s, False)), s))
@@ -856,7 +880,7 @@ class Checkpoint:
         for a linear layer whose output's gradient is dy (bf16 [tokens, outputs]);
         ``bias_out`` receives dy's sums over tokens.  ``accumulate``: add to what
         ``out`` and ``bias_out`` hold."""
-        if _grad_on():
+        if dy.requires_grad and _grad_on():
             _by_hand(("dy", dy))
         if stream is not None:
             with torch.cuda.stream(stream):
@@ -876,8 +900,8 @@ class Checkpoint:
             _check(lib().pulse_keep_wgrad_sizes(self.desc, n, m, b))
             need = self.sizes[n, m] = b.value
         ws = _bytes_at(need, dy.device)
-        _check(lib().pulse_keep_wgrad(
-            self.desc, n, m, _rows(dy, "dy", (n, m), torch.bfloat16, dev),
+        _check(_fast["keep_wgrad"](
+            self.at, n, m, _rows(dy, "dy", (n, m), torch.bfloat16, dev),
             *self._kept(kept, "kept", n, dev, s, True),
             _flat(out, "out", m * self.channels, f32, dev),
             _flat(bias_out, "bias_out", m, f32, dev), 1 if accumulate else 0, ws.data_ptr(), need,
@@ -899,7 +923,7 @@ class Linear8:
         self.desc = Lin8Desc(self.inputs, self.outputs, _choice(act, _ACTS, "act"), BF16)
         n = ctypes.c_size_t()
         _check(lib().pulse_lin8_sizes(self.desc, 0, n, None))
-        self.bytes, self.sizes = n.value, {}
+        self.at, self.bytes, self.sizes = ctypes.addressof(self.desc), n.value, {}
         self.weights = _bytes_at(n.value, weight.device)
         self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
         self.update(weight, bias)
@@ -946,9 +970,9 @@ class Linear8:
             b = ctypes.c_size_t()
             _check(lib().pulse_lin8_sizes(self.desc, n, None, b))
             need = self.sizes[n] = b.value
-        ws = _bytes_at(need, x.device)
-        _check(lib().pulse_lin8_forward(
-            self.desc, n, _rows(x, "x", (n, self.inputs), bf, dev), self._weights(dev, s),
+        ws = _bytes_at(need, x.device) if need else None
+        _check(_fast["lin8_forward"](
+            self.at, n, _rows(x, "x", (n, self.inputs), bf, dev), self._weights(dev, s),
             self.bytes, self.bias_ptr, _rows(out, "out", (n, self.outputs), bf, dev),
-            ws.data_ptr(), need, s))
+            ws.data_ptr() if need else None, need, s))
         return out
