@@ -720,11 +720,10 @@ Plan plan_of(int tokens, int C, int N) {
   return p;
 }
 
-hipError_t run(const KgradArgs& a, const Plan& p, hipStream_t st) {
+hipError_t run(const KgradArgs& a, const Plan& p, const uint8_t* q, const uint8_t* e,
+               hipStream_t st) {
   using Small = Tile<64, 64, 32, 32>;
   using W = Wide<128, 2>;
-  const uint8_t* q = static_cast<const uint8_t*>(a.kept);
-  const uint8_t* e = q + keep_exps_at(a.C, a.tokens);
   if (!p.large) {
     auto kern = a.db ? k_kgrad<Small, true> : k_kgrad<Small, false>;
     hipLaunchKernelGGL(kern, dim3(p.s.tiles * p.s.splits), dim3(Small::NT), 0, st, a, p.s, q, e);
@@ -745,26 +744,48 @@ hipError_t clear(float* p, long n, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Tokens at a time: their fragments take at most 512 MB.
+int chunk_of(int tokens, int C) {
+  const long most = (INT64_C(1) << 28) / ((C + WIDE_C - 1) / WIDE_C * WIDE_C) / BK * BK;
+  return tokens < most ? tokens : (int)most;
+}
+
 }  // namespace
 
-size_t kgrad_bytes(int tokens, int C, int N) { return plan_of(tokens, C, N).bytes; }
+size_t kgrad_bytes(int tokens, int C, int N) {
+  if (tokens == 0) return 0;
+  const int chunk = chunk_of(tokens, C), rest = tokens % chunk;
+  const size_t a = plan_of(chunk, C, N).bytes, b = rest ? plan_of(rest, C, N).bytes : 0;
+  return a > b ? a : b;
+}
 
-hipError_t launch_kgrad(const KgradArgs& a, hipStream_t st) {
-  if (a.tokens == 0) {
-    if (a.accumulate) return hipSuccess;
-    const hipError_t e = clear(a.dw, (long)a.N * a.C, st);
-    return e != hipSuccess || !a.db ? e : clear(a.db, a.N, st);
+hipError_t launch_kgrad(const KgradArgs& args, hipStream_t st) {
+  if (args.tokens == 0) {
+    if (args.accumulate) return hipSuccess;
+    const hipError_t e = clear(args.dw, (long)args.N * args.C, st);
+    return e != hipSuccess || !args.db ? e : clear(args.db, args.N, st);
   }
-  Plan p = plan_of(a.tokens, a.C, a.N);
-  p.s.part = a.ws;
-  p.s.bias = a.ws + (p.s.splits > 1 ? (size_t)p.s.splits * a.N * a.C : 0);
-  hipError_t e = run(a, p, st);
-  if (e != hipSuccess) return e;
-  const int wblocks = p.s.splits > 1 ? (int)(((long)a.N * a.C / 4 + 255) / 256) : 0;
-  const int blocks = wblocks + (a.db ? (a.N + 63) / 64 : 0);
-  if (!blocks) return hipSuccess;
-  hipLaunchKernelGGL(k_kgrad_sum, dim3(blocks), dim3(256), 0, st, a, p.s, wblocks);
-  return hipGetLastError();
+  const uint8_t* q = static_cast<const uint8_t*>(args.kept);
+  const uint8_t* e = q + keep_exps_at(args.C, args.tokens);
+  const int chunk = chunk_of(args.tokens, args.C);
+  for (int t = 0; t < args.tokens; t += chunk) {
+    KgradArgs a = args;
+    a.tokens = args.tokens - t < chunk ? args.tokens - t : chunk;
+    a.dy = static_cast<const uint16_t*>(args.dy) + t * args.dyt;
+    if (t) a.accumulate = 1;
+    Plan p = plan_of(a.tokens, a.C, a.N);
+    p.s.part = a.ws;
+    p.s.bias = a.ws + (p.s.splits > 1 ? (size_t)p.s.splits * a.N * a.C : 0);
+    hipError_t err = run(a, p, q + t * keep_pitch(a.C), e + t * keep_exp_pitch(a.C), st);
+    if (err != hipSuccess) return err;
+    const int wblocks = p.s.splits > 1 ? (int)(((long)a.N * a.C / 4 + 255) / 256) : 0;
+    const int blocks = wblocks + (a.db ? (a.N + 63) / 64 : 0);
+    if (!blocks) continue;
+    hipLaunchKernelGGL(k_kgrad_sum, dim3(blocks), dim3(256), 0, st, a, p.s, wblocks);
+    err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 }  // namespace pulse

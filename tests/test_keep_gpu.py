@@ -201,6 +201,13 @@ def test_weight_grad_of_many(tokens, channels, outputs, bias):
     _wgrad(tokens, channels, outputs, bias=bias, accumulate=True)
 
 
+def test_weight_grad_in_parts():
+    """Tokens whose fragments would take more than 512 MB are taken in parts: 2^28 /
+    65536 channels = 4096 at a time, here two of them and 100 tokens."""
+    _wgrad(8292, 65536, 8)
+    _wgrad(4196, 65536, 136, accumulate=True)
+
+
 def test_weight_grad_without_tokens():
     plan = ops.Checkpoint(40)
     kept = plan.save(torch.empty(0, 40, dtype=BF, device="cuda"))

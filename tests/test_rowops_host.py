@@ -208,16 +208,18 @@ def test_weight_grad_shapes():
 
 
 def test_weight_grad_workspace_over_shapes():
-    """Partial gradients take less than 1 GB whatever the sizes: there are
-    splits only while their tiles do not fill the GPU, at most 512 tiles of 64 x 64
-    or 256 of 256 x 128 (fp32), and the columns' sums beside them."""
+    """The workspace stays bounded whatever the sizes.  There are splits only
+    while their tiles do not fill the GPU: fp32 partial gradients of at most 512
+    tiles of 128 x 128, 32 MB, and the columns' sums beside them (65536 outputs of 512
+    splits or channel tiles: 128 MB).  Fragments of x take at most 512 MB, since
+    more tokens are taken in parts."""
     rng = random.Random(3)
     n = ctypes.c_size_t()
     for _ in range(3000):
         c, m = (8 * int(2 ** rng.uniform(0, 13)) for _ in range(2))
         t = int(2 ** rng.uniform(0, 23))
         assert ops.lib().pulse_keep_wgrad_sizes(ops.KeepDesc(c, 0, S.BF16), t, m, n) == S.OK
-        assert n.value <= 1 << 30, (c, m, t, n.value)
+        assert n.value <= 700 << 20, (c, m, t, n.value)
 
 
 # ---- 8-bit linear layers -------------------------------------------------------------
