@@ -19,38 +19,28 @@ __host__ __device__ inline long pad_to(long v, long m) { return (v + m - 1) / m 
 // pairs
 __host__ __device__ inline int k_frags(int K) { return (int)(pad_to(K, 128) / 64); }
 
-// A scale m 2^e, 0.5 <= m < 1: a sum times two of them passes fp32's range only
-// where the result does.
-struct Scale {
-  float m;
-  int e;
-};
-// a laid-out operand: the scales of its padded rows, then [rows / 16][k / 64]
+// a laid-out operand: fp32 scales of its padded rows, then [rows / 16][k / 64]
 // fragments
 struct Laid {
-  const Scale* scale;
+  const float* scale;
   const char* frag;
 };
 __host__ __device__ inline Laid laid(const void* p, int rows) {
   const char* c = static_cast<const char*>(p);
-  return Laid{reinterpret_cast<const Scale*>(c), c + pad_to(rows, ROWS) * sizeof(Scale)};
+  return Laid{reinterpret_cast<const float*>(c), c + pad_to(rows, ROWS) * 4};
 }
 size_t laid_bytes(int rows, int K) {
-  return (size_t)pad_to(rows, ROWS) * sizeof(Scale) + (size_t)pad_to(rows, ROWS) * k_frags(K) * 64;
+  return (size_t)pad_to(rows, ROWS) * 4 + (size_t)pad_to(rows, ROWS) * k_frags(K) * 64;
 }
 
 // What a row's largest value gives: the factor of its values, and its scale.
 struct Turn {
-  float r;
-  Scale s;
+  float r, s;
 };
 __device__ __forceinline__ Turn turn_of(uint32_t m) {
   const float top = fmaxf(__uint_as_float(m), 0x1p-100f);
   const bool bad = m >= 0x7f800000u;
-  const float s = top / 127.f;  // at least 2^-107: never denormal
-  return Turn{bad ? 0.f : 127.f / top,
-              Scale{bad ? __uint_as_float(0x7fc00000u) : __builtin_amdgcn_frexp_mantf(s),
-                    bad ? 0 : __builtin_amdgcn_frexp_expf(s)}};
+  return Turn{bad ? 0.f : 127.f / top, bad ? __uint_as_float(0x7fc00000u) : top / 127.f};
 }
 
 template <typename T>
@@ -91,7 +81,7 @@ __device__ __forceinline__ uint2 bytes8(const Vec8<T>& v, float r) {
 // meet in one L2.  Rows of up to 512 NV values stay in registers between the
 // search for the largest and the bytes.
 template <typename T, int NV>
-__global__ __launch_bounds__(1024) void k_rows8(int rows, int K, const T* x, long xt, Scale* scale,
+__global__ __launch_bounds__(1024) void k_rows8(int rows, int K, const T* x, long xt, float* scale,
                                                 char* frag) {
   const int row = blockIdx.x * 16 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int KS = k_frags(K);
@@ -132,27 +122,38 @@ __global__ __launch_bounds__(1024) void k_rows8(int rows, int K, const T* x, lon
 
 // What four outputs share: their scales and biases.
 struct Outs {
-  float m[4], b[4];
-  int e[4];
-  __device__ __forceinline__ void load(const Lin8Args& a, const Scale* sw, int n) {
-    const int4* pw = reinterpret_cast<const int4*>(sw + n);
-    const int4 w0 = pw[0], w1 = pw[1];
-    m[0] = __int_as_float(w0.x), m[1] = __int_as_float(w0.z);
-    m[2] = __int_as_float(w1.x), m[3] = __int_as_float(w1.z);
-    e[0] = w0.y, e[1] = w0.w, e[2] = w1.y, e[3] = w1.w;
+  float s[4], b[4];
+  __device__ __forceinline__ void load(const Lin8Args& a, const float* sw, int n) {
+    const float4 w = *reinterpret_cast<const float4*>(sw + n);
+    s[0] = w.x, s[1] = w.y, s[2] = w.z, s[3] = w.w;
     const float4 v = a.bias ? *reinterpret_cast<const float4*>(a.bias + n)
                             : make_float4(0.f, 0.f, 0.f, 0.f);
     b[0] = v.x, b[1] = v.y, b[2] = v.z, b[3] = v.w;
   }
 };
+// a sum of less than 2^31 times two such scales stays within fp32's range
+__device__ __forceinline__ bool plain(float s) { return s >= 0x1p-40f && s <= 0x1p40f; }
+__device__ __forceinline__ bool plain(const Outs& o) {
+  return plain(o.s[0]) && plain(o.s[1]) && plain(o.s[2]) && plain(o.s[3]);
+}
 
-// four outputs of a row
-template <int ACT>
-__device__ __forceinline__ uint2 out4(i32x4_t acc, Scale sx, const Outs& o) {
+// Four outputs of a row.  Scales that are not plain are multiplied apart from
+// their powers of two, so that a product passes fp32's range only where the
+// result does; the roundings, and so the bits, are the same.
+template <int ACT, bool PLAIN>
+__device__ __forceinline__ uint2 out4(i32x4_t acc, float sx, const Outs& o) {
+#pragma clang fp contract(off)
   float v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i] = act_f<ACT>(ldexpf((float)acc[i] * sx.m * o.m[i], sx.e + o.e[i]) + o.b[i]);
+  for (int i = 0; i < 4; ++i) {
+    float z = (float)acc[i];
+    if constexpr (PLAIN)
+      z = z * sx * o.s[i];
+    else
+      z = ldexpf(z * __builtin_amdgcn_frexp_mantf(sx) * __builtin_amdgcn_frexp_mantf(o.s[i]),
+                 __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(o.s[i]));
+    v[i] = act_f<ACT>(z + o.b[i]);
+  }
   return uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
@@ -164,7 +165,7 @@ template <int ACT, int TT, bool FUSED>
 __global__ __launch_bounds__(256) void k_lin8_few(Lin8Args a, Laid x, Laid w) {
   extern __shared__ __attribute__((aligned(16))) char rows[];  // FUSED: [tokens][pitch]
   __shared__ i32x4_t part[4][TT][64];
-  __shared__ Scale scales[16];
+  __shared__ float scales[16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int KS = k_frags(a.K);
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(256) void k_lin8_few(Lin8Args a, Laid x, Laid w) {
       Outs o;
       o.load(a, w.scale, n);
       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.yt + n) =
-          out4<ACT>(s, FUSED ? scales[t] : x.scale[t], o);
+          out4<ACT, false>(s, FUSED ? scales[t] : x.scale[t], o);
     }
   }
 }
@@ -382,19 +383,30 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
   char* out = smem + wave * C::OUT;
   const long t0 = (long)tt * C::BT + wt * C::WT;
   const int n0 = tn * C::BN + wn * C::WN;
-  Scale sx[C::TT];
+  float sx[C::TT];
+  bool ok = true;
 #pragma unroll
-  for (int i = 0; i < C::TT; ++i) sx[i] = x.scale[t0 + i * 16 + (lane & 15)];
+  for (int i = 0; i < C::TT; ++i) {
+    sx[i] = x.scale[t0 + i * 16 + (lane & 15)];
+    ok = ok && (plain(sx[i]) || t0 + i * 16 + (lane & 15) >= a.tokens);
+  }
+  ok = __all(ok);
 #pragma unroll
   for (int j = 0; j < C::TN; ++j) {
     const int n = j * 16 + 4 * (lane >> 4);
     if (n0 + n >= a.N) continue;
     Outs o;
     o.load(a, w.scale, n0 + n);
+    const auto put = [&](auto tag) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < C::TT; ++i)
-      *reinterpret_cast<uint2*>(out + (i * 16 + (lane & 15)) * C::PY + n * 2) =
-          out4<ACT>(acc[j][i], sx[i], o);
+      for (int i = 0; i < C::TT; ++i)
+        *reinterpret_cast<uint2*>(out + (i * 16 + (lane & 15)) * C::PY + n * 2) =
+            out4<ACT, decltype(tag)::value>(acc[j][i], sx[i], o);
+    };
+    if (ok && __all(plain(o)))
+      put(std::true_type());
+    else
+      put(std::false_type());
   }
   lgkm_wait0();
 #pragma unroll 4
@@ -428,7 +440,7 @@ hipError_t rows8(int rows, int K, const void* x, long xt, Laid to, hipStream_t s
               : K <= 2048 ? k_rows8<T, 4>
                           : k_rows8<T, 6>;
   hipLaunchKernelGGL(kern, dim3(pad_to(rows, 16) / 16), dim3(1024), 0, st, rows, K,
-                     static_cast<const T*>(x), xt, const_cast<Scale*>(to.scale),
+                     static_cast<const T*>(x), xt, const_cast<float*>(to.scale),
                      const_cast<char*>(to.frag));
   return hipGetLastError();
 }

@@ -913,8 +913,8 @@ class Linear8:
     """y = act(x W^T + bias) in 8-bit integers, for sampling: W (fp32 or bf16
     [outputs, inputs]) is laid out once, with a scale for each output channel; a
     call lays out x (bf16 [tokens, inputs]) with a scale for each token, and
-    integer sums are exact.  ``bias``: fp32 [outputs].  After the weights change,
-    call :meth:`update`."""
+    integer sums are exact.  ``bias``: fp32 [outputs], copied.  After the weights
+    change, call :meth:`update`."""
 
     def __init__(self, weight, bias=None, act=None):
         if weight.dim() != 2:
@@ -926,10 +926,13 @@ class Linear8:
         self.at, self.bytes, self.sizes = ctypes.addressof(self.desc), n.value, {}
         self.weights = _bytes_at(n.value, weight.device)
         self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
+        self.bias, self.bias_ptr = torch.empty(self.outputs, dtype=torch.float32,
+                                               device=weight.device), None
         self.update(weight, bias)
 
     def update(self, weight, bias=None, stream=None):
-        """Lay out other weights of the same shape."""
+        """Lay out other weights of the same shape, in place: captured calls take
+        them too, where they have a bias or have none as before."""
         if _grad_on():
             _by_hand(("weight", weight), ("bias", bias))
         if stream is not None:
@@ -939,18 +942,19 @@ class Linear8:
         if tuple(weight.shape) != (self.outputs, self.inputs):
             _bad(f"weight is {tuple(weight.shape)}, expected {(self.outputs, self.inputs)}")
         at = _flat(weight, "weight", self.outputs * self.inputs, weight.dtype, dev)
-        self.bias_ptr = _flat(bias, "bias", self.outputs, torch.float32, dev)
+        _flat(bias, "bias", self.outputs, torch.float32, dev)
         _check(lib().pulse_lin8_pack(self.desc, at, _dtype(weight.dtype), self._weights(dev, s),
                                      self.bytes, s))
-        self.bias = bias
+        if bias is not None:
+            self.bias.copy_(bias)
+        self.bias_ptr = None if bias is None else self.bias.data_ptr()
 
     def _weights(self, dev, s):
         if self.weights.get_device() != dev:
             _bad(f"the weights are on {self.weights.device}, not on the current GPU")
         if s != self.home:
             _used_on(self.weights, dev)
-            if getattr(self, "bias", None) is not None:
-                _used_on(self.bias, dev)
+            _used_on(self.bias, dev)
         return self.ptr
 
     def forward(self, x, out=None, stream=None):

@@ -176,3 +176,36 @@ def test_streams_and_graph(tokens):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, layer.forward(x)), i
+
+
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_update_reaches_a_captured_call(tokens):
+    """The layer's memory stays where it is: a replay takes the weights and bias of
+    the last update, also when the caller's tensors are gone."""
+    x = _randn(1, tokens, 72).to(BF).cuda()
+    layer = ops.Linear8(_randn(2, 136, 72).cuda(), bias=_randn(3, 136).cuda())
+    layer.forward(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = layer.forward(x)
+    w, b = _randn(4, 136, 72), _randn(5, 136)
+    layer.update(w.cuda(), bias=b.cuda())
+    junk = [torch.full((136,), float("nan"), device="cuda") for _ in range(8)]
+    for _ in range(2):
+        g.replay()
+        torch.cuda.synchronize()
+        _check(got, x.cpu(), w, b, None)
+    del junk
+
+
+@pytest.mark.parametrize("tokens", [5, 70, 2100])
+def test_scales_of_any_size_give_the_same_rounding(tokens):
+    """Rows of tiny and huge scales next to ordinary ones, whose product is
+    ordinary: the bits are those of scales near 1."""
+    n = 4096 if tokens > 1000 else 64
+    x, w = _randn(1, tokens, 136).to(BF), _randn(2, n, 136).to(BF)
+    ref = ops.Linear8(w.cuda()).forward(x.cuda())
+    got = ops.Linear8((w.float() * 2.0 ** 70).to(BF).cuda()).forward(
+        (x.float() * 2.0 ** -70).to(BF).cuda())
+    assert torch.equal(got, ref)
