@@ -268,10 +268,9 @@ typedef enum { PULSE_ACT_NONE = 0, PULSE_ACT_GELU = 1, PULSE_ACT_SILU = 2 } puls
  * value rounds to at most 127; a value is kept as q = round(x 2^-e), to
  * nearest even, and stands for q 2^e, which bf16 holds exactly (at e = 121 q is
  * cut to [-127, 127]).  A group that holds a NaN or an infinity stands for
- * NaN.  Layout: [tokens][P] bytes q +
- * 128, P = C rounded up to a multiple of 32 (channels past C hold 0), then, on
- * the next multiple of 16 bytes, [tokens][E] bytes e + 126, or 255 for NaN, E =
- * P / 32 rounded up to a multiple of 4. */
+ * NaN.  Layout: [tokens][P] bytes q, P = C rounded up to a multiple of 32
+ * (channels past C hold 0), then, on the next multiple of 16 bytes, [tokens][E]
+ * bytes e + 126, or 255 for NaN, E = P / 32 rounded up to a multiple of 4. */
 typedef struct {
   int32_t channels; /* a multiple of 8, 8..65536                            */
   int32_t act;      /* pulse_act                                            */

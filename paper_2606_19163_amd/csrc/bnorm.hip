@@ -4,10 +4,10 @@
 // A row lies in the registers of the lanes that share it, 8 channels each, so
 // that every tensor is read and written once; as many waves take a row as that
 // needs, since with 24 or 32 channels a lane the sums over rows that the backward
-// pass keeps beside the row spilled (83 us instead of 43 at 8192 x 1408).  Bound
+// pass keeps beside the row spilled (83 us instead of 43 at 8192 x 1408 then).  Bound
 // by memory: 8192 x 1408 in bf16 forward 19.6 us in the kernel (92 MB, 4.7 TB/s),
-// backward 32 (139 MB, 4.3) and 7.7 for the sums over blocks; 15795 x 1280 with an
-// fp32 stream and a norm on both sides 79 (365 MB, 4.6) + 9.3 + 4.7; a copy of 2
+// backward 32 (139 MB, 4.3) and 5.0 for the sums over blocks; 15795 x 1280 with an
+// fp32 stream and a norm on both sides 79 (365 MB, 4.6) + 6.5 + 4.7; a copy of 2
 // GiB reaches 4.9 TB/s.  512 x 768 forward: 4.4 us, a chain of loads, two sums
 // and a store.
 #include "rowvec.hpp"
@@ -293,9 +293,30 @@ __global__ __launch_bounds__(ROW_THREADS<L>) void k_norm_bwd(NormArgs a, int R, 
 constexpr int SUM_C = 64, SUM_K = 16;
 using Sums = float[3][SUM_K][SUM_C];
 
-__device__ __forceinline__ void add4(float4& s, const float* p) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+// p[i] += the sums over n rows of three vectors, the first at src, the others
+// `step` floats apart, for the vectors i that are there.  Four rows at a time
+// are on their way: in turn, each would wait for memory.
+__device__ __forceinline__ void add_rows(float4 (&p)[3], const float* src, long step, int n, int C,
+                                         bool first2, bool third) {
+  constexpr int AHEAD = 4;
+  for (int r0 = 0; r0 < n; r0 += AHEAD) {
+    float4 v[AHEAD][3];
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        v[r][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r0 + r < n && (i < 2 ? first2 : third))
+          v[r][i] = *reinterpret_cast<const float4*>(src + (r0 + r) * step + (long)i * C);
+      }
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        p[i].x += v[r][i].x, p[i].y += v[r][i].y;
+        p[i].z += v[r][i].z, p[i].w += v[r][i].w;
+      }
+  }
 }
 
 // thread t < 192: the total of sum t / 64, channel t % 64
@@ -324,28 +345,23 @@ __global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads 
     const int r1 = a.off ? min(a.off[d + 1], a.tokens) : a.tokens;
     float4 p[3];
     p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
+    // what the totals are turned with, on its way beside them
+    const int c = blockIdx.x * SUM_C + threadIdx.x;
+    const bool out = threadIdx.x < SUM_C && c < a.C;
+    const float w = out && a.weight ? a.weight[c] : 1.f, b = out && a.bias ? a.bias[c] : 0.f;
+    const float s = 1.f + (out && a.scale ? a.scale[(long)d * a.scale_t + c] : 0.f);
+    const float g = a.r * (out && a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
+    const float wp = out && a.post_weight ? a.post_weight[c] : 1.f;
     if (r1 > r0 && c4 < a.C) {
-      const int last = (r1 - 1) / R;
-#pragma unroll 4
-      for (int b = r0 / R + k; b <= last; b += SUM_K) {
-        const float* src = part + ((long)b + d) * 3 * a.C + c4;
-        if (a.pre) {
-          add4(p[0], src);
-          add4(p[1], src + a.C);
-        }
-        if (a.branch) add4(p[2], src + 2 * a.C);
-      }
+      const int b0 = r0 / R + k, n = ((r1 - 1) / R - b0 + SUM_K) / SUM_K;
+      add_rows(p, part + ((long)b0 + d) * 3 * a.C + c4, (long)SUM_K * 3 * a.C, n, a.C, a.pre != 0,
+               a.branch != 0);
     }
     const float total = meet(sm, p);
     if (threadIdx.x < 3 * SUM_C) tot[threadIdx.x >> 6][threadIdx.x & 63] = total;
     __syncthreads();
-    const int c = blockIdx.x * SUM_C + threadIdx.x;
-    if (threadIdx.x < SUM_C && c < a.C) {
+    if (out) {
       const float p0 = tot[0][threadIdx.x], p1 = tot[1][threadIdx.x], p2 = tot[2][threadIdx.x];
-      const float w = a.weight ? a.weight[c] : 1.f, b = a.bias ? a.bias[c] : 0.f;
-      const float s = 1.f + (a.scale ? a.scale[(long)d * a.scale_t + c] : 0.f);
-      const float g = a.r * (a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
-      const float wp = a.post_weight ? a.post_weight[c] : 1.f;
       const long at = (long)d * a.C + c;
       if (o.dshift) o.dshift[at] = p0;
       if (o.dscale) o.dscale[at] = w * p1 + b * p0;
@@ -365,13 +381,9 @@ __global__ __launch_bounds__(256) void k_norm_weights(NormArgs a, pulse_norm_gra
   const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
   float4 p[3];
   p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (c4 < a.C)
-#pragma unroll 4
-    for (int d = k; d < a.docs; d += SUM_K) {
-      const float* src = docsum + (long)d * 3 * a.C + c4;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) add4(p[i], src + (long)i * a.C);
-    }
+  if (c4 < a.C && k < a.docs)
+    add_rows(p, docsum + (long)k * 3 * a.C + c4, (long)SUM_K * 3 * a.C,
+             (a.docs - k + SUM_K - 1) / SUM_K, a.C, true, true);
   const float total = meet(sm, p);
   const int i = threadIdx.x >> 6, c = blockIdx.x * SUM_C + (threadIdx.x & 63);
   float* dst = i == 0 ? o.dweight : i == 1 ? o.dbias : i == 2 ? o.dpost_weight : nullptr;

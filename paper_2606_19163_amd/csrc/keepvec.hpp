@@ -23,10 +23,10 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m) {
   return max(m, __float_as_uint(dpp<DPP_XOR2>(__uint_as_float(m))));
 }
 
-// round(v[0..4) inv) + 128 as four bytes, cut to [1, 255]: the sum with 1.5
+// round(v[0..4) inv) as four signed bytes, cut to [-127, 127]: the sum with 1.5
 // 2^23 rounds to a whole number, to nearest even, whose low byte is at the bottom
 __device__ __forceinline__ uint32_t bytes4(const float* v, float inv) {
-  constexpr float MAGIC = 12582912.f + 128.f;
+  constexpr float MAGIC = 12582912.f;
   uint32_t b[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -52,7 +52,7 @@ __device__ __forceinline__ float keep_step(uint32_t b) {
 
 __device__ __forceinline__ void unkeep4(float* v, uint32_t w, float step) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = ((float)((w >> (8 * i)) & 255u) - 128.f) * step;
+  for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i)) * step;
 }
 
 __device__ __forceinline__ void load8(float (&v)[8], const uint8_t* q, uint32_t b) {

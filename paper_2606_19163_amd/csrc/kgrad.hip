@@ -3,7 +3,7 @@
 // number of at most 7 bits times a power of two, which bf16 holds exactly, so
 // that products are exact and only the fp32 sums round.
 //
-// Bound by what feeds the MFMAs.  Turning a value to bf16 takes three and a half
+// Bound by what feeds the MFMAs.  Turning a value to bf16 takes two and a half
 // vector instructions, and vector and matrix instructions hardly overlap on a
 // SIMD: turned in every block that reads it (once per 64 outputs), 16384 x 1408
 // x 5632 took 300 us.  From 7 GFLOP on a launch of its own turns x once, to the
@@ -24,11 +24,8 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
-// What lanes past the last token, output or channel fetch: zeros of dy, and of x
-// with their exponent.
-__device__ __attribute__((aligned(16))) const uint32_t kgrad_zero[12] = {
-    0,           0,           0,           0, 0x80808080u, 0x80808080u,
-    0x80808080u, 0x80808080u, 0,           0, 0,           0};
+// what lanes past the last token, output or channel fetch
+__device__ __attribute__((aligned(16))) const uint32_t kgrad_zero[4] = {0, 0, 0, 0};
 
 constexpr int BK = 64;  // tokens per step
 
@@ -156,7 +153,7 @@ struct Split {
 };
 
 template <class C, bool BIAS>
-__global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uint8_t* q,
+__global__ __launch_bounds__(C::NT, 3) void k_kgrad(KgradArgs a, Split s, const uint8_t* q,
                                                  const uint8_t* e) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS];
@@ -205,14 +202,14 @@ __global__ __launch_bounds__(C::NT) void k_kgrad(KgradArgs a, Split s, const uin
     uint4 q[C::XU];
     uint32_t e[C::XU];
   };
-  const uint8_t* const pad = reinterpret_cast<const uint8_t*>(kgrad_zero) + 16;
+  const uint8_t* const pad = reinterpret_cast<const uint8_t*>(kgrad_zero);
   // steps are fetched in order
   auto fetch_x = [&](int kt, X& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < C::XU; ++u) {
       const bool ok = kt * BK + xrow[u] < len;
       x.q[u] = ld_once<uint4>(ok ? xsrc[u] : pad);
-      x.e[u] = ld_once<uint32_t>(ok ? esrc[u] : pad + 16);
+      x.e[u] = ld_once<uint32_t>(ok ? esrc[u] : pad);
       xsrc[u] += BK * P;
       esrc[u] += BK * E;
     }
@@ -415,7 +412,7 @@ __global__ __launch_bounds__(256) void k_kgrad_turn(KgradArgs a, const uint8_t* 
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int i = u * 256 + tid, r = i >> 3, k = i & 7, c = c0 + 16 * k;
-    uint4 w = uint4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+    uint4 w = uint4{0, 0, 0, 0};
     float step = 0.f;
     if (t0 + r < a.tokens && c < P) {
       w = *reinterpret_cast<const uint4*>(q + (t0 + r) * P + c);
