@@ -670,10 +670,16 @@ class Norm:
     def forward(self, x, y=None, offsets=None, gate=None, scale=None, shift=None, weight=None,
                 bias=None, post_weight=None, out=None, stream=None):
         """(h, u), written into the tensors of ``out`` if given (h may be x's own
-        memory, u may be y's).  h is x without a branch, u is None without
+        memory, u may be y's; the backward passes of this joint and of the one
+        before it read y and x).  h is x without a branch, u is None without
         ``pre``."""
-        if _grad_on() and any(t is not None and t.requires_grad for t in
-                              (x, y, gate, scale, shift, weight, bias, post_weight)):
+        if _grad_on() and (x.requires_grad or y is not None and y.requires_grad or
+                           gate is not None and gate.requires_grad or
+                           scale is not None and scale.requires_grad or
+                           shift is not None and shift.requires_grad or
+                           weight is not None and weight.requires_grad or
+                           bias is not None and bias.requires_grad or
+                           post_weight is not None and post_weight.requires_grad):
             _by_hand(("x", x), ("y", y), ("gate", gate), ("scale", scale), ("shift", shift),
                      ("weight", weight), ("bias", bias), ("post_weight", post_weight))
         if stream is not None:

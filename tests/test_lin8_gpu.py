@@ -65,14 +65,16 @@ def _case(tokens, inputs, outputs, bias=True, act=None, wtype=BF, seed=0):
 
 @pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 33, 64, 65, 129, 300])
 @pytest.mark.parametrize("inputs,outputs", [(8, 8), (24, 136), (64, 64), (72, 24), (320, 520),
-                                            (1408, 264), (2000, 16)])
+                                            (1408, 264), (2000, 16), (32000, 8)])
 def test_sizes(tokens, inputs, outputs):
     log(f"case lin8 {tokens}x{inputs}->{outputs}")
     _case(tokens, inputs, outputs)
 
 
 @pytest.mark.parametrize("tokens,inputs,outputs", [(2048, 200, 4096), (8192, 328, 1544),
-                                                   (2100, 64, 6000), (1100, 768, 2304)])
+                                                   (2100, 64, 6000), (1100, 768, 2304),
+                                                   (1300, 136, 2816), (1300, 1504, 2816),
+                                                   (300, 2048, 2056), (2300, 1104, 4096)])
 @pytest.mark.parametrize("act", [None, "gelu", "silu"])
 def test_many(tokens, inputs, outputs, act):
     log(f"case lin8 {tokens}x{inputs}->{outputs} {act}")

@@ -184,6 +184,19 @@ def test_documents(channels, tokens, off):
     Case(tokens, channels, off, post="rms").check()
 
 
+@pytest.mark.parametrize("channels", [64, 328, 1408])
+@pytest.mark.parametrize("tokens,off", [
+    (4099, [0, 1, 2, 7, 1000, 1001, 4000, 4000, 4090]), (8195, [0, 3, 5, 4097, 8191, 8194]),
+    (8200, None), (5003, list(range(5001))),
+])
+def test_many_rows(channels, tokens, off):
+    """Where a group of lanes takes several rows in order, across documents and
+    into the padding; and more documents than one look at 64 offsets finds.  Sums run
+    over up to 8200 rows, 11 in a row per block and 768 blocks: as in the rest."""
+    log(f"case norm many rows {channels} {tokens}")
+    Case(tokens, channels, off, post="rms" if channels == 328 else None).check()
+
+
 def test_no_tokens():
     c = Case(0, 64, [0, 0, 0])
     h, u = c.forward()
