@@ -322,7 +322,6 @@ __device__ __forceinline__ void add_rows(float4 (&p)[3], const float* src, long 
 // thread t < 192: the total of sum t / 64, channel t % 64
 __device__ __forceinline__ float meet(Sums& sm, const float4 (&p)[3]) {
   const int k = threadIdx.x >> 4, c = 4 * (threadIdx.x & 15);
-  __syncthreads();  // the last totals were read
 #pragma unroll
   for (int i = 0; i < 3; ++i) *reinterpret_cast<float4*>(&sm[i][k][c]) = p[i];
   __syncthreads();
@@ -333,46 +332,87 @@ __device__ __forceinline__ float meet(Sums& sm, const float4 (&p)[3]) {
   return s;
 }
 
-// Sums over a document's slots.  `docsum` [docs][3][C] receives what the
-// weights' gradients sum over documents.
+// What a document's sums p0 of du, p1 of du n and p2 of dH ny, channel c, turn
+// into.  `docsum` [docs][3][C] receives what the weights' gradients sum over
+// documents.
+struct DocOut {
+  float w, b, s, g, wp;
+  __device__ __forceinline__ void load(const NormArgs& a, int d, int c) {
+    w = a.weight ? a.weight[c] : 1.f, b = a.bias ? a.bias[c] : 0.f;
+    s = 1.f + (a.scale ? a.scale[(long)d * a.scale_t + c] : 0.f);
+    g = a.r * (a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
+    wp = a.post_weight ? a.post_weight[c] : 1.f;
+  }
+  __device__ __forceinline__ void put(const NormArgs& a, const pulse_norm_grads& o, float* docsum,
+                                      int d, int c, float p0, float p1, float p2) const {
+    const long at = (long)d * a.C + c;
+    if (o.dshift) o.dshift[at] = p0;
+    if (o.dscale) o.dscale[at] = w * p1 + b * p0;
+    if (o.dgate) o.dgate[at] = a.r * wp * p2;
+    if (docsum) {
+      docsum[(long)d * 3 * a.C + c] = s * p1;
+      docsum[(long)d * 3 * a.C + a.C + c] = s * p0;
+      docsum[(long)d * 3 * a.C + 2 * a.C + c] = g * p2;
+    }
+    if (a.docs == 1) {  // nothing to sum over documents
+      if (o.dweight) o.dweight[c] = s * p1;
+      if (o.dbias) o.dbias[c] = s * p0;
+      if (o.dpost_weight) o.dpost_weight[c] = g * p2;
+    }
+  }
+};
+
+// blocks that hold rows of document d: the first, and how many
+__device__ __forceinline__ int2 blocks_of(const NormArgs& a, int R, int d) {
+  const int r0 = a.off ? max(a.off[d], 0) : 0;
+  const int r1 = a.off ? min(a.off[d + 1], a.tokens) : a.tokens;
+  return r1 > r0 ? make_int2(r0 / R, (r1 - 1) / R - r0 / R + 1) : make_int2(0, 0);
+}
+
+// Many documents of few slots: 16 documents per block, 16 lanes of four
+// channels each.
+__global__ __launch_bounds__(256) void k_norm_many(NormArgs a, pulse_norm_grads o, int R,
+                                                   const float* part, float* docsum) {
+  const int d = blockIdx.x * SUM_K + (threadIdx.x >> 4);
+  const int c = blockIdx.y * SUM_C + 4 * (threadIdx.x & 15);
+  if (d >= a.docs || c >= a.C) return;
+  DocOut out[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i].load(a, d, c + i);
+  float4 p[3];
+  p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int2 b = blocks_of(a, R, d);
+  add_rows(p, part + ((long)b.x + d) * 3 * a.C + c, 3L * a.C, b.y, a.C, a.pre != 0,
+           a.branch != 0);
+  out[0].put(a, o, docsum, d, c, p[0].x, p[1].x, p[2].x);
+  out[1].put(a, o, docsum, d, c + 1, p[0].y, p[1].y, p[2].y);
+  out[2].put(a, o, docsum, d, c + 2, p[0].z, p[1].z, p[2].z);
+  out[3].put(a, o, docsum, d, c + 3, p[0].w, p[1].w, p[2].w);
+}
+
+// Few documents of many slots: a block per document and 64 channels.
 __global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads o, int R,
                                                    const float* part, float* docsum) {
   __shared__ __attribute__((aligned(16))) Sums sm;
   __shared__ float tot[3][SUM_C];
   const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
-  for (int d = blockIdx.y; d < a.docs; d += gridDim.y) {
-    const int r0 = a.off ? max(a.off[d], 0) : 0;
-    const int r1 = a.off ? min(a.off[d + 1], a.tokens) : a.tokens;
-    float4 p[3];
-    p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
-    // what the totals are turned with, on its way beside them
-    const int c = blockIdx.x * SUM_C + threadIdx.x;
-    const bool out = threadIdx.x < SUM_C && c < a.C;
-    const float w = out && a.weight ? a.weight[c] : 1.f, b = out && a.bias ? a.bias[c] : 0.f;
-    const float s = 1.f + (out && a.scale ? a.scale[(long)d * a.scale_t + c] : 0.f);
-    const float g = a.r * (out && a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
-    const float wp = out && a.post_weight ? a.post_weight[c] : 1.f;
-    if (r1 > r0 && c4 < a.C) {
-      const int b0 = r0 / R + k, n = ((r1 - 1) / R - b0 + SUM_K) / SUM_K;
-      add_rows(p, part + ((long)b0 + d) * 3 * a.C + c4, (long)SUM_K * 3 * a.C, n, a.C, a.pre != 0,
-               a.branch != 0);
-    }
-    const float total = meet(sm, p);
-    if (threadIdx.x < 3 * SUM_C) tot[threadIdx.x >> 6][threadIdx.x & 63] = total;
-    __syncthreads();
-    if (out) {
-      const float p0 = tot[0][threadIdx.x], p1 = tot[1][threadIdx.x], p2 = tot[2][threadIdx.x];
-      const long at = (long)d * a.C + c;
-      if (o.dshift) o.dshift[at] = p0;
-      if (o.dscale) o.dscale[at] = w * p1 + b * p0;
-      if (o.dgate) o.dgate[at] = a.r * wp * p2;
-      if (docsum) {
-        docsum[(long)d * 3 * a.C + c] = s * p1;
-        docsum[(long)d * 3 * a.C + a.C + c] = s * p0;
-        docsum[(long)d * 3 * a.C + 2 * a.C + c] = g * p2;
-      }
-    }
-  }
+  const int d = blockIdx.y;
+  float4 p[3];
+  p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
+  // what the totals are turned with, on its way beside them
+  const int c = blockIdx.x * SUM_C + threadIdx.x;
+  const bool mine = threadIdx.x < SUM_C && c < a.C;
+  DocOut out{};
+  if (mine) out.load(a, d, c);
+  const int2 b = blocks_of(a, R, d);
+  if (k < b.y && c4 < a.C)
+    add_rows(p, part + ((long)b.x + k + d) * 3 * a.C + c4, (long)SUM_K * 3 * a.C,
+             (b.y - k + SUM_K - 1) / SUM_K, a.C, a.pre != 0, a.branch != 0);
+  const float total = meet(sm, p);
+  if (threadIdx.x < 3 * SUM_C) tot[threadIdx.x >> 6][threadIdx.x & 63] = total;
+  __syncthreads();
+  if (mine)
+    out.put(a, o, docsum, d, c, tot[0][threadIdx.x], tot[1][threadIdx.x], tot[2][threadIdx.x]);
 }
 
 __global__ __launch_bounds__(256) void k_norm_weights(NormArgs a, pulse_norm_grads o,
@@ -484,12 +524,20 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
     if (e != hipSuccess) return e;
   }
   if (!part) return hipSuccess;
-  float* docsum = weights ? ws + p.slots : nullptr;
-  hipLaunchKernelGGL(k_norm_docs, dim3((a.C + 63) / 64, a.docs < 32768 ? a.docs : 32768),
-                     dim3(256), 0, st, a, o, p.R, part, docsum);
+  float* docsum = weights && a.docs > 1 ? ws + p.slots : nullptr;
+  // 16 documents to a block where they have eight slots or less on average: 20000
+  // x 2048 of 200 documents 129 us instead of 136
+  const int tiles = (a.C + SUM_C - 1) / SUM_C;
+  const bool many = a.docs * 8L >= p.nb;
+  if (many)
+    hipLaunchKernelGGL(k_norm_many, dim3((a.docs + SUM_K - 1) / SUM_K, tiles), dim3(256), 0, st, a,
+                       o, p.R, part, docsum);
+  else
+    hipLaunchKernelGGL(k_norm_docs, dim3(tiles, a.docs), dim3(256), 0, st, a, o, p.R, part,
+                       docsum);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !weights) return e;
-  hipLaunchKernelGGL(k_norm_weights, dim3((a.C + 63) / 64), dim3(256), 0, st, a, o, docsum);
+  if (e != hipSuccess || !docsum) return e;
+  hipLaunchKernelGGL(k_norm_weights, dim3(tiles), dim3(256), 0, st, a, o, docsum);
   return hipGetLastError();
 }
 

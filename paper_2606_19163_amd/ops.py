@@ -172,6 +172,7 @@ def lib():
 
 
 _fast = {}
+_NORM_GRADS = [k for k, _ in NormGrads._fields_]
 _pack_rows = struct.Struct("=qq").pack
 _pack_params = struct.Struct("=qqqqqqqqqq").pack
 _pack_grads = struct.Struct("=qqqqqq").pack
@@ -729,36 +730,43 @@ class Norm:
         if at is None:
             _bad("no gradient is given")
         dev, s = _here()
-        n, c, f32 = at.shape[0], self.channels, torch.float32
+        n, c, st, dt = at.shape[0], self.channels, self.stream_dtype, self.dtype
         shape, device = (n, c), at.device
-        res = {} if out is None else dict(out)
-        wanted = [("dx", shape, self.stream_dtype)]
+        given = {} if out is None else {k: v for k, v in out.items() if v is not None}
+        conds = [k for k, t in (("dgate", gate), ("dscale", scale), ("dshift", shift))
+                 if t is not None]
+        vectors = [k for k, t in (("dweight", weight), ("dbias", bias),
+                                  ("dpost_weight", post_weight)) if t is not None]
+        res = {"dx": given.pop("dx", None)}
+        if res["dx"] is None:
+            res["dx"] = torch.empty(shape, dtype=st, device=device)
         if self.branch:
-            wanted.append(("dy", shape, self.dtype))
-        for name, t in (("dgate", gate), ("dscale", scale), ("dshift", shift)):
-            if t is not None:
-                wanted.append((name, (self.docs, c), f32))
-        for name, t in (("dweight", weight), ("dbias", bias), ("dpost_weight", post_weight)):
-            if t is not None:
-                wanted.append((name, (c,), f32))
-        names = [w[0] for w in wanted]
-        for k in res:
-            if k not in names:
-                _bad(f"out has {k}, which this call does not compute")
-        for name, size, dt in wanted:
-            if res.get(name) is None:
-                res[name] = torch.empty(size, dtype=dt, device=device)
-        grads = _pack_grads(*[
-            0 if res.get(k) is None else
-            _flat(res[k], k, self.docs * c if k in ("dgate", "dscale", "dshift") else c, f32, dev)
-            for k, _ in NormGrads._fields_])
+            res["dy"] = given.pop("dy", None)
+            if res["dy"] is None:
+                res["dy"] = torch.empty(shape, dtype=dt, device=device)
+        ptr = dict.fromkeys(_NORM_GRADS, 0)
+        for names, size in ((conds, self.cond_shape), (vectors, (c,))):
+            new, many = [], size[0] * c if len(size) == 2 else c
+            for k in names:
+                if k in given:
+                    res[k] = given.pop(k)
+                    ptr[k] = _flat(res[k], k, many, torch.float32, dev)
+                else:
+                    res[k] = None
+                    new.append(k)
+            if new:  # one allocation
+                buf = torch.empty((len(new), *size), dtype=torch.float32, device=device)
+                base = buf.data_ptr()
+                for i, (k, t) in enumerate(zip(new, buf.unbind(0))):
+                    res[k], ptr[k] = t, base + 4 * many * i
+        if given:
+            _bad(f"out has {sorted(given)[0]}, which this call does not compute")
         need = self.sizes.get(n)
         if need is None:
             b = ctypes.c_size_t()
             _check(lib().pulse_norm_sizes(self.desc, n, b))
             need = self.sizes[n] = b.value
         ws = _bytes_at(need, device)
-        st, dt = self.stream_dtype, self.dtype
         _check(_fast["norm_backward"](
             self.at, n, None if du is None else _rows(du, "du", shape, dt, dev),
             None if dh is None else _rows(dh, "dh", shape, st, dev),
@@ -766,9 +774,9 @@ class Norm:
             _rows(y, "y", shape, dt, dev) if self.branch else None,
             self._params(offsets, gate, scale, shift, weight, bias, post_weight, dev),
             _rows(res["dx"], "dx", shape, st, dev),
-            _rows(res["dy"], "dy", shape, dt, dev) if self.branch else None, grads,
-            ws.data_ptr(), need, s))
-        return {k: res[k] for k in names}
+            _rows(res["dy"], "dy", shape, dt, dev) if self.branch else None,
+            _pack_grads(*ptr.values()), ws.data_ptr(), need, s))
+        return res
 
 
 class Kept:
