@@ -289,9 +289,10 @@ __global__ __launch_bounds__(ROW_THREADS<L>) void k_norm_bwd(NormArgs a, int R, 
 }
 
 // A block of the sums over slots and documents: 64 channels, four each of 16
-// lanes, times 16 lanes of what is summed, which meet in a fixed order.
+// lanes, times K lanes of what is summed, which meet in a fixed order.
 constexpr int SUM_C = 64, SUM_K = 16;
-using Sums = float[3][SUM_K][SUM_C];
+template <int K>
+using Sums = float[3][K][SUM_C];
 
 // p[i] += the sums over n rows of three vectors, the first at src, the others
 // `step` floats apart, for the vectors i that are there.  Four rows at a time
@@ -320,7 +321,8 @@ __device__ __forceinline__ void add_rows(float4 (&p)[3], const float* src, long 
 }
 
 // thread t < 192: the total of sum t / 64, channel t % 64
-__device__ __forceinline__ float meet(Sums& sm, const float4 (&p)[3]) {
+template <int K>
+__device__ __forceinline__ float meet(Sums<K>& sm, const float4 (&p)[3]) {
   const int k = threadIdx.x >> 4, c = 4 * (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < 3; ++i) *reinterpret_cast<float4*>(&sm[i][k][c]) = p[i];
@@ -328,7 +330,7 @@ __device__ __forceinline__ float meet(Sums& sm, const float4 (&p)[3]) {
   float s = 0.f;
   if (threadIdx.x < 3 * SUM_C)
 #pragma unroll
-    for (int j = 0; j < SUM_K; ++j) s += sm[threadIdx.x >> 6][j][threadIdx.x & 63];
+    for (int j = 0; j < K; ++j) s += sm[threadIdx.x >> 6][j][threadIdx.x & 63];
   return s;
 }
 
@@ -391,9 +393,10 @@ __global__ __launch_bounds__(256) void k_norm_many(NormArgs a, pulse_norm_grads 
 }
 
 // Few documents of many slots: a block per document and 64 channels.
-__global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads o, int R,
-                                                   const float* part, float* docsum) {
-  __shared__ __attribute__((aligned(16))) Sums sm;
+template <int K>
+__global__ __launch_bounds__(16 * K) void k_norm_docs(NormArgs a, pulse_norm_grads o, int R,
+                                                      const float* part, float* docsum) {
+  __shared__ __attribute__((aligned(16))) Sums<K> sm;
   __shared__ float tot[3][SUM_C];
   const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
   const int d = blockIdx.y;
@@ -406,9 +409,9 @@ __global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads 
   if (mine) out.load(a, d, c);
   const int2 b = blocks_of(a, R, d);
   if (k < b.y && c4 < a.C)
-    add_rows(p, part + ((long)b.x + k + d) * 3 * a.C + c4, (long)SUM_K * 3 * a.C,
-             (b.y - k + SUM_K - 1) / SUM_K, a.C, a.pre != 0, a.branch != 0);
-  const float total = meet(sm, p);
+    add_rows(p, part + ((long)b.x + k + d) * 3 * a.C + c4, (long)K * 3 * a.C,
+             (b.y - k + K - 1) / K, a.C, a.pre != 0, a.branch != 0);
+  const float total = meet<K>(sm, p);
   if (threadIdx.x < 3 * SUM_C) tot[threadIdx.x >> 6][threadIdx.x & 63] = total;
   __syncthreads();
   if (mine)
@@ -417,14 +420,14 @@ __global__ __launch_bounds__(256) void k_norm_docs(NormArgs a, pulse_norm_grads 
 
 __global__ __launch_bounds__(256) void k_norm_weights(NormArgs a, pulse_norm_grads o,
                                                       const float* docsum) {
-  __shared__ __attribute__((aligned(16))) Sums sm;
+  __shared__ __attribute__((aligned(16))) Sums<SUM_K> sm;
   const int k = threadIdx.x >> 4, c4 = blockIdx.x * SUM_C + 4 * (threadIdx.x & 15);
   float4 p[3];
   p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c4 < a.C && k < a.docs)
     add_rows(p, docsum + (long)k * 3 * a.C + c4, (long)SUM_K * 3 * a.C,
              (a.docs - k + SUM_K - 1) / SUM_K, a.C, true, true);
-  const float total = meet(sm, p);
+  const float total = meet<SUM_K>(sm, p);
   const int i = threadIdx.x >> 6, c = blockIdx.x * SUM_C + (threadIdx.x & 63);
   float* dst = i == 0 ? o.dweight : i == 1 ? o.dbias : i == 2 ? o.dpost_weight : nullptr;
   if (dst && c < a.C) dst[c] = total;
@@ -525,15 +528,19 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
   }
   if (!part) return hipSuccess;
   float* docsum = weights && a.docs > 1 ? ws + p.slots : nullptr;
-  // 16 documents to a block where they have eight slots or less on average: 20000
-  // x 2048 of 200 documents 129 us instead of 136
+  // 16 documents to a block where they have eight slots or less on average
   const int tiles = (a.C + SUM_C - 1) / SUM_C;
-  const bool many = a.docs * 8L >= p.nb;
-  if (many)
+  // (20000 x 2048 of 200 documents 129 us instead of 136), 64 lanes to a document's
+  // slots where they are more than 64 (8192 x 1408 of one document 44 us instead of
+  // 47.7)
+  if (a.docs * 8L >= p.nb)
     hipLaunchKernelGGL(k_norm_many, dim3((a.docs + SUM_K - 1) / SUM_K, tiles), dim3(256), 0, st, a,
                        o, p.R, part, docsum);
+  else if (p.nb > 64L * a.docs)
+    hipLaunchKernelGGL(k_norm_docs<64>, dim3(tiles, a.docs), dim3(1024), 0, st, a, o, p.R, part,
+                       docsum);
   else
-    hipLaunchKernelGGL(k_norm_docs, dim3(tiles, a.docs), dim3(256), 0, st, a, o, p.R, part,
+    hipLaunchKernelGGL(k_norm_docs<16>, dim3(tiles, a.docs), dim3(256), 0, st, a, o, p.R, part,
                        docsum);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !docsum) return e;
