@@ -6,8 +6,8 @@
 // needs, since with 24 or 32 channels a lane the sums over rows that the backward
 // pass keeps beside the row spilled (83 us instead of 43 at 8192 x 1408 then).  Bound
 // by memory: 8192 x 1408 in bf16 forward 19.6 us in the kernel (92 MB, 4.7 TB/s),
-// backward 32 (139 MB, 4.3) and 5.0 for the sums over blocks; 15795 x 1280 with an
-// fp32 stream and a norm on both sides 79 (365 MB, 4.6) + 6.5 + 4.7; a copy of 2
+// backward 32 (139 MB, 4.3) and 4.3 for the sums over blocks; 15795 x 1280 with an
+// fp32 stream and a norm on both sides 80 (365 MB, 4.6) + 5.1 + 4.7; a copy of 2
 // GiB reaches 4.9 TB/s.  512 x 768 forward: 4.4 us, a chain of loads, two sums
 // and a store.
 #include "rowvec.hpp"
@@ -473,7 +473,7 @@ hipError_t by_type(const NormArgs& a, F f) {
 
 // Three blocks of three waves per CU: more blocks are more partial sums to
 // write and read.  8192 x 1408: 42.7 us with 512, 43.2 with 768, 43.5 with 1024, 50.8
-// with 1536; 15795 x 1280: 96.0, 96.6, 109 and 105.
+// with 1536; 15795 x 1280: 96.0, 96.6, 109 and 105 (with slower sums over them).
 constexpr int BACK_BLOCKS = 768;
 
 struct BackPlan {
@@ -528,11 +528,10 @@ hipError_t launch_norm_bwd(const NormArgs& a, const pulse_norm_grads& o, float* 
   }
   if (!part) return hipSuccess;
   float* docsum = weights && a.docs > 1 ? ws + p.slots : nullptr;
-  // 16 documents to a block where they have eight slots or less on average
   const int tiles = (a.C + SUM_C - 1) / SUM_C;
-  // (20000 x 2048 of 200 documents 129 us instead of 136), 64 lanes to a document's
-  // slots where they are more than 64 (8192 x 1408 of one document 44 us instead of
-  // 47.7)
+  // 16 documents to a block where they have eight slots or less on average (20000
+  // x 2048 of 200 documents 129 us instead of 136), 64 lanes to a document's slots
+  // where they are more than 64 (8192 x 1408 of one document 44 us instead of 47.7)
   if (a.docs * 8L >= p.nb)
     hipLaunchKernelGGL(k_norm_many, dim3((a.docs + SUM_K - 1) / SUM_K, tiles), dim3(256), 0, st, a,
                        o, p.R, part, docsum);

@@ -5,12 +5,12 @@
 // as they are and which reads without bank conflicts.
 //
 // 8192 x 1408 x 5632: laying out x 10 us (35 MB, bound by memory), the product 80
-// (1.6 POP/s) and with GELU 94; K of 5632 at 2.1 POP/s, where torch's int8 product
+// (1.6 POP/s) and with GELU 90; K of 5632 at 2.1 POP/s, where torch's int8 product
 // reaches 2.4 at 16384^3.  Bound by the LDS-DMA, 48 KB per 2 x 128 x 256 x 64 and
-// CU, and the outputs' vector work (24 instructions each with GELU), which two
+// CU, and the outputs' vector work (two dozen instructions each with GELU), which two
 // blocks per CU overlap.  Tried: 256 x 256 tiles of eight waves (117 us instead of
-// 107 in all), fragments read a step ahead behind the MFMAs (even).  1 x 1408 x
-// 8448: 4.2 us, 12 MB of weights at 2.8 TB/s, a launch's length.
+// 107 in all then), fragments read a step ahead behind the MFMAs (even).  1 x 1408
+// x 8448: 4.2 us, 12 MB of weights at 2.8 TB/s, a launch's length.
 #include "rowvec.hpp"
 
 namespace pulse {
