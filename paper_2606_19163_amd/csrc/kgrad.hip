@@ -89,7 +89,6 @@ struct Tile {
   static constexpr int YU = Y_BYTES / (NT * 16);  // 16-byte loads per thread and step
   static constexpr int XU = BK * BC / (NT * 16);
   static constexpr int STAGES = 3, LDS = STAGES * STAGE;
-  static constexpr int LOADS = YU + 2 * XU;  // per thread and step
   static_assert(YU * NT * 16 == Y_BYTES && XU * NT * 16 == BK * BC && XU >= 1, "loads");
   static_assert(36 * PY < 65536 && Y_BYTES + 36 * PX < 65536 && LDS <= 160 * 1024, "LDS");
   static_assert(4 * 3 * (BN / 16 + 4) < 4096, "rotations stay below 4 rows of chunks");
