@@ -12,8 +12,9 @@
 // 2 x 128 x 128 x 64 and CU.  256 x 128 tiles move a quarter less, but leave one
 // block per CU: 272 against 260 us in all, 518 against 565 for 16384 x 2048 x 8192.
 // Four waves of 128 x 64 took 450: the compiler moves accumulators between
-// register files.  Below 7 GFLOP a block of 64 x 64 turns its own x: 2747 x 320 x
-// 1280 in five parts 14.5 us and 4 for their sums, ten steps of load latency.
+// register files.  Below 7 GFLOP, or with an axis of 64, a block of 64 x 64
+// turns its own x: 2747 x 320 x 1280 in five parts 16.4 us with their sums, ten
+// steps of load latency.
 #include "keepvec.hpp"
 
 namespace pulse {
@@ -662,15 +663,23 @@ __global__ __launch_bounds__(C::NT, 2) void k_kgrad_wide(KgradArgs a, Split s,
 }
 
 // Blocks below `wblocks`: four values of dw each thread, summed over the
-// splits; the others: db, 64 outputs x 4 lanes of partial sums.
+// splits; the others: db, 16 outputs x 16 partial sums of the rows. Eight loads
+// are in flight together: a load's latency, and no rate, is what bounds both.
 __global__ __launch_bounds__(256) void k_kgrad_sum(KgradArgs a, Split s, int wblocks) {
   if ((int)blockIdx.x < wblocks) {
     const long at = 4 * ((long)blockIdx.x * 256 + threadIdx.x), total = (long)a.N * a.C;
     if (at >= total) return;
     float4 v = *reinterpret_cast<const float4*>(s.part + at);
-    for (int z = 1; z < s.splits; ++z) {
-      const float4 w = *reinterpret_cast<const float4*>(s.part + z * total + at);
-      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    for (int z = 1; z < s.splits; z += 8) {
+      float4 w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = z + k < s.splits ? z + k : z;
+        w[k] = *reinterpret_cast<const float4*>(s.part + i * total + at);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (z + k < s.splits) v.x += w[k].x, v.y += w[k].y, v.z += w[k].z, v.w += w[k].w;
     }
     float4* p = reinterpret_cast<float4*>(a.dw + at);
     if (a.accumulate) {
@@ -680,16 +689,25 @@ __global__ __launch_bounds__(256) void k_kgrad_sum(KgradArgs a, Split s, int wbl
     *p = v;
     return;
   }
-  __shared__ float sm[4][64];
-  const int lane = threadIdx.x & 63, k = threadIdx.x >> 6;
-  const int n = (blockIdx.x - wblocks) * 64 + lane;
+  __shared__ float sm[16][16];
+  const int lane = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int n = (blockIdx.x - wblocks) * 16 + lane, rows = s.splits * s.tilesC;
   float v = 0.f;
   if (n < a.N)
-    for (int r = k; r < s.splits * s.tilesC; r += 4) v += s.bias[(long)r * a.N + n];
-  sm[k][lane] = v;
+    for (int r = g; r < rows; r += 128) {
+      float w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        w[k] = s.bias[(long)(r + 16 * k < rows ? r + 16 * k : r) * a.N + n];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += r + 16 * k < rows ? w[k] : 0.f;
+    }
+  sm[g][lane] = v;
   __syncthreads();
-  if (k == 0 && n < a.N) {
-    v = (sm[0][lane] + sm[1][lane]) + (sm[2][lane] + sm[3][lane]);
+  if (g == 0 && n < a.N) {
+    v = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v += sm[k][lane];
     a.db[n] = a.accumulate ? a.db[n] + v : v;
   }
 }
@@ -710,9 +728,11 @@ Plan plan_of(int tokens, int C, int N) {
   Plan p{};
   // The launch that turns x first pays from 7 GFLOP on: 16.5 against 12.7 us at
   // 512 x 768 x 2304, 28.4 against 28.3 at 2048 x 768 x 2304, 31.3 against 36.7 at
-  // 8192 x 768 x 768, 23.5 against 30.2 at 512 x 1408 x 5632.
-  p.large = (double)tokens * N * C >= 3.5e9;
-    const int bn = p.large ? 128 : 64, bc = p.large ? 128 : 64;
+  // 8192 x 768 x 768, 23.5 against 30.2 at 512 x 1408 x 5632. An axis of 64 fills
+  // half of its tile: 56 against 129 us at 20000 x 6000 x 64, 58 against 67 at
+  // 20000 x 64 x 6000.
+  p.large = (double)tokens * N * C >= 3.5e9 && N > 64 && C > 64;
+  const int bn = p.large ? 128 : 64, bc = p.large ? 128 : 64;
   p.s.tilesC = (C + bc - 1) / bc;
   p.s.tiles = (N + bn - 1) / bn * p.s.tilesC;
   const int steps = (tokens + BK - 1) / BK;
@@ -787,7 +807,7 @@ hipError_t launch_kgrad(const KgradArgs& args, hipStream_t st) {
     hipError_t err = run(a, p, q + t * keep_pitch(a.C), e + t * keep_exp_pitch(a.C), st);
     if (err != hipSuccess) return err;
     const int wblocks = p.s.splits > 1 ? (int)(((long)a.N * a.C / 4 + 255) / 256) : 0;
-    const int blocks = wblocks + (a.db ? (a.N + 63) / 64 : 0);
+    const int blocks = wblocks + (a.db ? (a.N + 15) / 16 : 0);
     if (!blocks) continue;
     hipLaunchKernelGGL(k_kgrad_sum, dim3(blocks), dim3(256), 0, st, a, p.s, wblocks);
     err = hipGetLastError();

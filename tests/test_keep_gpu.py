@@ -201,6 +201,16 @@ def test_weight_grad_of_many(tokens, channels, outputs, bias):
     _wgrad(tokens, channels, outputs, bias=bias, accumulate=True)
 
 
+@pytest.mark.parametrize("tokens,channels,outputs", [
+    (4100, 6000, 40), (9000, 64, 6008), (10000, 136, 136), (70000, 64, 64),
+])
+def test_weight_grad_of_a_narrow_axis(tokens, channels, outputs):
+    """Many partial sums of one value: more than eight of dw, more than 128 of db."""
+    log(f"case wgrad {tokens}x{channels}->{outputs}")
+    _wgrad(tokens, channels, outputs)
+    _wgrad(tokens, channels, outputs, accumulate=True)
+
+
 def test_weight_grad_in_parts():
     """Tokens whose fragments would take more than 512 MB are taken in parts: 2^28 /
     65536 channels = 4096 at a time, here two of them and 100 tokens."""
