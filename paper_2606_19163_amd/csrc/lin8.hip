@@ -482,6 +482,7 @@ hipError_t run(const Lin8Args& a, Laid x, Laid w, hipStream_t st) {
   // against 33 with 64 x 128, 512 x 1408 x 5632 18.0 against 19.7; past that 64 x
   // 128: 1232 x 1408 x 2816 16 against 19.6.  Two fragments along K per step: one
   // takes 28 us instead of 24 for K of 5632, the same for K of 768 and 1408.
+  // Eight stages where one tile is on a CU: even (128 x 5632 x 1408 24.4 and 24.8).
   return count(64, 64) <= 768 ? tiles<Tile<64, 64, 32, 32, 3, 2>, ACT>(a, x, w, st)
                               : tiles<Tile<64, 128, 32, 64, 3, 2>, ACT>(a, x, w, st);
 }
