@@ -161,8 +161,8 @@ def lib():
                 ("lin8_forward", [ld, _i32, rp, _vp, sz, _vp, rp, _vp, sz, _vp])):
             fn = getattr(L, "pulse_" + name)
             fn.argtypes, fn.restype = args, st
-            # the same entry for structures that come as bytes or addresses: packing
-            # takes a third of the time of building one
+            # the same entry for structures that come as bytes: packing takes a third
+            # of the time of building one
             fn = L["pulse_" + name]
             fn.argtypes = [a if a in (_i32, sz, _szp) else _vp for a in args]
             fn.restype = st
@@ -639,7 +639,8 @@ class Norm:
                              residual_scale, _dtype(self.dtype), _dtype(self.stream_dtype))
         n = ctypes.c_size_t()
         _check(lib().pulse_norm_sizes(self.desc, 0, n))
-        self.at, self.sizes = ctypes.addressof(self.desc), {0: n.value}
+        # its bytes, and no address: a copy of the object has its own
+        self.packed, self.sizes = bytes(self.desc), {0: n.value}
         self.cond_shape = (docs, channels)
 
     def _cond(self, t, name, dev):
@@ -700,7 +701,7 @@ class Norm:
         elif u is None:
             u = torch.empty(shape, dtype=self.dtype, device=x.device)
         _check(_fast["norm_forward"](
-            self.at, shape[0], _rows(x, "x", shape, self.stream_dtype, dev),
+            self.packed, shape[0], _rows(x, "x", shape, self.stream_dtype, dev),
             _rows(y, "y", shape, self.dtype, dev) if self.branch else None,
             self._params(offsets, gate, scale, shift, weight, bias, post_weight, dev),
             _rows(h, "h", shape, self.stream_dtype, dev) if self.branch else None,
@@ -768,7 +769,7 @@ class Norm:
             need = self.sizes[n] = b.value
         ws = _bytes_at(need, device)
         _check(_fast["norm_backward"](
-            self.at, n, None if du is None else _rows(du, "du", shape, dt, dev),
+            self.packed, n, None if du is None else _rows(du, "du", shape, dt, dev),
             None if dh is None else _rows(dh, "dh", shape, st, dev),
             None if h is None else _rows(h, "h", shape, st, dev),
             _rows(y, "y", shape, dt, dev) if self.branch else None,
@@ -803,7 +804,7 @@ class Checkpoint:
         self.dtype = torch.bfloat16 if dtype is None else dtype
         self.channels, self.act = channels, act
         self.desc = KeepDesc(channels, _choice(act, _ACTS, "act"), _dtype(self.dtype))
-        self.at, self.sizes = ctypes.addressof(self.desc), {}
+        self.packed, self.sizes = bytes(self.desc), {}
         _check(lib().pulse_keep_sizes(self.desc, 0, ctypes.c_size_t()))
 
     def buffer(self, tokens, device="cuda"):
@@ -835,7 +836,7 @@ class Checkpoint:
         if kept is None:
             kept = Kept(n, self.channels, x.device)
         _check(_fast["keep_save"](
-            self.at, n, _rows(x, "x", shape, self.dtype, dev),
+            self.packed, n, _rows(x, "x", shape, self.dtype, dev),
             None if out is None else _rows(out, "out", shape, self.dtype, dev),
             *self._kept(kept, "kept", n, dev, s, False), s))
         kept.full = True
@@ -862,7 +863,7 @@ class Checkpoint:
         at = self._kept(kept, "kept", None, dev, s, True)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=kept.buffer.device)
-        _check(_fast["keep_load"](self.at, kept.tokens, *at,
+        _check(_fast["keep_load"](self.packed, kept.tokens, *at,
                                   _rows(out, "out", shape, self.dtype, dev), s))
         return out
 
@@ -881,7 +882,7 @@ class Checkpoint:
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=da.device)
         _check(_fast["keep_backward"](
-            self.at, n, _rows(da, "da", shape, self.dtype, dev),
+            self.packed, n, _rows(da, "da", shape, self.dtype, dev),
             *self._kept(kept, "kept", n, dev, s, True),
             _rows(out, "out", shape, self.dtype, dev),
             *((None, 0) if again is None else self._kept(again, "again", n, dev, s, False)), s))
@@ -915,7 +916,7 @@ class Checkpoint:
             need = self.sizes[n, m] = b.value
         ws = _bytes_at(need, dy.device)
         _check(_fast["keep_wgrad"](
-            self.at, n, m, _rows(dy, "dy", (n, m), torch.bfloat16, dev),
+            self.packed, n, m, _rows(dy, "dy", (n, m), torch.bfloat16, dev),
             *self._kept(kept, "kept", n, dev, s, True),
             _flat(out, "out", m * self.channels, f32, dev),
             _flat(bias_out, "bias_out", m, f32, dev), 1 if accumulate else 0, ws.data_ptr(), need,
@@ -937,7 +938,7 @@ class Linear8:
         self.desc = Lin8Desc(self.inputs, self.outputs, _choice(act, _ACTS, "act"), BF16)
         n = ctypes.c_size_t()
         _check(lib().pulse_lin8_sizes(self.desc, 0, n, None))
-        self.at, self.bytes, self.sizes = ctypes.addressof(self.desc), n.value, {}
+        self.packed, self.bytes, self.sizes = bytes(self.desc), n.value, {}
         self.weights = _bytes_at(n.value, weight.device)
         self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
         self.bias, self.bias_ptr = torch.empty(self.outputs, dtype=torch.float32,
@@ -990,7 +991,7 @@ class Linear8:
             need = self.sizes[n] = b.value
         ws = _bytes_at(need, x.device) if need else None
         _check(_fast["lin8_forward"](
-            self.at, n, _rows(x, "x", (n, self.inputs), bf, dev), self._weights(dev, s),
+            self.packed, n, _rows(x, "x", (n, self.inputs), bf, dev), self._weights(dev, s),
             self.bytes, self.bias_ptr, _rows(out, "out", (n, self.outputs), bf, dev),
             ws.data_ptr() if need else None, need, s))
         return out
