@@ -20,11 +20,13 @@ call refuses inputs that require a gradient where torch records one.  Work is
 enqueued on ``stream`` (default: torch's current one), and what a call allocates
 belongs to that stream.  An object may be used from several: the caller orders
 them, and the memory that an object holds is kept until all are done with it.
+Copies (copy, deepcopy, pickle) have memory of their own.
 """
 
 from __future__ import annotations
 
 import bisect
+import copy
 import ctypes
 import math
 import struct
@@ -262,6 +264,32 @@ def _used_on(t, dev):
     t.record_stream(torch.cuda.current_stream(dev))
 
 
+class _Owner:
+    """An object that holds GPU memory (``_memory``, names of its tensors) and what
+    its calls look up there once: addresses, and the stream the memory is from.
+    Every copy, a shallow or an unpickled one too, has memory of its own and looks
+    these up again (``_locate``)."""
+
+    __slots__ = ()
+    _memory, _found = (), ("ptr", "home")
+
+    def __copy__(self):
+        return copy.deepcopy(self)
+
+    def __getstate__(self):
+        for t in (getattr(self, k) for k in self._memory):
+            # the copy reads it on the current stream
+            if t.is_cuda and _raw_stream(t.get_device()) != self.home:
+                _used_on(t, t.get_device())
+        names = getattr(self, "__dict__", None) or self.__slots__
+        return {k: getattr(self, k) for k in names if k not in self._found}
+
+    def __setstate__(self, state):
+        for k, v in state.items():
+            setattr(self, k, v)
+        self._locate()
+
+
 def rope_freqs(axis_dim, base=10000.0, device="cuda"):
     """freq[p] = base^(-2 i / n) for pair i of an axis of n channels, the axes
     one after another (fp32)."""
@@ -323,13 +351,15 @@ class Rope:
         return self._run(dout, pos, freq, out, 1, stream)
 
 
-class Mask:
+class Mask(_Owner):
     """Which of ``keys`` keys each of ``queries`` rows attends.  Beside the
     rows lies a table over them that attention reads, so :class:`Attn` takes
     a mask only once ``build`` or ``from_rows`` has filled both: after writing
     into ``rows``, call ``from_rows(mask.rows)``.  Both overwrite the mask in
     place: with several batches between forward and backward, each needs a
     mask of its own."""
+
+    _memory, _found = ("buffer",), ("ptr", "home", "rows", "inference")
 
     def __init__(self, queries, keys=None, docs=0, causal=False, device="cuda"):
         self.queries, self.keys = queries, queries if keys is None else keys
@@ -339,11 +369,24 @@ class Mask:
         _check(lib().pulse_mask_sizes(ctypes.byref(self.desc), ctypes.byref(n)))
         self.bytes = n.value
         self.buffer = torch.empty(max(n.value // 4, 4), dtype=torch.int32, device=device)
+        self.stamp, self.serial = None, 0
+        self._locate()
+
+    def _locate(self):
         self.ptr, self.home = self.buffer.data_ptr(), _home(self.buffer)
         #: [queries, 4]: lo, hi, pos, doc of every row
-        self.rows = self.buffer[:4 * queries].view(queries, 4)
+        self.rows = self.buffer[:4 * self.queries].view(self.queries, 4)
         self.inference = self.buffer.is_inference()
-        self.stamp, self.serial = None, 0
+
+    def __getstate__(self):
+        # the stamp is of this buffer's version: whether it holds is what a copy keeps
+        stamp = self.stamp if self.stamp is None else self.stamp == self._stamp()
+        return {**super().__getstate__(), "stamp": stamp}
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        if self.stamp is not None:
+            self.stamp = self._stamp() if self.stamp else -1
 
     def _stamp(self):
         """Changes with every torch operation that writes the rows."""
@@ -394,22 +437,34 @@ class Mask:
         return self.rows
 
 
-class Saved:
+class Saved(_Owner):
     """What a forward leaves for its backward beside the output: the scores'
     log sum exp (``lse``, fp32 [heads, queries]), what the rounding of the
     output left out, and which mask it ran under."""
 
     __slots__ = ("buffer", "shape", "lse_ptr", "low_ptr", "home", "mask", "serial")
+    _memory, _found = ("buffer",), ("lse_ptr", "low_ptr", "home")
 
     def __init__(self, heads, queries, head_dim, device, home=None):
         n = -(-heads * queries // 4) * 4  # the second part is 16-byte aligned
         self.buffer = torch.empty(n + heads * queries * head_dim // 2, dtype=torch.float32,
                                   device=device)
         self.shape = (heads, queries, head_dim)
-        self.lse_ptr = self.buffer.data_ptr()
-        self.low_ptr = self.lse_ptr + 4 * n
-        self.home = _home(self.buffer) if home is None else home
         self.mask, self.serial = None, 0
+        self._locate(home)
+
+    def _locate(self, home=None):
+        heads, queries, _ = self.shape
+        self.lse_ptr = self.buffer.data_ptr()
+        self.low_ptr = self.lse_ptr + 4 * (-(-heads * queries // 4) * 4)
+        self.home = _home(self.buffer) if home is None else home
+
+    def __deepcopy__(self, memo):
+        # it ran under that mask still, but where the mask is copied along
+        new, state = Saved.__new__(Saved), self.__getstate__()
+        memo[id(self)], mask = new, state.pop("mask")
+        new.__setstate__({**copy.deepcopy(state, memo), "mask": memo.get(id(mask), mask)})
+        return new
 
     @property
     def lse(self):
@@ -780,17 +835,21 @@ class Norm:
         return res
 
 
-class Kept:
+class Kept(_Owner):
     """Rows of ``channels`` channels in 8 bits: what :class:`Checkpoint` keeps."""
 
     __slots__ = ("tokens", "channels", "bytes", "buffer", "ptr", "home", "full")
+    _memory = ("buffer",)
 
     def __init__(self, tokens, channels, device="cuda"):
         n = ctypes.c_size_t()
         _check(lib().pulse_keep_sizes(KeepDesc(channels, 0, BF16), tokens, n))
         self.tokens, self.channels, self.bytes = tokens, channels, n.value
-        self.buffer = _bytes_at(max(n.value, 16), device)
-        self.ptr, self.home, self.full = self.buffer.data_ptr(), _home(self.buffer), False
+        self.buffer, self.full = _bytes_at(max(n.value, 16), device), False
+        self._locate()
+
+    def _locate(self):
+        self.ptr, self.home = self.buffer.data_ptr(), _home(self.buffer)
 
 
 class Checkpoint:
@@ -924,12 +983,14 @@ class Checkpoint:
         return out
 
 
-class Linear8:
+class Linear8(_Owner):
     """y = act(x W^T + bias) in 8-bit integers, for sampling: W (fp32 or bf16
     [outputs, inputs]) is laid out once, with a scale for each output channel; a
     call lays out x (bf16 [tokens, inputs]) with a scale for each token, and
     integer sums are exact.  ``bias``: fp32 [outputs], copied.  After the weights
     change, call :meth:`update`."""
+
+    _memory, _found = ("weights", "bias"), ("ptr", "bias_ptr", "home")
 
     def __init__(self, weight, bias=None, act=None):
         if weight.dim() != 2:
@@ -940,10 +1001,14 @@ class Linear8:
         _check(lib().pulse_lin8_sizes(self.desc, 0, n, None))
         self.packed, self.bytes, self.sizes = bytes(self.desc), n.value, {}
         self.weights = _bytes_at(n.value, weight.device)
-        self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
-        self.bias, self.bias_ptr = torch.empty(self.outputs, dtype=torch.float32,
-                                               device=weight.device), None
+        self.bias = torch.empty(self.outputs, dtype=torch.float32, device=weight.device)
+        self.biased = False
+        self._locate()
         self.update(weight, bias)
+
+    def _locate(self):
+        self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
+        self.bias_ptr = self.bias.data_ptr() if self.biased else None
 
     def update(self, weight, bias=None, stream=None):
         """Lay out other weights of the same shape, in place: captured calls take
@@ -962,7 +1027,8 @@ class Linear8:
                                      self.bytes, s))
         if bias is not None:
             self.bias.copy_(bias)
-        self.bias_ptr = None if bias is None else self.bias.data_ptr()
+        self.biased = bias is not None
+        self.bias_ptr = self.bias.data_ptr() if self.biased else None
 
     def _weights(self, dev, s):
         if self.weights.get_device() != dev:
