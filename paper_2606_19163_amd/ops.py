@@ -20,7 +20,8 @@ call refuses inputs that require a gradient where torch records one.  Work is
 enqueued on ``stream`` (default: torch's current one), and what a call allocates
 belongs to that stream.  An object may be used from several: the caller orders
 them, and the memory that an object holds is kept until all are done with it.
-Copies (copy, deepcopy, pickle) have memory of their own.
+Copies (copy, deepcopy, pickle) have memory of their own; a :class:`GradClip`,
+which knows its gradients by address, refuses to be copied.
 """
 
 from __future__ import annotations
@@ -639,6 +640,10 @@ class GradClip:
                 self.h = _vp()
         except Exception:
             pass
+
+    def __reduce_ex__(self, protocol):
+        # the handle is destroyed once, and its table names these very tensors
+        _bad("a GradClip cannot be copied: make one of the copied gradients")
 
     def run(self, max_norm, eps=1e-6, norm=None, stream=None):
         """Clip to ``max_norm``; returns the norm before it, fp32 [1].  Calls

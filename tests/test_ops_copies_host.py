@@ -114,3 +114,12 @@ def test_masks_of_inference_mode():
         mask = ops.Mask(8, docs=2, device="cpu")
         mask._built()
         copy.deepcopy(mask).check()
+
+
+@pytest.mark.parametrize("make", [copy.copy, copy.deepcopy, unpickled])
+def test_clips_are_not_copied(make):
+    """Two objects would destroy one handle.  Here it is NULL."""
+    clip = object.__new__(ops.GradClip)
+    clip.h, clip.grads, clip.outs = ops._vp(), [], []
+    with pytest.raises(ops.PulseError, match="cannot be copied"):
+        make(clip)
