@@ -238,7 +238,8 @@ pulse_status pulse_norm_sizes(const pulse_norm_desc* desc, int32_t tokens,
  *   h = x + r gate[d] Post(y)                  rounded to stream_dtype,
  *   u = Pre(h) (1 + scale[d]) + shift[d]       of h as rounded.
  * Padding takes no part: h = x, u = 0, and nothing there reaches a result
- * (x apart).  Statistics and sums are fp32.  h may be x itself and u may be y
+ * (x apart); a document without rows adds nothing to any gradient, whatever
+ * its conditions hold.  Statistics and sums are fp32.  h may be x itself and u may be y
  * itself (same pointer and stride); otherwise outputs must not overlap
  * inputs.  Without `branch` y and h are not used, without `pre` u is not
  * (NULL).  0 <= tokens <= 2^23. */

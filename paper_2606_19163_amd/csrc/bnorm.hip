@@ -345,6 +345,8 @@ struct DocOut {
     g = a.r * (a.gate ? a.gate[(long)d * a.gate_t + c] : 1.f);
     wp = a.post_weight ? a.post_weight[c] : 1.f;
   }
+  // a document without rows adds nothing, whatever its conditions hold
+  __device__ __forceinline__ void none() { w = b = s = g = wp = 0.f; }
   __device__ __forceinline__ void put(const NormArgs& a, const pulse_norm_grads& o, float* docsum,
                                       int d, int c, float p0, float p1, float p2) const {
     const long at = (long)d * a.C + c;
@@ -384,6 +386,9 @@ __global__ __launch_bounds__(256) void k_norm_many(NormArgs a, pulse_norm_grads 
   float4 p[3];
   p[0] = p[1] = p[2] = make_float4(0.f, 0.f, 0.f, 0.f);
   const int2 b = blocks_of(a, R, d);
+  if (b.y == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i].none();
   add_rows(p, part + ((long)b.x + d) * 3 * a.C + c, 3L * a.C, b.y, a.C, a.pre != 0,
            a.branch != 0);
   out[0].put(a, o, docsum, d, c, p[0].x, p[1].x, p[2].x);
@@ -408,6 +413,7 @@ __global__ __launch_bounds__(16 * K) void k_norm_docs(NormArgs a, pulse_norm_gra
   DocOut out{};
   if (mine) out.load(a, d, c);
   const int2 b = blocks_of(a, R, d);
+  if (b.y == 0) out.none();
   if (k < b.y && c4 < a.C)
     add_rows(p, part + ((long)b.x + k + d) * 3 * a.C + c4, (long)K * 3 * a.C,
              (b.y - k + K - 1) / K, a.C, a.pre != 0, a.branch != 0);
