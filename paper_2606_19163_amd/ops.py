@@ -112,7 +112,7 @@ _bound = None
 
 
 def lib():
-    global _bound
+    global _bound, _fast
     if _bound is None:
         L = _lib()
         st, hp, f = ctypes.c_int, ctypes.POINTER(Heads), ctypes.c_float
@@ -147,8 +147,7 @@ def lib():
         rp, sz, nd = ctypes.POINTER(Rows), ctypes.c_size_t, ctypes.POINTER(NormDesc)
         pp, gp = ctypes.POINTER(NormParams), ctypes.POINTER(NormGrads)
         kd, ld = ctypes.POINTER(KeepDesc), ctypes.POINTER(Lin8Desc)
-        global _fast
-        _fast = {}
+        fast = {}
         for name, args in (
                 ("norm_sizes", [nd, _i32, _szp]),
                 ("norm_forward", [nd, _i32, rp, rp, pp, rp, rp, _vp]),
@@ -169,7 +168,9 @@ def lib():
             fn = L["pulse_" + name]
             fn.argtypes = [a if a in (_i32, sz, _szp) else _vp for a in args]
             fn.restype = st
-            _fast[name] = fn
+            fast[name] = fn
+        # whole, and before any object can be made: another thread may be here too
+        _fast = fast
         _bound = L
     return _bound
 
