@@ -989,6 +989,9 @@ class Checkpoint:
         return out
 
 
+_SAME = object()  # Linear8.update: the bias stays
+
+
 class Linear8(_Owner):
     """y = act(x W^T + bias) in 8-bit integers, for sampling: W (fp32 or bf16
     [outputs, inputs]) is laid out once, with a scale for each output channel; a
@@ -1016,14 +1019,19 @@ class Linear8(_Owner):
         self.ptr, self.home = self.weights.data_ptr(), _home(self.weights)
         self.bias_ptr = self.bias.data_ptr() if self.biased else None
 
-    def update(self, weight, bias=None, stream=None):
-        """Lay out other weights of the same shape, in place: captured calls take
-        them too, where they have a bias or have none as before."""
+    def update(self, weight, bias=_SAME, stream=None):
+        """Lay out other weights of the same shape, in place, and copy another
+        ``bias``, if one is given: without it the layer keeps the one that it has,
+        and with None it has none from then on.  Captured calls take the new weights
+        too, and those captured with a bias the new bias (0 for none)."""
+        same = bias is _SAME
+        if same:
+            bias = None
         if _grad_on():
             _by_hand(("weight", weight), ("bias", bias))
         if stream is not None:
             with torch.cuda.stream(stream):
-                return self.update(weight, bias)
+                return self.update(weight, _SAME if same else bias)
         dev, s = _here()
         if tuple(weight.shape) != (self.outputs, self.inputs):
             _bad(f"weight is {tuple(weight.shape)}, expected {(self.outputs, self.inputs)}")
@@ -1031,8 +1039,12 @@ class Linear8(_Owner):
         _flat(bias, "bias", self.outputs, torch.float32, dev)
         _check(lib().pulse_lin8_pack(self.desc, at, _dtype(weight.dtype), self._weights(dev, s),
                                      self.bytes, s))
+        if same:
+            return
         if bias is not None:
             self.bias.copy_(bias)
+        elif self.biased:
+            self.bias.zero_()
         self.biased = bias is not None
         self.bias_ptr = self.bias.data_ptr() if self.biased else None
 
