@@ -42,7 +42,7 @@ pulse_status check_rows(const pulse_rows* x, const char* name, int tokens, int c
 struct Span {
   uintptr_t begin, end;
 };
-Span span_of(const pulse_rows* x, int tokens, int channels, int esz) {
+Span span_of(const pulse_rows* x, int tokens, int64_t channels, int esz) {
   if (!x || !tokens) return Span{0, 0};
   const uintptr_t p = reinterpret_cast<uintptr_t>(x->ptr);
   return Span{p, p + ((uintptr_t)(tokens - 1) * x->token_stride + channels) * esz};
@@ -61,7 +61,9 @@ bool apart(Span a, int64_t step_a, int64_t row_a, Span b, int64_t step_b, int64_
 struct View {
   const pulse_rows* x;
   const char* name;
-  int tokens, channels, esz;
+  int tokens;
+  int64_t channels;
+  int esz;
 };
 bool same(const View& a, const View& b) {
   return a.x->ptr == b.x->ptr && a.esz == b.esz &&
@@ -75,8 +77,8 @@ pulse_status check_apart(const View& out, const View& in, bool alias) {
     return v.tokens > 1 ? v.x->token_stride * v.esz : INT64_C(0);
   };
   if (!apart(span_of(out.x, out.tokens, out.channels, out.esz), step(out),
-             (int64_t)out.channels * out.esz, span_of(in.x, in.tokens, in.channels, in.esz),
-             step(in), (int64_t)in.channels * in.esz))
+             out.channels * out.esz, span_of(in.x, in.tokens, in.channels, in.esz), step(in),
+             in.channels * in.esz))
     return ofail(PULSE_E_INVALID_ARG, "%s overlaps %s", out.name, in.name);
   return PULSE_OK;
 }
@@ -179,9 +181,7 @@ struct Flat {
   View v;
   Flat(const void* p, size_t bytes, const char* name) : r(flat(p)) {
     // a span in units of 16 bytes, rounded up: kept rows are aligned to as much
-    v = View{&r, name, p && bytes ? 1 : 0, (int)((bytes + 15) / 16 > 0x7fffffff
-                                                    ? 0x7fffffff
-                                                    : (bytes + 15) / 16), 16};
+    v = View{&r, name, p && bytes ? 1 : 0, (int64_t)((bytes + 15) / 16), 16};
   }
   Flat(const Flat&) = delete;
 };
