@@ -222,7 +222,8 @@ typedef struct {
 } pulse_norm_params;
 
 /* The gradients of pulse_norm_params: fp32, contiguous, 16-byte aligned, each
- * NULL if not wanted.  They are overwritten.  dgate may be asked for without
+ * NULL if not wanted.  They are overwritten, and overlap neither one another nor
+ * anything that the call reads or writes.  dgate may be asked for without
  * a gate (that of a gate of 1), and so on. */
 typedef struct {
   float *dgate, *dscale, *dshift;         /* [docs][channels]                */

@@ -136,6 +136,44 @@ pulse_status check_params(const pulse_norm_desc* d, const pulse_norm_params* p) 
   return PULSE_OK;
 }
 
+// What a joint applies, and its gradients, as views (those that are not there have
+// no rows).
+struct ParamViews {
+  pulse_rows r[7];
+  View v[7];
+  ParamViews(const pulse_norm_desc* d, const pulse_norm_params* p) {
+    const int docs = d->docs;
+    const int64_t C = d->channels;
+    set(0, p->offsets, 0, "offsets", 1, (int64_t)docs + 1);
+    set(1, p->gate, p->gate_stride, "gate", docs, C);
+    set(2, p->scale, p->scale_stride, "scale", docs, C);
+    set(3, p->shift, p->shift_stride, "shift", docs, C);
+    set(4, p->weight, 0, "weight", 1, C);
+    set(5, p->bias, 0, "bias", 1, C);
+    set(6, p->post_weight, 0, "post_weight", 1, C);
+  }
+  ParamViews(const pulse_norm_desc* d, const pulse_norm_grads* g) {
+    const int64_t C = d->channels, many = C * d->docs;
+    set(0, g->dgate, 0, "dgate", 1, many);
+    set(1, g->dscale, 0, "dscale", 1, many);
+    set(2, g->dshift, 0, "dshift", 1, many);
+    set(3, g->dweight, 0, "dweight", 1, C);
+    set(4, g->dbias, 0, "dbias", 1, C);
+    set(5, g->dpost_weight, 0, "dpost_weight", 1, C);
+    set(6, nullptr, 0, "", 0, 0);
+  }
+  ParamViews(const ParamViews&) = delete;
+  void set(int i, const void* p, int64_t stride, const char* name, int rows, int64_t channels) {
+    r[i] = pulse_rows{const_cast<void*>(p), stride};
+    v[i] = View{&r[i], name, p ? rows : 0, channels, 4};
+  }
+};
+
+pulse_status check_apart(const View& out, const ParamViews& in) {
+  for (const View& v : in.v) OCHK(check_apart(out, v, false));
+  return PULSE_OK;
+}
+
 NormArgs norm_args(const pulse_norm_desc* d, int tokens, const pulse_norm_params* p) {
   NormArgs a{};
   a.tokens = tokens, a.C = d->channels, a.docs = d->docs;
@@ -263,7 +301,9 @@ pulse_status pulse_norm_forward(const pulse_norm_desc* desc, int32_t tokens, con
     OCHK(check_apart(vu, vx, false));
     OCHK(check_apart(vu, vy, true));
     OCHK(check_apart(vu, vh, false));
+    OCHK(check_apart(vu, ParamViews(desc, params)));
   }
+  OCHK(check_apart(vh, ParamViews(desc, params)));
   return launched(launch_norm_fwd(a, static_cast<hipStream_t>(stream)), "norm forward");
 }
 
@@ -321,6 +361,15 @@ pulse_status pulse_norm_backward(const pulse_norm_desc* desc, int32_t tokens, co
   OCHK(check_apart(vdy, vdh, false));
   OCHK(check_apart(vdy, vh, false));
   OCHK(check_ws(workspace, workspace_bytes, norm_bwd_bytes(*desc, tokens)));
+  const ParamViews in(desc, params), out(desc, grads);
+  OCHK(check_apart(vdx, in));
+  OCHK(check_apart(vdy, in));
+  for (int i = 0; i < 7; ++i) {
+    OCHK(check_apart(out.v[i], in));
+    for (const View* v : {&vdu, &vdh, &vh, &vy, &vdx, &vdy})
+      OCHK(check_apart(out.v[i], *v, false));
+    for (int j = 0; j < i; ++j) OCHK(check_apart(out.v[i], out.v[j], false));
+  }
   return launched(launch_norm_bwd(a, *grads, static_cast<float*>(workspace),
                                   static_cast<hipStream_t>(stream)),
                   "norm backward");

@@ -45,3 +45,51 @@ def test_large_kept_rows(at):
     for dw, db in ((at, None), (FREE << 1, at)):
         _refused(L.pulse_keep_wgrad(DESC, T, 64, R(FREE, 64), KEPT, n, dw, db, 0, ws, 1 << 40,
                                     None))
+
+
+# ---- norms: parameters and their gradients ------------------------------------------
+
+X, Y, H, U, DU, DH, DX, DY = ((1 << 32) + (i << 16) for i in range(8))
+GATE, SCALE, SHIFT, WEIGHT, BIAS, POST, OFF = ((1 << 33) + (i << 16) for i in range(7))
+DGATE, DSCALE, DSHIFT, DWEIGHT, DBIAS, DPOST = ((1 << 34) + (i << 16) for i in range(6))
+ROWS = dict(x=X, y=Y, h=H, u=U, du=DU, dh=DH, dx=DX, dy=DY)
+PARAMS = dict(offsets=OFF, gate=GATE, scale=SCALE, shift=SHIFT, weight=WEIGHT, bias=BIAS,
+              post_weight=POST)
+GRADS = dict(dgate=DGATE, dscale=DSCALE, dshift=DSHIFT, dweight=DWEIGHT, dbias=DBIAS,
+             dpost_weight=DPOST)
+TOKENS, DOCS, CH = 4, 3, 64
+
+
+def _norm(backward, at):
+    """Status of a call whose tensors lie at the addresses above, but for `at`."""
+    a = {**ROWS, **PARAMS, **GRADS, **at}
+    r = {k: R(a[k], CH) for k in ROWS}
+    desc = ops.NormDesc(CH, DOCS, 1, 2, 1, 1e-6, 1.0, S.BF16, S.BF16)
+    p = ops.NormParams(gate_stride=CH, scale_stride=CH, shift_stride=CH,
+                       **{k: a[k] for k in PARAMS})
+    if not backward:
+        return ops.lib().pulse_norm_forward(desc, TOKENS, r["x"], r["y"], p, r["h"], r["u"], None)
+    return ops.lib().pulse_norm_backward(desc, TOKENS, r["du"], r["dh"], r["h"], r["y"], p,
+                                         r["dx"], r["dy"],
+                                         ops.NormGrads(**{k: a[k] for k in GRADS}), 1 << 40,
+                                         1 << 30, None)
+
+
+@pytest.mark.parametrize("name", PARAMS)
+@pytest.mark.parametrize("backward,out", [(False, "h"), (False, "u"), (True, "dx"), (True, "dy")])
+def test_norm_outputs_and_parameters(backward, out, name):
+    row = 16 if name == "offsets" else 4 * CH if name.endswith(("weight", "bias")) else 12 * CH
+    for at in (ROWS[out], ROWS[out] + TOKENS * CH * 2 - 16, ROWS[out] - row + 16):
+        _refused(_norm(backward, {name: at}))
+
+
+@pytest.mark.parametrize("grad", GRADS)
+def test_norm_gradients(grad):
+    """The same memory twice, or that of a tensor the call reads or writes."""
+    for name, at in {**GRADS, **PARAMS, **{k: ROWS[k] for k in ("du", "dh", "h", "y", "dx",
+                                                                 "dy")}}.items():
+        if name != grad:
+            _refused(_norm(True, {grad: at}))
+            if name != "offsets":
+                _refused(_norm(True, {grad: at + 4 * CH - 16}))
+            _refused(_norm(True, {grad: at - 4 * CH + 16}))
