@@ -965,6 +965,8 @@ class Checkpoint:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.weight_grad(dy, kept, out, bias_out, accumulate)
+        if dy.dim() != 2:
+            _bad(f"dy is {tuple(dy.shape)}, expected [tokens, outputs]")
         dev, s = _here()
         n, m = dy.shape
         f32 = torch.float32
