@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void k_keep_save(KeepArgs a, int rows, uint32_
     keep8(v, q + (t * V + k) * 8, e + t * keep_exp_pitch(a.C) + (k >> 2), (k & 3) == 0);
     if (PUT && in) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = act_f<ACT>(v[i]);
+      for (int i = 0; i < 8; ++i) v[i] = act_f<ACT, T>(v[i]);
       put8(static_cast<T*>(a.y) + t * a.yt + 8 * k, v);
     }
   });
@@ -80,12 +80,12 @@ __global__ __launch_bounds__(256) void k_keep_back(KeepArgs a, int rows, uint32_
       Vec8<T> g;
       g.load(static_cast<const T*>(a.x) + t * a.xt + 8 * k);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = g.get(i) * act_d<ACT>(z[i]);
+      for (int i = 0; i < 8; ++i) v[i] = g.get(i) * act_d<ACT, T>(z[i]);
       put8(static_cast<T*>(a.y) + t * a.yt + 8 * k, v);
     }
     if (PUT) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = in ? act_f<ACT>(z[i]) : 0.f;
+      for (int i = 0; i < 8; ++i) z[i] = in ? act_f<ACT, T>(z[i]) : 0.f;
       keep8(z, q2 + (t * V + k) * 8, e2 + t * keep_exp_pitch(a.C) + (k >> 2), (k & 3) == 0);
     }
   });

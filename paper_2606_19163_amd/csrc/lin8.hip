@@ -160,7 +160,7 @@ __device__ __forceinline__ uint2 out4(i32x4_t acc, float sx, const Outs& o) {
     else
       z = ldexpf(z * __builtin_amdgcn_frexp_mantf(sx) * __builtin_amdgcn_frexp_mantf(o.s[i]),
                  __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(o.s[i]));
-    v[i] = act_f<ACT>(z + o.b[i]);
+    v[i] = act_f<ACT, uint16_t>(z + o.b[i]);
   }
   return uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
