@@ -9,15 +9,16 @@
 // reaches 2.4 at 16384^3.  Bound by the LDS-DMA, 48 KB per 2 x 128 x 256 x 64 and
 // CU, and the outputs' vector work (two dozen instructions each with GELU), which two
 // blocks per CU overlap.  Tried: 256 x 256 tiles of eight waves (117 us instead of
-// 107 in all then), fragments read a step ahead behind the MFMAs (even).  1 x 1408
+// 107 in all then), fragments read a step ahead behind the MFMAs (even), and in
+// flight unknown to the compiler (even, and no compiler promises their registers).  1 x 1408
 // x 8448: 4.2 us, 12 MB of weights at 2.8 TB/s, a launch's length.
+#include "ldscopy.hpp"
 #include "rowvec.hpp"
 
 namespace pulse {
 namespace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
 constexpr int FRAG = 1024;
 constexpr int ROWS = 256;  // rows of both operands are padded to whole tiles
@@ -267,38 +268,6 @@ struct Tile {
   static_assert(LDS <= 160 * 1024 && (STAGES - 2) * NU < 64, "LDS, vmcnt");
 };
 
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-}
-__device__ __forceinline__ void lgkm_wait0() {
-  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-}
-// ds_read_b128 at addr + OFF; inline, since the compiler would wait for the
-// LDS-DMA before it; the caller waits
-template <int OFF>
-__device__ __forceinline__ i32x4_t ds_rd128(uint32_t addr) {
-  i32x4_t v;
-  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
-  return v;
-}
-// N fragments, STEP apart
-template <int N, int STEP>
-__device__ __forceinline__ void ds_rd_n(i32x4_t* f, uint32_t addr) {
-  if constexpr (N > 0) {
-    ds_rd_n<N - 1, STEP>(f, addr);
-    f[N - 1] = ds_rd128<(N - 1) * STEP * FRAG>(addr);
-  }
-}
-__device__ __forceinline__ void tie(i32x4_t& v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ uint32_t lds_at(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
-}
-__device__ __forceinline__ int xcd_order(int b, int n) {
-  const int q = n >> 3, r = n & 7, x = b & 7;
-  return x * q + (x < r ? x : r) + (b >> 3);
-}
-
 template <class C, int ACT>
 __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, int tilesN,
                                                    int GT) {
@@ -324,31 +293,27 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
                         : w.frag + ((long)tn * C::FN + r - C::FT) * KS * FRAG) +
              f % C::KB * FRAG + lane * 16;
   }
+  const uint32_t sbase = lds_at(smem);
   auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < C::NU; ++u)
-      __builtin_amdgcn_global_load_lds(
-          src[u] + (long)kt * C::KB * FRAG,
-          (lds_ptr_t)(smem + stage * C::STAGE + (u * C::NW + wave) * FRAG), 16, 0, 0);
+      lds_copy16(src[u] + (long)kt * C::KB * FRAG,
+                 sbase + stage * C::STAGE + (u * C::NW + wave) * FRAG);
   };
   i32x4_t acc[C::TN][C::TT];
 #pragma unroll
   for (int j = 0; j < C::TN; ++j)
 #pragma unroll
     for (int i = 0; i < C::TT; ++i) acc[j][i] = i32x4_t{0, 0, 0, 0};
-  const uint32_t base = lds_at(smem) + lane * 16;
   i32x4_t fx[C::KB][C::TT], fw[C::KB][C::TN];
-  auto read = [&](uint32_t sb, auto tag) __attribute__((always_inline)) {
-    constexpr int P = decltype(tag)::value;
-    ds_rd_n<C::TT, C::KB>(fx[P], sb + (wt * C::TT * C::KB + P) * FRAG);
-    ds_rd_n<C::TN, C::KB>(fw[P], sb + ((C::FT + wn * C::TN) * C::KB + P) * FRAG);
-  };
-  auto arrive = [&](int P) __attribute__((always_inline)) {
-    lgkm_wait0();
+  auto read = [&](int stage, int P) __attribute__((always_inline)) {
+    const char* sb = smem + stage * C::STAGE + P * FRAG + lane * 16;
 #pragma unroll
-    for (int i = 0; i < C::TT; ++i) tie(fx[P][i]);
+    for (int i = 0; i < C::TT; ++i)
+      fx[P][i] = *reinterpret_cast<const i32x4_t*>(sb + (wt * C::TT + i) * C::KB * FRAG);
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) tie(fw[P][j]);
+    for (int j = 0; j < C::TN; ++j)
+      fw[P][j] = *reinterpret_cast<const i32x4_t*>(sb + (C::FT + wn * C::TN + j) * C::KB * FRAG);
   };
   auto mul = [&](int P) __attribute__((always_inline)) {
 #pragma unroll
@@ -362,26 +327,20 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
     if (i < KT) issue(i, i);
   int stage = 0;
   for (int kt = 0; kt < KT; ++kt) {
-    // this step's fragments are there: at most the later stages' loads are not
+    // this step's fragments are there: at most the later stages' copies are not
     if (kt + C::STAGES - 2 < KT)
-      wait_vmcnt<(C::STAGES - 2) * C::NU>();
+      lds_meet<(C::STAGES - 2) * C::NU>();
     else
-      wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
+      lds_meet<0>();
     if (kt + C::STAGES - 1 < KT)
       issue(kt + C::STAGES - 1, stage == 0 ? C::STAGES - 1 : stage - 1);
-    const uint32_t sb = base + stage * C::STAGE;
-    read(sb, std::integral_constant<int, 0>());
-    arrive(0);
-    if constexpr (C::KB == 2) {
-      read(sb, std::integral_constant<int, 1>());
-      mul(0);
-      __builtin_amdgcn_sched_barrier(0);
-      arrive(1);
-    }
-    mul(C::KB - 1);
+#pragma unroll
+    for (int P = 0; P < C::KB; ++P) read(stage, P);
+    // all reads are on their way before the first product: taken in turn by the
+    // compiler, 8192 x 5632 x 1408 takes 113 us instead of 109
     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int P = 0; P < C::KB; ++P) mul(P);
     stage = stage + 1 == C::STAGES ? 0 : stage + 1;
   }
   // lane: outputs 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16.  They
@@ -416,7 +375,8 @@ __global__ __launch_bounds__(C::NT, 2) void k_lin8(Lin8Args a, Laid x, Laid w, i
     else
       put(std::false_type());
   }
-  lgkm_wait0();
+  // a wave reads what it wrote itself
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 4
   for (int e = lane; e < C::WT * C::CPR; e += 64) {
     const int r = e / C::CPR, c = e % C::CPR;
