@@ -10,7 +10,7 @@ import pytest
 from test_host_sanitizers import ROOT
 
 CSRC = os.path.join(ROOT, "paper_2606_19163_amd", "csrc")
-SOURCES = ["lin8.hip", "ldscopy.hpp", "rowvec.hpp", "keepvec.hpp", "bnorm.hip", "keep.hip"]
+SOURCES = ["lin8.hip", "kgrad.hip", "ldscopy.hpp", "rowvec.hpp", "keepvec.hpp", "bnorm.hip", "keep.hip"]
 
 
 def inline_asm(text):
