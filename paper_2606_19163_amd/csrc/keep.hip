@@ -128,7 +128,9 @@ hipError_t launch_keep_save(const KeepArgs& a, hipStream_t st) {
   return by_kind(a, [&](auto t, auto act) {
     using T = decltype(t);
     constexpr int ACT = decltype(act)::value;
-    auto kern = a.y ? k_keep_save<T, ACT, true> : k_keep_save<T, PULSE_ACT_NONE, false>;
+    auto kern = k_keep_save<T, PULSE_ACT_NONE, false>;
+    if constexpr (ACT != PULSE_ACT_NONE)
+      if (a.y) kern = k_keep_save<T, ACT, true>;
     hipLaunchKernelGGL(kern, dim3(g.blocks), dim3(256), 0, st, a, g.rows, g.V, g.M,
                        static_cast<uint8_t*>(a.kept), exps(a, a.kept));
     return hipGetLastError();
@@ -150,11 +152,15 @@ hipError_t launch_keep_back(const KeepArgs& a, hipStream_t st) {
   return by_kind(a, [&](auto t, auto act) {
     using T = decltype(t);
     constexpr int ACT = decltype(act)::value;
-    auto kern = a.a_kept ? k_keep_back<T, ACT, true> : k_keep_back<T, ACT, false>;
-    hipLaunchKernelGGL(kern, dim3(g.blocks), dim3(256), 0, st, a, g.rows, g.V, g.M,
-                       static_cast<const uint8_t*>(a.kept), exps(a, a.kept),
-                       static_cast<uint8_t*>(a.a_kept), a.a_kept ? exps(a, a.a_kept) : nullptr);
-    return hipGetLastError();
+    if constexpr (ACT == PULSE_ACT_NONE) {
+      return hipErrorInvalidValue;
+    } else {
+      auto kern = a.a_kept ? k_keep_back<T, ACT, true> : k_keep_back<T, ACT, false>;
+      hipLaunchKernelGGL(kern, dim3(g.blocks), dim3(256), 0, st, a, g.rows, g.V, g.M,
+                         static_cast<const uint8_t*>(a.kept), exps(a, a.kept),
+                         static_cast<uint8_t*>(a.a_kept), a.a_kept ? exps(a, a.a_kept) : nullptr);
+      return hipGetLastError();
+    }
   });
 }
 

@@ -56,9 +56,6 @@ constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_HALF_MIRROR = 0x141, DPP_MIR
 struct Add {
   __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
-struct Max {
-  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
 
 // op over the 16 (32, 64) lanes that hold a row, the same on each: vector
 // instructions alone, where a shuffle would go through LDS
@@ -168,9 +165,9 @@ __device__ __forceinline__ float act_f(float z) {
 }
 template <int ACT, typename T>
 __device__ __forceinline__ float act_d(float z) {
+  static_assert(ACT == PULSE_ACT_GELU || ACT == PULSE_ACT_SILU, "there is an act");
   if constexpr (ACT == PULSE_ACT_GELU) return gelu_qd<T>(z);
-  if constexpr (ACT == PULSE_ACT_SILU) return silu_qd<T>(z);
-  return 1.f;
+  return silu_qd<T>(z);
 }
 
 }  // namespace pulse
