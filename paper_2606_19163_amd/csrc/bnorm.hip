@@ -4,7 +4,10 @@
 // A row lies in the registers of the lanes that share it, 8 channels each, so
 // that every tensor is read and written once; as many waves take a row as that
 // needs, since with 24 or 32 channels a lane the sums over rows that the backward
-// pass keeps beside the row spilled (83 us instead of 43 at 8192 x 1408 then).  Bound
+// pass keeps beside the row spilled (83 us instead of 43 at 8192 x 1408 then).  Only
+// the backward pass of an fp32 stream of more than 4096 channels does spill, 52 to 88
+// bytes a lane: its 16 waves have 128 registers each (1408 x 8192 70 us, where 2816 x
+// 4096 takes 47).  Bound
 // by memory: 8192 x 1408 in bf16 forward 19.6 us in the kernel (92 MB, 4.7 TB/s),
 // backward 32 (139 MB, 4.3) and 4.3 for the sums over blocks; 15795 x 1280 with an
 // fp32 stream and a norm on both sides 80 (365 MB, 4.6) + 5.1 + 4.7; a copy of 2
