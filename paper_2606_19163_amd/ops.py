@@ -283,7 +283,7 @@ class _Owner:
             # the copy reads it on the current stream
             if t.is_cuda and _raw_stream(t.get_device()) != self.home:
                 _used_on(t, t.get_device())
-        names = getattr(self, "__dict__", None) or self.__slots__
+        names = {*getattr(self, "__dict__", ()), *self.__slots__}
         return {k: getattr(self, k) for k in names if k not in self._found}
 
     def __setstate__(self, state):
