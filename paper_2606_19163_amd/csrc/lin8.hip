@@ -4,9 +4,10 @@
 // (l / 16) to + 15.  A tile in LDS is a list of fragments, which LDS-DMA copies
 // as they are and which reads without bank conflicts.
 //
-// 8192 x 1408 x 5632: laying out x 10 us (35 MB, bound by memory), the product 80
-// (1.6 POP/s) and with GELU 90; K of 5632 at 2.1 POP/s, where torch's int8 product
-// reaches 2.4 at 16384^3.  Bound by the LDS-DMA, 48 KB per 2 x 128 x 256 x 64 and
+// 8192 x 1408 x 5632: laying out x 11 us (35 MB, bound by memory), the product 84
+// (1.55 POP/s) and with GELU 103, traced (the least 76 and 92; a pass in a loop of such
+// takes 88 and 102 in all); K of 5632 at 2.1 POP/s, where torch's int8 product reaches
+// 2.4 at 16384^3.  Bound by the LDS-DMA, 48 KB per 2 x 128 x 256 x 64 and
 // CU, and the outputs' vector work (two dozen instructions each with GELU), which two
 // blocks per CU overlap.  Tried: 256 x 256 tiles of eight waves (117 us instead of
 // 107 in all then), fragments read a step ahead behind the MFMAs (even), and in
