@@ -123,3 +123,16 @@ def test_clips_are_not_copied(make):
     clip.h, clip.grads, clip.outs = ops._vp(), [], []
     with pytest.raises(ops.PulseError, match="cannot be copied"):
         make(clip)
+
+
+class Named(ops.Kept):
+    """A subclass with attributes beside the slots."""
+
+
+@pytest.mark.parametrize("make", [copy.copy, copy.deepcopy, unpickled])
+def test_subclasses(make):
+    kept = Named(3, 64, "cpu")
+    kept.name, kept.full = "u1", True
+    k = make(kept)
+    assert type(k) is Named and k.name == "u1" and k.full and k.tokens == 3
+    assert k.ptr == k.buffer.data_ptr() != kept.ptr
